@@ -330,6 +330,74 @@ int ec_row_entropy(const float *logits, int32_t rows, int32_t vocab, size_t ld, 
 int ec_row_entropy_noalloc(const float *logits, int32_t rows, int32_t vocab, size_t ld,
                            float *stats, void *hip_stream);
 
+/* Types of the tensors that the calls below take.  EC_T_MXFP4 is microscaled 4-bit floating point: 32 consecutive values of a
+ * row share a scale 2^(s - 127), s one byte (255: the block is NaN), and a value is a 4-bit e2m1 code (1 sign, 2 exponent bits with
+ * bias 1, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) times the scale.  Codes uint8 [rows, k/2], an even k in the low four bits;
+ * scales uint8 [rows, k/32]; both without gaps between rows. */
+enum { EC_T_F32 = 0, EC_T_BF16 = 1, EC_T_MXFP4 = 2 };
+
+/* How ec_row_sample draws.  temperature: finite, >= 0; 0 takes the most probable token (top_k 1 at temperature 1).  top_k: 0 or
+ * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all. */
+typedef struct {
+  float temperature;
+  int32_t top_k;
+  float top_p, min_p;
+} ec_sample_cfg;
+
+/* A token drawn from each row of a matrix of logits that sits on the device, from a given uniform number.  With
+ * e_i = exp((z_i - max z) / temperature), S the sum of all e and the tokens in the order (z descending, id ascending), a row keeps
+ * the token of rank j if  j < top_k;  the e of the ranks before j sum to less than top_p times the sum of the top_k e;
+ * e >= min_p;  z > -inf.  The token drawn is the lowest id for which the running sum of the kept e, in the order of the ids, exceeds u
+ * times the sum of all kept.  e is computed in 64 bits and all sums are exact sums of e rounded to multiples of 2^-46, so the result does not
+ * depend on the order of anything: the same arguments give the same bits.
+ *  logits     DEVICE [rows, vocab] of `type` (EC_T_F32 or EC_T_BF16), row stride ld elements (ld >= vocab); read only
+ *  rows       0 .. 65535; vocab 2 .. 163840
+ *  uniforms   DEVICE float32 [rows], u in [0, 1); below 0 and NaN count as 0, 1 and above as the largest float32 below 1
+ *  cfg        HOST, read before the call returns
+ *  tokens     DEVICE int32 [rows]; written.  -1 for a row that holds a NaN or has no finite maximum (all -inf, a +inf)
+ *  stats      DEVICE float32 [rows, 4], 16-byte aligned; written: the drawn token's probability among the kept tokens, its probability
+ *             e / S among all, how many are kept, the share of S that they hold.  NaN where the token is -1
+ *  workspace  DEVICE, 256-byte aligned, >= ec_row_sample_workspace_bytes(rows, vocab) (0 for arguments outside the limits); BORROWED for
+ *             the call: calls that overlap in time, and captured graphs that may run side by side, need one each
+ * Enqueues on hip_stream (NULL = default stream) and returns without synchronising; may be captured into a graph.
+ * Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP; ec_last_error(NULL) names the cause. */
+size_t ec_row_sample_workspace_bytes(int32_t rows, int32_t vocab);
+int ec_row_sample(const void *logits, int32_t type, int32_t rows, int32_t vocab, size_t ld, const float *uniforms,
+                  const ec_sample_cfg *cfg, int32_t *tokens, float *stats, void *workspace, size_t workspace_bytes,
+                  void *hip_stream);
+
+/* Matrices to EC_T_MXFP4 and back.  Each block's scale is the largest power of two that leaves its largest magnitude at 4 or more
+ * (floor(log2 max|x|) - 2, at least 2^-127); a value goes to the nearest code, ties to the even one, and to 6 beyond it.
+ * A block that holds an infinity or a NaN gets scale byte 255 and codes 0.  Back, every value is exact (s = 253 and 254 can overflow to an
+ * infinity).
+ *  x, out     DEVICE [rows, k] of `type` (EC_T_F32 or EC_T_BF16), row stride ld elements (ld >= k), aligned to its elements; columns
+ *             past k are neither read nor written
+ *  rows       0 .. 2^24; k a multiple of 32, at most 131072
+ *  codes      DEVICE, 16-byte aligned
+ * Enqueue on hip_stream and return without synchronising; may be captured.  Errors: EC_ERR_ARG, EC_ERR_HIP. */
+int ec_mx_quantize(const void *x, int32_t type, int64_t rows, int32_t k, size_t ld, uint8_t *codes, uint8_t *scales,
+                   void *hip_stream);
+int ec_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t k, void *out, int32_t type, size_t ld,
+                     void *hip_stream);
+
+/* y = x W^T for a matrix W [n, k] that was quantised, which ec_mx_pack lays out once as the product reads it (an EC_T_MXFP4
+ * matrix of any origin).  x is bfloat16, or EC_T_MXFP4 itself: then the products of codes run in 4 bits.  Products are exact, sums
+ * float32, and y is rounded once.
+ *  packed     DEVICE, 256-byte aligned, ec_mx_packed_bytes(n, k) (0 for arguments outside the limits)
+ *  x          DEVICE, 16-byte aligned; EC_T_BF16: [rows, k], row stride ld a multiple of 8 elements; EC_T_MXFP4: codes [rows, k/2], with
+ *             x_scales [rows, k/32] (x_scales is ignored for EC_T_BF16, ld for EC_T_MXFP4)
+ *  rows       0 .. 524288; n 1 .. 1048576; k a multiple of 32, at most 131072
+ *  y          DEVICE [rows, n] of y_type (EC_T_F32 or EC_T_BF16), row stride ldy elements, aligned to its elements; written, columns past
+ *             n are not
+ *  workspace  DEVICE, 256-byte aligned, >= ec_mx_linear_workspace_bytes(x_type, rows, n, k); BORROWED for the call, as ec_row_sample's
+ * Enqueue on hip_stream and return without synchronising; may be captured.  Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP. */
+size_t ec_mx_packed_bytes(int32_t n, int32_t k);
+int ec_mx_pack(const uint8_t *codes, const uint8_t *scales, int32_t n, int32_t k, void *packed, size_t packed_bytes,
+               void *hip_stream);
+size_t ec_mx_linear_workspace_bytes(int32_t x_type, int64_t rows, int32_t n, int32_t k);
+int ec_mx_linear(const void *x, const uint8_t *x_scales, int32_t x_type, int64_t rows, size_t ld, const void *packed, int32_t n,
+                 int32_t k, void *y, int32_t y_type, size_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Frees host-side state only; never frees weights or workspace.  NULL is allowed. */
 void ec_destroy(ec_ctx *ctx);
 

@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -24,6 +24,7 @@ EC_ERR_HOST_MEMORY = -6
 EC_ERR_NONFINITE = -7
 (EC_K_EMBED, EC_K_NORM, EC_K_QKV, EC_K_ROPE_KV, EC_K_ATTN, EC_K_OPROJ, EC_K_GATEUP, EC_K_SWIGLU,
  EC_K_DOWN, EC_K_LMHEAD, EC_K_VOCAB_REDUCE, EC_K_DECIDE, EC_K_COUNT) = range(13)
+EC_T_F32, EC_T_BF16, EC_T_MXFP4 = 0, 1, 2
 KERNEL_CLASS_NAMES = ["embed", "norm", "qkv", "rope_kv", "attn", "oproj", "gateup", "swiglu",
                       "down", "lmhead", "vocab_reduce", "decide"]
 (EC_DBG_LOGITS, EC_DBG_KCACHE, EC_DBG_VCACHE, EC_DBG_X, EC_DBG_MASKED, EC_DBG_HIST, EC_DBG_ROWS,
@@ -33,7 +34,9 @@ EXPORTS = ["ec_workspace_bytes", "ec_init", "ec_reset", "ec_step", "ec_step_forc
            "ec_step_forced_batch", "ec_generate", "ec_profile_enable", "ec_profile_read",
            "ec_debug_read", "ec_debug_read_seq", "ec_debug_block_shape", "ec_debug_attn_tiles", "ec_debug_meeting",
            "ec_destroy", "ec_strerror", "ec_last_error",
-           "ec_row_entropy_workspace_bytes", "ec_row_entropy", "ec_row_entropy_noalloc"]
+           "ec_row_entropy_workspace_bytes", "ec_row_entropy", "ec_row_entropy_noalloc",
+           "ec_row_sample_workspace_bytes", "ec_row_sample", "ec_mx_quantize", "ec_mx_dequantize",
+           "ec_mx_packed_bytes", "ec_mx_pack", "ec_mx_linear_workspace_bytes", "ec_mx_linear"]
 
 
 class ec_model_cfg(C.Structure):
@@ -77,6 +80,10 @@ class ec_step_result(C.Structure):
                 "n_recent_next": self.n_recent_next, "max_entropy": float(self.max_entropy),
                 "positions": list(self.positions[:n]), "tokens": list(self.tokens[:n]),
                 "entropy": list(self.entropy[:n]), "confidence": list(self.confidence[:n])}
+
+
+class ec_sample_cfg(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
 class ec_gen_stats(C.Structure):
@@ -140,6 +147,24 @@ def load_library() -> C.CDLL:
     lib.ec_row_entropy.argtypes = [vp, C.c_int32, C.c_int32, C.c_size_t, vp, vp, C.c_size_t, vp]
     lib.ec_row_entropy_noalloc.restype = C.c_int
     lib.ec_row_entropy_noalloc.argtypes = [vp, C.c_int32, C.c_int32, C.c_size_t, vp, vp]
+    lib.ec_row_sample_workspace_bytes.restype = C.c_size_t
+    lib.ec_row_sample_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+    lib.ec_row_sample.restype = C.c_int
+    lib.ec_row_sample.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, C.c_size_t, vp, C.POINTER(ec_sample_cfg),
+                                  vp, vp, vp, C.c_size_t, vp]
+    lib.ec_mx_quantize.restype = C.c_int
+    lib.ec_mx_quantize.argtypes = [vp, C.c_int32, C.c_int64, C.c_int32, C.c_size_t, vp, vp, vp]
+    lib.ec_mx_dequantize.restype = C.c_int
+    lib.ec_mx_dequantize.argtypes = [vp, vp, C.c_int64, C.c_int32, vp, C.c_int32, C.c_size_t, vp]
+    lib.ec_mx_packed_bytes.restype = C.c_size_t
+    lib.ec_mx_packed_bytes.argtypes = [C.c_int32, C.c_int32]
+    lib.ec_mx_pack.restype = C.c_int
+    lib.ec_mx_pack.argtypes = [vp, vp, C.c_int32, C.c_int32, vp, C.c_size_t, vp]
+    lib.ec_mx_linear_workspace_bytes.restype = C.c_size_t
+    lib.ec_mx_linear_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
+    lib.ec_mx_linear.restype = C.c_int
+    lib.ec_mx_linear.argtypes = [vp, vp, C.c_int32, C.c_int64, C.c_size_t, vp, C.c_int32, C.c_int32, vp, C.c_int32,
+                                 C.c_size_t, vp, C.c_size_t, vp]
     lib.ec_destroy.restype = None
     lib.ec_destroy.argtypes = [vp]
     lib.ec_strerror.restype = C.c_char_p
@@ -282,6 +307,173 @@ def row_entropy_noalloc(logits, stats, stream=None):
                                     _raw_stream(torch, stream, current))
     if rc != EC_OK:
         raise EcError(rc, lib.ec_last_error(None).decode())
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _place(stream, call, *tensors):
+    """Runs call() where the tensors are: on their device, and on `stream` if one is given, whose pool then owns what it
+    allocates and which is waited for (as row_entropy does); on the device's current stream otherwise."""
+    import torch
+    dev = tensors[0].get_device()
+    _need(dev >= 0 and all(t.get_device() == dev for t in tensors), "tensors must be on one GPU")
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _place(stream, call, *tensors)
+    if stream is None:
+        return call(_raw_stream(torch, None, dev))
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        out = call(_raw_stream(torch, None, dev))
+    stream.synchronize()
+    if stream != here:
+        for t in out if isinstance(out, tuple) else (out,):
+            if hasattr(t, "record_stream"):
+                t.record_stream(here)    # the caller goes on with it there
+    return out
+
+
+def _done(lib, rc: int) -> None:
+    if rc != EC_OK:
+        raise EcError(rc, lib.ec_last_error(None).decode())
+
+
+def _plain_type(dtype) -> int:
+    import torch
+    _need(dtype in (torch.float32, torch.bfloat16), "float32 or bfloat16 is needed")
+    return EC_T_F32 if dtype == torch.float32 else EC_T_BF16
+
+
+def _rows_of(x):
+    """rows, columns and row stride of a matrix whose columns are next to each other"""
+    _need(x.dim() == 2, "a matrix is needed")
+    rows, cols = x.shape
+    _need(x.stride(1) == 1 or cols <= 1, "the columns of a row must be next to each other")
+    ld = x.stride(0) if rows > 1 else cols
+    _need(ld >= cols, "rows must not overlap")
+    return rows, cols, ld
+
+
+def row_sample(logits, uniforms, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+               stream=None):
+    """ec_row_sample: a token drawn from each row of a float32 or bfloat16 CUDA matrix [rows, vocab], from the numbers
+    `uniforms` (float32 [rows], in [0, 1)).  Returns an int32 tensor [rows] of tokens and a float32 tensor [rows, 4]
+    (probability among the kept tokens, among all, number kept, share of the probability kept).  `stream` as for row_entropy."""
+    import torch
+    kind = _plain_type(logits.dtype)
+    rows, vocab, ld = _rows_of(logits)
+    _need(uniforms.dtype == torch.float32 and uniforms.shape == (rows,) and (rows <= 1 or uniforms.stride(0) == 1),
+          "uniforms must be float32 [rows]")
+    lib = _lib or load_library()
+    cfg = ec_sample_cfg(temperature, top_k, top_p, min_p)
+
+    def call(raw):
+        tokens = torch.empty((rows,), dtype=torch.int32, device=logits.device)
+        stats = torch.empty((rows, 4), dtype=torch.float32, device=logits.device)
+        size = lib.ec_row_sample_workspace_bytes(rows, vocab)
+        ws = torch.empty((max(size, 256),), dtype=torch.uint8, device=logits.device)
+        _done(lib, lib.ec_row_sample(logits.data_ptr(), kind, rows, vocab, ld, uniforms.data_ptr(), C.byref(cfg),
+                                     tokens.data_ptr(), stats.data_ptr(), ws.data_ptr(), size, raw))
+        return tokens, stats
+    return _place(stream, call, logits, uniforms)
+
+
+class Mxfp4(NamedTuple):
+    """A matrix in microscaled 4-bit floating point: uint8 codes [rows, k/2] (an even k in the low four bits) and uint8
+    scales [rows, k/32] (2^(s - 127) for 32 values; 255: NaN)."""
+    codes: object
+    scales: object
+
+
+class Mxfp4Matrix(NamedTuple):
+    """An n x k matrix as mxfp4_linear reads it."""
+    data: object
+    n: int
+    k: int
+
+
+def _mx_of(q):
+    import torch
+    codes, scales = q
+    _need(codes.dtype == torch.uint8 and scales.dtype == torch.uint8, "codes and scales must be uint8")
+    _need(codes.dim() == 2 and scales.dim() == 2 and codes.shape[0] == scales.shape[0] and
+          codes.shape[1] == 16 * scales.shape[1], "codes [rows, k/2] and scales [rows, k/32] are needed")
+    _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales must be contiguous")
+    return codes, scales, codes.shape[0], 2 * codes.shape[1]
+
+
+def mxfp4_quantize(x, stream=None) -> Mxfp4:
+    """ec_mx_quantize: a float32 or bfloat16 CUDA matrix [rows, k] (k a multiple of 32) in 4 bits."""
+    import torch
+    kind = _plain_type(x.dtype)
+    rows, k, ld = _rows_of(x)
+    lib = _lib or load_library()
+
+    def call(raw):
+        codes = torch.empty((rows, k // 2), dtype=torch.uint8, device=x.device)
+        scales = torch.empty((rows, k // 32), dtype=torch.uint8, device=x.device)
+        _done(lib, lib.ec_mx_quantize(x.data_ptr(), kind, rows, k, ld, codes.data_ptr(), scales.data_ptr(), raw))
+        return Mxfp4(codes, scales)
+    return _place(stream, call, x)
+
+
+def mxfp4_dequantize(q: Mxfp4, dtype=None, stream=None):
+    """ec_mx_dequantize: the values of a 4-bit matrix, float32 (the default) or bfloat16; exact in either."""
+    import torch
+    dtype = torch.float32 if dtype is None else dtype
+    kind = _plain_type(dtype)
+    codes, scales, rows, k = _mx_of(q)
+    lib = _lib or load_library()
+
+    def call(raw):
+        out = torch.empty((rows, k), dtype=dtype, device=codes.device)
+        _done(lib, lib.ec_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, out.data_ptr(), kind, k, raw))
+        return out
+    return _place(stream, call, codes, scales)
+
+
+def mxfp4_pack(q: Mxfp4, stream=None) -> Mxfp4Matrix:
+    """ec_mx_pack: lays a 4-bit matrix [n, k] out for mxfp4_linear, once."""
+    import torch
+    codes, scales, n, k = _mx_of(q)
+    lib = _lib or load_library()
+
+    def call(raw):
+        size = lib.ec_mx_packed_bytes(n, k)
+        data = torch.empty((max(size, 256),), dtype=torch.uint8, device=codes.device)
+        _done(lib, lib.ec_mx_pack(codes.data_ptr(), scales.data_ptr(), n, k, data.data_ptr(), size, raw))
+        return Mxfp4Matrix(data, n, k)
+    return _place(stream, call, codes, scales)
+
+
+def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
+    """ec_mx_linear: x W^T, float32 or bfloat16 (the default), for x a bfloat16 CUDA matrix [rows, k] (row stride a multiple
+    of 8 elements) or one in 4 bits (Mxfp4)."""
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    kind = _plain_type(dtype)
+    if isinstance(x, tuple):
+        codes, scales, rows, k = _mx_of(x)
+        tensors, x_kind, ld, x_scales = (codes, scales, w.data), EC_T_MXFP4, k, scales.data_ptr()
+    else:
+        _need(x.dtype == torch.bfloat16, "x must be bfloat16 or Mxfp4")
+        rows, k, ld = _rows_of(x)
+        ld = ld if rows > 1 else (k + 7) // 8 * 8
+        tensors, x_kind, x_scales = (x, w.data), EC_T_BF16, None
+    _need(k == w.k, "x has another k than the matrix")
+    lib = _lib or load_library()
+
+    def call(raw):
+        y = torch.empty((rows, w.n), dtype=dtype, device=w.data.device)
+        size = lib.ec_mx_linear_workspace_bytes(x_kind, rows, w.n, k)
+        ws = torch.empty((max(size, 256),), dtype=torch.uint8, device=w.data.device)
+        _done(lib, lib.ec_mx_linear(tensors[0].data_ptr(), x_scales, x_kind, rows, ld, w.data.data_ptr(), w.n, k,
+                                    y.data_ptr(), kind, w.n, ws.data_ptr(), size, raw))
+        return y
+    return _place(stream, call, *tensors)
 
 
 class EntropyCache:

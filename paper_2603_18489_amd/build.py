@@ -11,8 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libec.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 
-SOURCES = ["ec_api.hip", "ec_rowstats.hip", "k_glue.hip", "k_gemm_f32.hip", "k_gemm_bf16.hip", "k_attn.hip", "k_attn_mfma.hip",
-           "k_decide.hip"]
+SOURCES = ["ec_api.hip", "ec_rowstats.hip", "ec_operators.hip", "k_glue.hip", "k_gemm_f32.hip", "k_gemm_bf16.hip", "k_attn.hip", "k_attn_mfma.hip",
+           "k_decide.hip", "k_sample.hip", "k_mxfp4.hip"]
 FLAGS = ["-O3", *os.environ.get("EC_EXTRA_FLAGS", "").split(), "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function",
          # (some packed-fp32 forms the compiler makes of plain float code have given wrong results)
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -25,7 +25,7 @@ def _hipcc() -> str:
     return "hipcc"
 
 
-MFMA_SOURCES = ["k_gemm_bf16.hip", "k_attn_mfma.hip", "k_gemm_f32.hip", "k_attn.hip"]
+MFMA_SOURCES = ["k_gemm_bf16.hip", "k_attn_mfma.hip", "k_gemm_f32.hip", "k_attn.hip", "k_mxfp4.hip"]
 
 
 def check_no_masked_mfma(hipcc: str) -> None:

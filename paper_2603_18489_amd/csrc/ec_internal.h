@@ -265,6 +265,30 @@ void launch_vocab_reduce(const float* logits, int n_rows, int V, size_t ld, floa
 // n_rows * vocab_reduce_parts(V) tuples
 void launch_row_stats(const float* logits, int n_rows, int V, size_t ld, float4* partials,
                       float4* stats, hipStream_t s);
+
+// sampling (k_sample.hip)
+struct SampleArgs {
+  double scale;         // log2(e) / temperature
+  int top_k;            // 0: all
+  double top_p;
+  unsigned long long min_weight;   // least weight kept (the maximum's is 2^46)
+};
+// logits [rows, V] with row stride ld, float32 or bfloat16 -> a token id (-1: none) and (probability among the kept, among all,
+// number kept, share of the kept) a row
+void launch_sample_rows(const void* logits, bool bf16, int rows, int V, size_t ld, const float* uniforms, const SampleArgs& a,
+                        int* tokens, float4* stats, hipStream_t s);
+
+// microscaled 4-bit matrices (k_mxfp4.hip); kb: blocks of 32 along k
+__host__ __device__ inline int mx_tiles_of_k(int kb) { return (kb + 3) / 4; }
+size_t mx_packed_bytes(int n, int kb);
+void launch_mx_quantize(const void* x, bool bf16, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s);
+void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows, int kb, void* out, bool bf16, size_t ld,
+                          hipStream_t s);
+void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, uint8_t* packed, hipStream_t s);
+// x: bfloat16 rows, or codes where x_scales is given
+void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,
+                      bool y_bf16, size_t ldy, hipStream_t s);
+
 void launch_decide(const DecideArgs& a, int B, hipStream_t s);
 void launch_init_state(int* x, uint8_t* masked, int* hist, DevState* st, const int* prompt_dev,
                        int P, int N, int mask_id, hipStream_t s);
