@@ -280,14 +280,16 @@ void launch_sample_rows(const void* logits, bool bf16, int rows, int V, size_t l
 
 // microscaled 4-bit matrices (k_mxfp4.hip); kb: blocks of 32 along k
 __host__ __device__ inline int mx_tiles_of_k(int kb) { return (kb + 3) / 4; }
+constexpr size_t kMxGroupBytes = 4352;   // of 64 rows and 128 k: 4 KiB of codes, 256 bytes of scales
 size_t mx_packed_bytes(int n, int kb);
 void launch_mx_quantize(const void* x, bool bf16, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s);
 void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows, int kb, void* out, bool bf16, size_t ld,
                           hipStream_t s);
 void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, uint8_t* packed, hipStream_t s);
-// x: bfloat16 rows, or codes where x_scales is given
+// x: bfloat16 rows, or codes where x_scales is given; workspace: mx_linear_workspace bytes
+size_t mx_linear_workspace(bool x4, long M, int N, int kb);
 void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,
-                      bool y_bf16, size_t ldy, hipStream_t s);
+                      bool y_bf16, size_t ldy, void* workspace, hipStream_t s);
 
 void launch_decide(const DecideArgs& a, int B, hipStream_t s);
 void launch_init_state(int* x, uint8_t* masked, int* hist, DevState* st, const int* prompt_dev,

@@ -132,7 +132,7 @@ int ec_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t n, int32_t k
 
 size_t ec_mx_linear_workspace_bytes(int32_t x_type, int64_t rows, int32_t n, int32_t k) {
   if ((x_type != EC_T_BF16 && x_type != EC_T_MXFP4) || rows < 0 || rows > kMxLinearRowsMax || !ec_mx_packed_bytes(n, k)) return 0;
-  return 256;
+  return mx_linear_workspace(x_type == EC_T_MXFP4, rows, n, k / 32);
 }
 
 int ec_mx_linear(const void* x, const uint8_t* x_scales, int32_t x_type, int64_t rows, size_t ld, const void* packed, int32_t n,
@@ -155,7 +155,7 @@ int ec_mx_linear(const void* x, const uint8_t* x_scales, int32_t x_type, int64_t
   if (workspace_bytes < ec_mx_linear_workspace_bytes(x_type, rows, n, k))
     return op_fail(EC_ERR_WORKSPACE, "workspace smaller than ec_mx_linear_workspace_bytes()");
   launch_mx_linear(x, x_type == EC_T_MXFP4 ? x_scales : nullptr, rows, ld, (const uint8_t*)packed, n, k / 32, y,
-                   y_type == EC_T_BF16, ldy, (hipStream_t)hip_stream);
+                   y_type == EC_T_BF16, ldy, workspace, (hipStream_t)hip_stream);
   return op_done("product kernel");
 }
 

@@ -5,8 +5,8 @@
 // low four bits, scales [rows, k/32].
 //
 // Laid out for the products ("packed"): tiles of 16 rows x 128 k.  Of a tile lane g*16 + r holds row r's block g, k = 32 g .. 32 g + 31:
-// 16 bytes of codes, so that a wave-wide load is one KiB, and one byte of scale.  Four tiles in a row along k have their scales in one
-// dword a lane, tile t's in byte t.  Codes [tile row][tile of k][lane][16], then scales [tile row][4 tiles of k][lane][4].
+// 16 bytes of codes, so that a wave-wide load is one KiB, and one byte of scale.  Four tiles of rows make a group: at each 128 k a
+// group has its codes [tile][lane][16], then its scales [lane][tile], 4352 bytes; groups go [64 rows][128 k].
 #include "ec_internal.h"
 
 namespace ec {
@@ -81,91 +81,453 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __res
 
 // one thread a block of 32 of the packed matrix; past the matrix' rows and k: zeros
 __global__ __launch_bounds__(256) void mx_pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int n,
-                                                      int kb, int nt, int kq4, uint8_t* __restrict__ packed) {
+                                                      int kb, long total, uint8_t* __restrict__ packed) {
   const long i = (long)blockIdx.x * 256 + threadIdx.x;
-  const int kq = mx_tiles_of_k(kb);
-  if (i >= (long)nt * kq4 * 4 * 64) return;
-  const int lane = (int)(i & 63);
-  const long t = i >> 6;
-  const int tile = (int)(t / (kq4 * 4)), q = (int)(t % (kq4 * 4));
-  const int row = tile * 16 + (lane & 15), b = q * 4 + (lane >> 4);
+  if (i >= total) return;
+  const int kq = mx_tiles_of_k(kb), lane = (int)(i & 63), t = (int)(i >> 6) & 3;
+  const long part = i >> 8;                        // group and 128 k
+  const int group = (int)(part / kq), q = (int)(part - (long)group * kq);
+  const int row = group * 64 + t * 16 + (lane & 15), b = q * 4 + (lane >> 4);
   const bool in = row < n && b < kb;
   const size_t from = (size_t)row * kb + b;
-  if (q < kq) {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (in) v = *(const uint4*)(codes + from * 16);
-    *(uint4*)(packed + (((size_t)tile * kq + q) * 64 + lane) * 16) = v;
-  }
-  uint8_t* sc = packed + (size_t)nt * kq * 1024;
-  sc[(((size_t)tile * kq4 + (q >> 2)) * 64 + lane) * 4 + (q & 3)] = in ? scales[from] : (uint8_t)127;
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (in) v = *(const uint4*)(codes + from * 16);
+  uint8_t* to = packed + (size_t)part * kMxGroupBytes;
+  *(uint4*)(to + t * 1024 + lane * 16) = v;
+  to[4096 + lane * 4 + t] = in ? scales[from] : (uint8_t)127;
 }
 
 // ---- product ------------------------------------------------------------------------------------
 struct MxProduct {
   const void* x;             // bf16 [M, K] with row stride ld, or codes [M, K/2]
-  const uint8_t* x_scales;   // [M, K/32]
+  const uint8_t* x_scales;   // [M, scale_ld]
   size_t ld;
+  int scale_ld;
   const uint8_t* w;          // packed
-  long M;
-  int N, kb;                 // rows of W; blocks of 32 along k
+  int M, N, kb;              // rows of x and of W; blocks of 32 along k
   void* y; size_t ldy;
+  int wide;                  // y takes the four features of a lane in one store
+  uint8_t* spread;           // room for the scales of 4-bit rows in whole dwords
+  float* parts; int part_ld; // where K is split over blocks: their sums, [ranges][M][part_ld]; else NULL
 };
+constexpr int kMxParts = 4;  // most ranges
+constexpr int kMxSplitRows = 1024;   // rows up to which K may be split
 
-// One wave a 16 x 16 tile of the result, all of K.
-template <bool X4, typename TY>
-__global__ __launch_bounds__(64) void mx_product_simple_kernel(MxProduct p) {
-  const int lane = threadIdx.x, g = lane >> 4, r = lane & 15;
-  const int kq = mx_tiles_of_k(p.kb), kq4 = (kq + 3) / 4, nt = (p.N + 15) / 16;
-  const int tile = blockIdx.x;
-  const long row0 = (long)blockIdx.y * 16, row = row0 + r;
-  const bool row_in = row < p.M;
-  const u32x4* wc = (const u32x4*)p.w + (size_t)tile * kq * 64 + lane;
-  const uint32_t* ws = (const uint32_t*)(p.w + (size_t)nt * kq * 1024) + (size_t)tile * kq4 * 64 + lane;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int q = 0; q < kq; ++q) {
-    const u32x4 c = wc[(size_t)q * 64];
-    const uint32_t s = ws[(size_t)(q >> 2) * 64] >> ((q & 3) * 8) & 255u;
-    const int b = q * 4 + g;                       // the lane's block
-    const bool in = row_in && b < p.kb;
-    if constexpr (X4) {
-      u32x4 v = {0u, 0u, 0u, 0u};
-      uint32_t sx = 127;
-      if (in) {
-        v = *(const u32x4*)((const uint8_t*)p.x + ((size_t)row * p.kb + b) * 16);
-        sx = p.x_scales[(size_t)row * p.kb + b];
-      }
-      const i32x8 a = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
-      const i32x8 bb = {(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, bb, acc, 4, 4, 0, s, 0, sx);
-    } else {
-      const float f = mx_to_values(s);
+// 8 codes as 8 bf16 values, exactly (scale: the bits of 2^(s - 127))
+__device__ __forceinline__ bf16x8 mx_widen(uint32_t codes, float scale) {
+  union { bf16x2 h[4]; bf16x8 v; } w;
+  w.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+  w.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+  w.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+  w.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+  return w.v;
+}
+__device__ __forceinline__ i32x8 mx_operand(u32x4 v) {
+  return (i32x8){(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+}
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) {
+  union { u32x4 u; bf16x8 b; } c;
+  c.u = v;
+  return c.b;
+}
+
+// features n .. n + 3 of row m
+template <typename TY>
+__device__ __forceinline__ void mx_store(const MxProduct& p, int m, int n, f32x4 v) {
+  TY* y = (TY*)p.y + (size_t)m * p.ldy + n;
+  if (p.wide) {
+    if (n < p.N) {   // (N is a multiple of 4)
+      if constexpr (sizeof(TY) == 4) *(float4*)y = make_float4(v[0], v[1], v[2], v[3]);
+      else *(uint2*)y = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+    }
+  } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        union { bf16x2 h[4]; bf16x8 v; } w;
-        w.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 0);
-        w.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 1);
-        w.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 2);
-        w.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 3);
-        union { u32x4 u; bf16x8 v; } x = {};
-        if (in) x.u = *(const u32x4*)((const bf16_t*)p.x + (size_t)row * p.ld + (size_t)b * 32 + j * 8);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v, x.v, acc, 0, 0, 0);
+    for (int i = 0; i < 4; ++i)
+      if (n + i < p.N) store_f32(y + i, v[i]);
+  }
+}
+
+enum { MX_RING = 0, MX_REGS = 1, MX_X4 = 2 };   // where a wave's rows go: bf16 to LDS or to registers, 4-bit ones to registers
+
+// Few rows: a stream of W.  A block owns NTW tiles of 16 features, all MT tiles of 16 rows and one of gridDim.y ranges of K; its KS
+// waves share that out, and their sums meet in LDS in the order of the waves.  What a wave multiplies next is on its way while
+// it multiplies: R sets of operands, W in registers, bf16 rows by direct loads to a ring in LDS of the wave's own (which takes no
+// registers and no barrier): rows of 256 bytes, their 16-byte chunks at their number XOR the row, so that 16 rows read at the same k hit all banks.
+template <int XF, typename TY, int MT, int NTW, int KS>
+__global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
+  constexpr int R = 2;
+  constexpr bool X4 = XF == MX_X4, RING = XF == MX_RING;
+  extern __shared__ f32x4 red[];   // the rings; then [KS][NTW * MT][64]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+  const int kq = mx_tiles_of_k(p.kb), groups = (p.N + 63) / 64, tile0 = blockIdx.x * NTW;
+  const int klo = (int)((long)blockIdx.y * kq / gridDim.y), kn = (int)((long)(blockIdx.y + 1) * kq / gridDim.y) - klo;
+  const int lo = klo + (int)((long)wave * kn / KS), n = klo + (int)((long)(wave + 1) * kn / KS) - lo;
+  const uint8_t* wp[NTW];
+#pragma unroll
+  for (int i = 0; i < NTW; ++i) {
+    const int t = tile0 + i < groups * 4 ? tile0 + i : 0;   // (a tile past the end is not stored)
+    wp[i] = p.w + ((size_t)(t >> 2) * kq + lo) * kMxGroupBytes + (t & 3) * 1024 + lane * 16;
+  }
+  // A tile's scale is the byte of its number in its group's dword; NTW tiles lie in GW groups.
+  constexpr int GW = NTW == 1 ? 1 : (NTW + 5) / 4 < (NTW + 3) / 4 ? 1 : NTW % 4 ? (NTW + 5) / 4 : NTW / 4;
+  static_assert(NTW == 1 || NTW == 2 || NTW == 4 || NTW == 6 || NTW == 8, "the bytes below");
+  const uint8_t* sp[GW];
+#pragma unroll
+  for (int i = 0; i < GW; ++i) {
+    const int gr = (tile0 >> 2) + i < groups ? (tile0 >> 2) + i : 0;
+    sp[i] = p.w + ((size_t)gr * kq + lo) * kMxGroupBytes + 4096 + lane * 4;
+  }
+  const int first_byte = tile0 & 3;
+  // To registers: the lane's own row of each tile.  To LDS: the row of which the lane brings 16 bytes, four rows a load.
+  constexpr int XL = RING ? MT * 4 : MT, XN = X4 ? 1 : 4;
+  const char* xp[XL];
+  const uint8_t* xs[MT];
+#pragma unroll
+  for (int j = 0; j < XL; ++j) {
+    const int row = RING ? j * 4 + g : j * 16 + r, m = row < p.M ? row : 0;
+    xp[j] = X4 ? (const char*)p.x + (size_t)m * p.kb * 16 : (const char*)p.x + (size_t)m * p.ld * 2;
+    if constexpr (X4) xs[j] = p.x_scales + (size_t)m * p.scale_ld;
+  }
+  char* ring = (char*)red + wave * (R * MT * 4096);
+
+  f32x4 acc[NTW][MT];
+#pragma unroll
+  for (int i = 0; i < NTW; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+  struct Set {
+    u32x4 w[NTW], x[RING ? 1 : MT][XN];
+    uint32_t ws[GW], xs[X4 ? MT : 1];
+  } set[R];
+  constexpr int LOADS = NTW + GW + 4 * MT;   // of a set, where there is a ring
+  // Blocks past K: their codes in W are 0; x is read where there is some, and set to 0 below.
+  auto load = [&](int s, int it) {
+    const int step = it < n ? it : n - 1, q = lo + step;
+    if constexpr (!RING) {
+      const int blk = min(q * 4 + g, p.kb - 1);
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+#pragma unroll
+        for (int h = 0; h < XN; ++h) set[s].x[j][h] = *(const u32x4*)(xp[j] + (size_t)blk * (XN * 16) + h * 16);
+        if constexpr (X4) set[s].xs[j] = xs[j][blk];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < XL; ++j) {
+        int c = r ^ ((j * 4 + g) & 15);
+        c = q * 4 + (c >> 2) < p.kb ? c : 0;
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(xp[j] + (size_t)q * 256 + c * 16),
+                                         (void __attribute__((address_space(3)))*)(ring + s * (MT * 4096) + j * 1024), 16, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NTW; ++i) set[s].w[i] = __builtin_nontemporal_load((const u32x4*)(wp[i] + (size_t)step * kMxGroupBytes));
+#pragma unroll
+    for (int i = 0; i < GW; ++i) set[s].ws[i] = *(const uint32_t*)(sp[i] + (size_t)step * kMxGroupBytes);
+  };
+  auto mma = [&](int s, int it) {
+    const bool tail = (lo + it + 1) * 4 > p.kb, in = (lo + it) * 4 + g < p.kb;
+    uint32_t sc[NTW > 4 ? 2 : 1];
+    if constexpr (NTW == 8) { sc[0] = set[s].ws[0]; sc[1] = set[s].ws[1]; }
+    else if constexpr (NTW == 6) {
+      sc[0] = __builtin_amdgcn_alignbyte(set[s].ws[1], set[s].ws[0], first_byte);
+      sc[1] = set[s].ws[1] >> (8 * first_byte);
+    } else {
+      sc[0] = set[s].ws[0] >> (8 * first_byte);
+    }
+    if constexpr (!RING) {
+      if (tail) {
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+#pragma unroll
+          for (int h = 0; h < XN; ++h) set[s].x[j][h] = in ? set[s].x[j][h] : (u32x4){0u, 0u, 0u, 0u};
+          if constexpr (X4) set[s].xs[j] = in ? set[s].xs[j] : 127u;
+        }
+      }
+    }
+    if constexpr (X4) {
+#pragma unroll
+      for (int i = 0; i < NTW; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          const i32x8 w = mx_operand(set[s].w[i]), x = mx_operand(set[s].x[j][0]);
+          const int a = (int)sc[i >> 2], b = (int)set[s].xs[j];
+          if ((i & 3) == 0) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[i][j], 4, 4, 0, a, 0, b);
+          else if ((i & 3) == 1) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[i][j], 4, 4, 1, a, 0, b);
+          else if ((i & 3) == 2) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[i][j], 4, 4, 2, a, 0, b);
+          else acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[i][j], 4, 4, 3, a, 0, b);
+        }
+    } else {
+      float f[NTW];
+#pragma unroll
+      for (int i = 0; i < NTW; ++i) f[i] = mx_to_values(sc[i >> 2] >> (8 * (i & 3)) & 255u);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        u32x4 x[MT];
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          if constexpr (RING) x[j] = *(const u32x4*)(ring + s * (MT * 4096) + (j * 16 + r) * 256 + ((g * 4 + h) ^ r) * 16);
+          else x[j] = set[s].x[j][h];
+        }
+        if (RING && tail)
+#pragma unroll
+          for (int j = 0; j < MT; ++j) x[j] = in ? x[j] : (u32x4){0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < NTW; ++i) {
+          const bf16x8 w = mx_widen(set[s].w[i][h], f[i]);
+#pragma unroll
+          for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, as_bf16x8(x[j]), acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+  };
+  if (n > 0) {
+#pragma unroll
+    for (int s = 0; s < R - 1; ++s) load(s, s);
+    for (int it = 0;; it += R) {
+      bool done = false;
+#pragma unroll
+      for (int s = 0; s < R; ++s) {
+        if (!done) {
+          // (a slot of the ring is filled again once its reads have been waited for, by the products before this)
+          load((s + R - 1) % R, it + s + R - 1);
+          if constexpr (RING) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((R - 1) * LOADS) : "memory");
+          __builtin_amdgcn_sched_barrier(0);
+          mma(s, it + s);
+          __builtin_amdgcn_sched_barrier(0);
+          done = it + s + 1 >= n;
+        }
+      }
+      if (done) break;
+    }
+  }
+  constexpr int UNITS = NTW * MT;
+  if constexpr (RING) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last loads to the ring, asked for but not used)
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < NTW; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) red[(wave * UNITS + i * MT + j) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  for (int o = threadIdx.x; o < UNITS * 64; o += KS * 64) {
+    f32x4 v = red[o];
+#pragma unroll
+    for (int w = 1; w < KS; ++w) v += red[w * UNITS * 64 + o];
+    const int l = o & 63, unit = o >> 6, i = unit / MT, m = (unit - i * MT) * 16 + (l & 15), f = (tile0 + i) * 16 + (l >> 4) * 4;
+    if (m < p.M) {
+      if (p.parts) {
+        if (f < p.N) *(f32x4*)(p.parts + ((size_t)blockIdx.y * p.M + m) * p.part_ld + f) = v;
+      } else {
+        mx_store<TY>(p, m, f, v);
       }
     }
   }
-  // the lane holds features 4 g .. 4 g + 3 of the tile for its row r
-  if (row_in)
+}
+
+// Many rows: 8 waves (WM x WN), a wave WTM tiles of 16 rows x 64 features.  QS steps of 128 k are a stage; S stages are in LDS, brought there by direct
+// loads, one barrier a stage.  W lies there as it is packed.  Rows of bf16 (256 bytes a step) and of codes (128 bytes, two steps)
+// have their 16-byte chunks at their number XOR the row, so that rows read at the same k hit all banks; the scales of 4-bit rows go
+// [step][row], four bytes each.
+template <bool X4, int WM, int WN, int WTM> struct MxTile {
+  static constexpr int BM = WM * WTM * 16, BN = WN * 64, QS = X4 ? 2 : 1;
+  static constexpr int XB = BM * (X4 ? 128 : 256), SB = X4 ? BM * 8 : 0, WB = WN * QS * (int)kMxGroupBytes;
+  static constexpr int STAGE = XB + SB + WB;
+  static constexpr int S = STAGE * 3 <= 160 * 1024 ? 3 : 2;
+};
+template <bool X4, typename TY, int WM, int WN, int WTM>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void mx_tiled_kernel(MxProduct p) {
+  typedef MxTile<X4, WM, WN, WTM> T;
+  static_assert(WM * WN == 8, "eight waves");
+  constexpr int QS = T::QS, S = T::S;
+  extern __shared__ char lds_[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+  const int wm = wave / WN, wn = wave % WN;
+  const int kq = mx_tiles_of_k(p.kb), groups = (p.N + 63) / 64;
+  const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
+  // An XCD takes a run of the blocks in an order that goes down 8 blocks of rows, then on along the features: what its 32 compute
+  // units work on at a time shares rows and features.
+  int bx, by;
+  {
+    const int nb = gx * gy, xcd = blockIdx.x & 7;
+    const int j = xcd * (nb >> 3) + min(xcd, nb & 7) + (blockIdx.x >> 3);
+    const int panel = j / (8 * gx), high = min(8, gy - panel * 8), in = j - panel * 8 * gx;
+    by = panel * 8 + in % high;
+    bx = in / high;
+  }
+  const int m0 = by * T::BM, group0 = bx * WN;
+  const int st_all = (kq + QS - 1) / QS;
+  const int st_lo = (int)((long)blockIdx.y * st_all / gridDim.y), ns = (int)((long)(blockIdx.y + 1) * st_all / gridDim.y) - st_lo;
+
+  // loads of a stage: rows, then W, whole waves of 16 bytes a lane; what does not divide over the waves is shared by all of them
+  constexpr int XL = T::XB / 1024 / 8, WU = T::WB / 16, WL = WU / 512, REST = WU % 512 / 8, UN = QS * 272;
+  static_assert(T::XB % 8192 == 0 && WU % 8 == 0 && (REST == 0 || 64 % REST == 0), "whole loads, and as many lanes of one for each wave");
+  const char* xsrc[XL];
+  int xchunk[XL];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = tile * 16 + g * 4 + i;
-      if (n < p.N) store_f32((TY*)p.y + (size_t)row * p.ldy + n, acc[i]);
+  for (int i = 0; i < XL; ++i) {
+    const int u = (i * 8 + wave) * 64 + lane, row = X4 ? u >> 3 : u >> 4;
+    const int m = min(m0 + row, p.M - 1);
+    xchunk[i] = X4 ? (u & 7) ^ (row & 7) : (u & 15) ^ (row & 15);
+    xsrc[i] = X4 ? (const char*)p.x + (size_t)m * p.kb * 16 : (const char*)p.x + (size_t)m * p.ld * 2;
+  }
+  auto w_unit = [&](int u, int& q) {   // where unit u of a stage's W comes from, at step 0
+    const int gr = u / UN, off = u - gr * UN, group = group0 + gr < groups ? group0 + gr : 0;
+    q = QS == 2 && off >= 272;
+    return (const char*)p.w + (size_t)group * kq * kMxGroupBytes + (size_t)(off - q * 272) * 16;
+  };
+  const char* wsrc[WL + (REST > 0)];
+  int wq[WL + (REST > 0)];
+#pragma unroll
+  for (int i = 0; i < WL; ++i) wsrc[i] = w_unit((i * 8 + wave) * 64 + lane, wq[i]);
+  const int rest0 = wave * REST, rest_load = WL * 8 + (rest0 >> 6);
+  const bool rest_mine = lane >= (rest0 & 63) && lane < (rest0 & 63) + REST;
+  if constexpr (REST > 0) wsrc[WL] = w_unit(min(rest_load * 64 + lane, WU - 1), wq[WL]);
+  // scales of 4-bit rows: a dword a row and step
+  constexpr int SLOADS = X4 ? QS * T::BM / 64 : 0, SL = (SLOADS + 7) / 8;
+  const uint8_t* ssrc[SL > 0 ? SL : 1];
+  int sat[SL > 0 ? SL : 1];
+#pragma unroll
+  for (int i = 0; i < SL; ++i) {
+    const int l = (i * 8 + wave) % (SLOADS ? SLOADS : 1);   // (brought twice where there are fewer than waves)
+    sat[i] = l;
+    ssrc[i] = p.x_scales + (size_t)min(m0 + (l % (T::BM / 64)) * 64 + lane, p.M - 1) * p.scale_ld;
+  }
+  constexpr int LOADS = XL + WL + (REST > 0) + SL;
+  auto load = [&](int stage) {
+    const int st = st_lo + min(stage, ns - 1), q0 = st * QS;
+    char* to = lds_ + (stage % S) * T::STAGE;
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      int b = X4 ? q0 * 4 + xchunk[i] : q0 * 4 + (xchunk[i] >> 2);   // (past K: read something that is there, and see below)
+      b = b < p.kb ? b : q0 * 4;
+      const char* from = xsrc[i] + (X4 ? (size_t)b * 16 : (size_t)b * 64 + (xchunk[i] & 3) * 16);
+      __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)from,
+                                       (void __attribute__((address_space(3)))*)(to + (i * 8 + wave) * 1024), 16, 0, 0);
     }
+#pragma unroll
+    for (int i = 0; i < SL; ++i) {
+      const int q = min(q0 + sat[i] / (T::BM / 64), kq - 1);
+      __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(ssrc[i] + (size_t)q * 4),
+                                       (void __attribute__((address_space(3)))*)(to + T::XB + sat[i] * 256), 4, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < WL + (REST > 0); ++i) {
+      const int q = min(q0 + wq[i], kq - 1), l = i < WL ? i * 8 + wave : rest_load;
+      const char* from = wsrc[i] + (size_t)q * kMxGroupBytes;
+      const auto slot = (void __attribute__((address_space(3)))*)(to + T::XB + T::SB + l * 1024);
+      if (i < WL) __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)from, slot, 16, 0, 0);
+      else if (rest_mine) __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)from, slot, 16, 0, 0);
+    }
+  };
+
+  f32x4 acc[4][WTM];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < WTM; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) load(s);
+  for (int s = 0; s < ns; ++s) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LOADS) : "memory");
+    char* at = lds_ + (s % S) * T::STAGE;
+    if (!X4 && (st_lo + s + 1) * 4 > p.kb) {   // bf16 past K: zeros, by the wave that brought them
+#pragma unroll
+      for (int i = 0; i < XL; ++i)
+        if ((st_lo + s) * 4 + (xchunk[i] >> 2) >= p.kb) *(u32x4*)(at + (i * 8 + wave) * 1024 + lane * 16) = (u32x4){0u, 0u, 0u, 0u};
+    }
+    block_barrier_nofence();
+    load(s + S - 1);
+    const char* wl = at + T::XB + T::SB + wn * QS * (int)kMxGroupBytes;
+#pragma unroll
+    for (int q = 0; q < QS; ++q) {
+      if (QS == 2 && q == 1 && (st_lo + s) * 2 + 1 >= kq) break;
+      u32x4 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = *(const u32x4*)(wl + q * kMxGroupBytes + i * 1024 + lane * 16);
+      const uint32_t ws = *(const uint32_t*)(wl + q * kMxGroupBytes + 4096 + lane * 4);
+      if constexpr (X4) {
+#pragma unroll
+        for (int j = 0; j < WTM; ++j) {
+          const int row = (wm * WTM + j) * 16 + r;
+          const i32x8 x = mx_operand(*(const u32x4*)(at + row * 128 + (((q * 4 + g) ^ (row & 7)) * 16)));
+          const int xs = (int)(*(const uint32_t*)(at + T::XB + (q * T::BM + row) * 4) >> (8 * g));
+          acc[0][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(w[0]), x, acc[0][j], 4, 4, 0, (int)ws, 0, xs);
+          acc[1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(w[1]), x, acc[1][j], 4, 4, 1, (int)ws, 0, xs);
+          acc[2][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(w[2]), x, acc[2][j], 4, 4, 2, (int)ws, 0, xs);
+          acc[3][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand(w[3]), x, acc[3][j], 4, 4, 3, (int)ws, 0, xs);
+        }
+      } else {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = mx_to_values(ws >> (8 * i) & 255u);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          bf16x8 x[WTM];
+#pragma unroll
+          for (int j = 0; j < WTM; ++j)
+            x[j] = as_bf16x8(*(const u32x4*)(at + ((wm * WTM + j) * 16 + r) * 256 + ((g * 4 + h) ^ r) * 16));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bf16x8 v = mx_widen(w[i][h], f[i]);
+#pragma unroll
+            for (int j = 0; j < WTM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, x[j], acc[i][j], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last loads, asked for but not used)
+#pragma unroll
+  for (int j = 0; j < WTM; ++j) {
+    const int m = m0 + (wm * WTM + j) * 16 + r;
+    if (m < p.M) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int f = (group0 + wn) * 64 + i * 16 + g * 4;
+        if (p.parts) {
+          if (f < p.N) *(f32x4*)(p.parts + ((size_t)blockIdx.y * p.M + m) * p.part_ld + f) = acc[i][j];
+        } else {
+          mx_store<TY>(p, m, f, acc[i][j]);
+        }
+      }
+    }
+  }
+}
+
+// scales of 4-bit rows with whole dwords a row: [M][kq][4], 127 past K
+__global__ __launch_bounds__(256) void mx_spread_scales_kernel(const uint8_t* __restrict__ scales, long total, int kb, int kq,
+                                                               uint32_t* __restrict__ out) {
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= total) return;
+  const long m = i / kq;
+  const int q = (int)(i - m * kq);
+  uint32_t v = 0;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) v |= (q * 4 + t < kb ? (uint32_t)scales[(size_t)m * kb + q * 4 + t] : 127u) << (8 * t);
+  out[i] = v;
+}
+
+// y = the sum of the parts, in their order.  Four features a thread.
+template <typename TY>
+__global__ __launch_bounds__(256) void mx_join_kernel(MxProduct p, int parts) {
+  const int f = (blockIdx.x * 256 + threadIdx.x) * 4, m = blockIdx.y;
+  if (f >= p.N) return;
+  const float* from = p.parts + (size_t)m * p.part_ld + f;
+  f32x4 v[kMxParts];
+#pragma unroll
+  for (int z = 0; z < kMxParts; ++z) v[z] = *(const f32x4*)(from + (size_t)(z < parts ? z : 0) * p.M * p.part_ld);
+#pragma unroll
+  for (int z = 1; z < kMxParts; ++z)
+    if (z < parts) v[0] += v[z];
+  mx_store<TY>(p, m, f, v[0]);
 }
 
 // ---- launchers ------------------------------------------------------------------------------------
-size_t mx_packed_bytes(int n, int kb) {
-  const size_t nt = (n + 15) / 16, kq = mx_tiles_of_k(kb), kq4 = (kq + 3) / 4;
-  return nt * kq * 1024 + nt * kq4 * 256;
-}
+size_t mx_packed_bytes(int n, int kb) { return (size_t)((n + 63) / 64) * mx_tiles_of_k(kb) * kMxGroupBytes; }
 
 void launch_mx_quantize(const void* x, bool bf16, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s) {
   const unsigned grid = (unsigned)((rows * kb + 255) / 256);
@@ -181,20 +543,150 @@ void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows
 }
 
 void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, uint8_t* packed, hipStream_t s) {
-  const int nt = (n + 15) / 16, kq4 = (mx_tiles_of_k(kb) + 3) / 4;
-  mx_pack_kernel<<<(unsigned)(((long)nt * kq4 * 4 * 64 + 255) / 256), 256, 0, s>>>(codes, scales, n, kb, nt, kq4, packed);
+  const long total = (long)((n + 63) / 64) * mx_tiles_of_k(kb) * 256;
+  mx_pack_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(codes, scales, n, kb, total, packed);
+}
+
+constexpr int mx_rows_lds(int xf, int mt, int ntw, int ks) {
+  const int ring = xf == MX_RING ? ks * 2 * mt * 4096 : 0, sums = ks * ntw * mt * 1024;
+  return ring > sums ? ring : sums;
+}
+template <int XF, typename TY, int MT, int NTW, int KS>
+static void launch_rows_t(const MxProduct& p, int parts, hipStream_t s) {
+  constexpr int smem = mx_rows_lds(XF, MT, NTW, KS);
+  static_assert(smem <= 160 * 1024, "the rings and the waves' sums fit the LDS");
+  if constexpr (smem > 48 * 1024) {
+    static const hipError_t once = hipFuncSetAttribute((const void*)mx_rows_kernel<XF, TY, MT, NTW, KS>,
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    (void)once;
+  }
+  const int tiles = (p.N + 15) / 16;
+  MxProduct q = p;
+  if (parts == 1) q.parts = nullptr;
+  mx_rows_kernel<XF, TY, MT, NTW, KS><<<dim3((tiles + NTW - 1) / NTW, parts), KS * 64, smem, s>>>(q);
+  if (parts > 1) mx_join_kernel<TY><<<dim3((p.N + 1023) / 1024, p.M), 256, 0, s>>>(p, parts);
+}
+
+// Tiles of features to a block and ranges of K.  A compute unit pulls about 50 KB/us in these kernels, so that what counts is what goes
+// through the busiest of the 256: its blocks' shares of W and, once a block, the rows; a join of K's ranges is another 3.5 us.
+struct MxRowsShape { int ntw, parts; };
+static MxRowsShape pick_rows(bool x4, int M, int N, int kb) {
+  const int tiles = (N + 15) / 16, rows = (M + 3) / 4 * 4;
+  MxRowsShape best = {1, 1};
+  double least = 1e30;
+  for (const int ntw : {1, 2, 4, 6, 8})
+    for (const int parts : {1, 2, 4}) {
+      if (parts > 1 && mx_tiles_of_k(kb) < 8 * parts) continue;
+      const int blocks = (tiles + ntw - 1) / ntw * parts;
+      const double kbytes = (ntw * 16 * 17.0 + rows * (x4 ? 17.0 : 64.0)) * kb / parts / 1000;
+      const double us = (blocks + 255) / 256 * kbytes / 50 + (parts > 1 ? 3.5 : 0);
+      if (us < least) { least = us; best = {ntw, parts}; }
+    }
+  return best;
+}
+template <int XF, typename TY, int MT>
+static void launch_rows_mt(const MxProduct& p, hipStream_t s) {
+  const MxRowsShape w = pick_rows(XF == MX_X4, p.M, p.N, p.kb);
+  // (eight waves where a compute unit has one block, and LDS for it)
+  const bool eight = MT == 1 && ((p.N + 15) / 16 + w.ntw - 1) / w.ntw * w.parts <= 256;
+  constexpr int K1 = mx_rows_lds(XF, MT, 1, 8) <= 160 * 1024 ? 8 : 4, E = MT == 1 ? 8 : 4;
+  switch (w.ntw) {
+    case 1: launch_rows_t<XF, TY, MT, 1, K1>(p, w.parts, s); break;
+    case 2: if (eight) launch_rows_t<XF, TY, MT, 2, E>(p, w.parts, s); else launch_rows_t<XF, TY, MT, 2, 4>(p, w.parts, s); break;
+    case 4: if (eight) launch_rows_t<XF, TY, MT, 4, E>(p, w.parts, s); else launch_rows_t<XF, TY, MT, 4, 4>(p, w.parts, s); break;
+    case 6: if (eight) launch_rows_t<XF, TY, MT, 6, E>(p, w.parts, s); else launch_rows_t<XF, TY, MT, 6, 4>(p, w.parts, s); break;
+    default: if (eight) launch_rows_t<XF, TY, MT, 8, E>(p, w.parts, s); else launch_rows_t<XF, TY, MT, 8, 4>(p, w.parts, s); break;
+  }
+}
+
+template <bool X4, typename TY, int WM, int WN, int WTM>
+static void launch_tiled_t(const MxProduct& p, int parts, hipStream_t s) {
+  typedef MxTile<X4, WM, WN, WTM> T;
+  constexpr int smem = T::STAGE * T::S;
+  static_assert(smem <= 160 * 1024, "the stages fit the LDS");
+  static const hipError_t once = hipFuncSetAttribute((const void*)mx_tiled_kernel<X4, TY, WM, WN, WTM>,
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  (void)once;
+  MxProduct q = p;
+  if (parts == 1) q.parts = nullptr;
+  const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
+  mx_tiled_kernel<X4, TY, WM, WN, WTM><<<dim3(gx * gy, parts), 512, smem, s>>>(q);
+  if (parts > 1) mx_join_kernel<TY><<<dim3((p.N + 1023) / 1024, p.M), 256, 0, s>>>(p, parts);
+}
+
+// Rows x features of a block and ranges of K, by what its rounds of 256 blocks take.  us a stage (128 k of bf16 rows, 256 k of 4-bit ones) and beside
+// the stages, from whole products of K 4096:
+//   bf16   128 x 256 1.65   64 x 256 1.05   128 x 128 1.05   (256 x 128 1.9: never the least)
+//   4 bits 128 x 256 1.60   64 x 256 1.00   128 x 128 1.00   256 x 256 2.75
+struct MxTiledShape { int shape, parts; };
+static MxTiledShape pick_tiled(bool x4, int M, int N, int kb) {
+  static const int bm[4] = {128, 64, 128, 256}, bn[4] = {256, 256, 128, 256};
+  static const double stage_us[2][4] = {{1.65, 1.05, 1.05, 1e9}, {1.6, 1.0, 1.0, 2.75}};
+  const int stages = x4 ? (mx_tiles_of_k(kb) + 1) / 2 : mx_tiles_of_k(kb);
+  MxTiledShape best = {0, 1};
+  double least = 1e30;
+  for (int shape = 0; shape < (x4 ? 4 : 3); ++shape)
+    for (const int parts : {1, 2, 4}) {
+      if (parts > 1 && (M > kMxSplitRows || stages < 4 * parts)) continue;
+      const long blocks = (long)((M + bm[shape] - 1) / bm[shape]) * ((N + bn[shape] - 1) / bn[shape]) * parts;
+      const double us = (double)((blocks + 255) / 256) * (((stages + parts - 1) / parts) * stage_us[x4][shape] + 3) +
+                        (parts > 1 ? 4 + (parts + 1) * 4.0 * M * N / 4e6 : 0);
+      if (us < least) { least = us; best = {shape, parts}; }
+    }
+  return best;
+}
+template <bool X4, typename TY>
+static void launch_tiled(const MxProduct& p, hipStream_t s) {
+  const MxTiledShape w = pick_tiled(X4, p.M, p.N, p.kb);
+  if (w.shape == 0) launch_tiled_t<X4, TY, 2, 4, 4>(p, w.parts, s);
+  else if (w.shape == 1) launch_tiled_t<X4, TY, 2, 4, 2>(p, w.parts, s);
+  else if (w.shape == 2) launch_tiled_t<X4, TY, 4, 2, 2>(p, w.parts, s);
+  else if constexpr (X4) launch_tiled_t<X4, TY, 2, 4, 8>(p, w.parts, s);
+}
+
+constexpr int kMxFewRows = 64;   // up to here W is streamed past all rows at once
+template <bool X4, typename TY>
+static void launch_linear_t(const MxProduct& p, hipStream_t s) {
+  constexpr int XF = X4 ? MX_X4 : MX_RING;
+  switch ((p.M + 15) / 16) {
+    case 1: if (p.M <= 4) launch_rows_mt<X4 ? MX_X4 : MX_REGS, TY, 1>(p, s); else launch_rows_mt<XF, TY, 1>(p, s); break;
+    case 2: launch_rows_mt<XF, TY, 2>(p, s); break;
+    case 3: launch_rows_mt<XF, TY, 3>(p, s); break;
+    case 4: launch_rows_mt<XF, TY, 4>(p, s); break;
+    default: {
+      MxProduct q = p;
+      if (X4 && (p.kb % 4 || (uintptr_t)p.x_scales % 4)) {
+        const int kq = mx_tiles_of_k(p.kb);
+        const long total = (long)p.M * kq;
+        mx_spread_scales_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(p.x_scales, total, p.kb, kq, (uint32_t*)p.spread);
+        q.x_scales = p.spread;
+        q.scale_ld = kq * 4;
+      }
+      launch_tiled<X4, TY>(q, s);
+    }
+  }
+}
+
+// parts' sums [ranges][M][N], then the scales of 4-bit rows in whole dwords
+static size_t mx_parts_bytes(long M, int N) {
+  if (M > kMxSplitRows) return 0;
+  return ((size_t)kMxParts * M * ((N + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256;
+}
+size_t mx_linear_workspace(bool x4, long M, int N, int kb) {
+  const size_t need = mx_parts_bytes(M, N) + (x4 && M > kMxFewRows ? (size_t)M * mx_tiles_of_k(kb) * 4 : 0);
+  return need < 256 ? 256 : need;
 }
 
 void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,
-                      bool y_bf16, size_t ldy, hipStream_t s) {
-  const MxProduct p = {x, x_scales, ld, packed, M, N, kb, y, ldy};
-  const dim3 grid((N + 15) / 16, (unsigned)((M + 15) / 16));
+                      bool y_bf16, size_t ldy, void* workspace, hipStream_t s) {
+  const int wide = N % 4 == 0 && ldy % 4 == 0 && (uintptr_t)y % (y_bf16 ? 8 : 16) == 0;
+  const MxProduct p = {x, x_scales, ld, kb, packed, (int)M, N, kb, y, ldy, wide, (uint8_t*)workspace + mx_parts_bytes(M, N), (float*)workspace, (N + 3) / 4 * 4};
   if (x_scales) {
-    if (y_bf16) mx_product_simple_kernel<true, bf16_t><<<grid, 64, 0, s>>>(p);
-    else mx_product_simple_kernel<true, float><<<grid, 64, 0, s>>>(p);
+    if (y_bf16) launch_linear_t<true, bf16_t>(p, s);
+    else launch_linear_t<true, float>(p, s);
   } else {
-    if (y_bf16) mx_product_simple_kernel<false, bf16_t><<<grid, 64, 0, s>>>(p);
-    else mx_product_simple_kernel<false, float><<<grid, 64, 0, s>>>(p);
+    if (y_bf16) launch_linear_t<false, bf16_t>(p, s);
+    else launch_linear_t<false, float>(p, s);
   }
 }
 
