@@ -268,7 +268,7 @@ void launch_row_stats(const float* logits, int n_rows, int V, size_t ld, float4*
 
 // sampling (k_sample.hip)
 struct SampleArgs {
-  double scale;         // log2(e) / temperature
+  double scale, per_z;  // log2(e) / temperature; 16 / temperature
   int top_k;            // 0: all
   double top_p;
   unsigned long long min_weight;   // least weight kept (the maximum's is 2^46)
@@ -276,7 +276,8 @@ struct SampleArgs {
 // logits [rows, V] with row stride ld, float32 or bfloat16 -> a token id (-1: none) and (probability among the kept, among all,
 // number kept, share of the kept) a row
 void launch_sample_rows(const void* logits, bool bf16, int rows, int V, size_t ld, const float* uniforms, const SampleArgs& a,
-                        int* tokens, float4* stats, hipStream_t s);
+                        int* tokens, float4* stats, void* workspace, hipStream_t s);
+size_t sample_workspace(int rows, int V);
 
 // microscaled 4-bit matrices (k_mxfp4.hip); kb: blocks of 32 along k
 __host__ __device__ inline int mx_tiles_of_k(int kb) { return (kb + 3) / 4; }

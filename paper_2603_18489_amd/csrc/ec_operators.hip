@@ -71,16 +71,18 @@ int ec_row_sample(const void* logits, int32_t type, int32_t rows, int32_t vocab,
   const bool greedy = cfg->temperature == 0.f;
   SampleArgs a;
   a.scale = 1.4426950408889634 / (greedy ? 1.0 : (double)cfg->temperature);
-  a.top_k = greedy ? 1 : cfg->top_k;
+  a.per_z = 16.0 / (greedy ? 1.0 : (double)cfg->temperature);
+  a.top_k = greedy ? 1 : cfg->top_k < vocab ? cfg->top_k : 0;
   a.top_p = cfg->top_p;
-  a.min_weight = (unsigned long long)std::ceil((double)cfg->min_p * 0x1p46);
-  launch_sample_rows(logits, type == EC_T_BF16, rows, vocab, ld, uniforms, a, tokens, (float4*)stats, (hipStream_t)hip_stream);
+  a.min_weight = cfg->min_p > 0.f ? (unsigned long long)std::ceil(std::fmax((double)cfg->min_p, 0x1p-45) * 0x1p46) : 0;
+  launch_sample_rows(logits, type == EC_T_BF16, rows, vocab, ld, uniforms, a, tokens, (float4*)stats, workspace,
+                     (hipStream_t)hip_stream);
   return op_done("sampling kernels");
 }
 
 size_t ec_row_sample_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 0 || rows > kSampleRowsMax || vocab < 2 || vocab > kVocabMax) return 0;
-  return 256;
+  return sample_workspace(rows, vocab);
 }
 
 int ec_mx_quantize(const void* x, int32_t type, int64_t rows, int32_t k, size_t ld, uint8_t* codes, uint8_t* scales,
