@@ -8,6 +8,8 @@
 // would pick a neighbour in per cents of the rows.  So e is a 64-bit exponential, rounded to a multiple of 2^-46, and every sum is
 // one of integers: exact, independent of the order, below 2^64 for the 163840 tokens a row may have.  (64-bit multiply-adds run at
 // the rate of 32-bit ones that are not packed.)
+#include <stddef.h>
+
 #include "ec_internal.h"
 #include "k_exp.h"
 
@@ -15,7 +17,7 @@ namespace ec {
 
 typedef unsigned long long u64;
 
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 512;
 constexpr int kSampleWaves = kSampleThreads / 64;
 
 // logits in order: larger for larger z, -0 and +0 the same
@@ -53,7 +55,7 @@ struct SampleRow {
   __device__ __forceinline__ u64 weight(float z) const { return exp2_fixed46(((double)z - m) * scale); }
 };
 
-// What a block of 1024 threads works through, in the order of the ids: each wave has a range of its own, 64 neighbours at a time.
+// What a block of 512 threads works through, in the order of the ids: each wave has a range of its own, 64 neighbours at a time.
 // each(f): f(place, logit, there) for the lane's elements; a place that is not there has a logit of -inf.
 template <int NE> struct InRegisters {
   float v[NE];
@@ -93,8 +95,26 @@ template <typename T> struct InMemory {
   }
 };
 
+struct InList {   // (logit, id) in LDS; places are those in the list
+  const int2* list;
+  int first, end, n;
+  __device__ __forceinline__ void fetch(const int2* from, int count) {
+    list = from; n = count;
+    const int per = ((n + kSampleWaves - 1) / kSampleWaves + 63) / 64 * 64, lo = min((int)(threadIdx.x >> 6) * per, n);
+    first = lo + (threadIdx.x & 63);
+    end = min(lo + per, n);
+  }
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+    const int rounds = (end - (first - (int)(threadIdx.x & 63)) + 63) / 64;
+    for (int e = 0; e < rounds; ++e) {
+      const int at = first + e * 64;
+      f(at, at < end ? __int_as_float(list[at].x) : -INFINITY, at < end);
+    }
+  }
+};
+
 // LDS of a block that looks for the cut
-constexpr int kDigits = 2048;
+constexpr int kDigits = 1024;
 struct Scratch {
   u64 mass[kDigits];
   uint32_t cnt[kDigits];
@@ -166,9 +186,100 @@ __device__ __forceinline__ void clear_bins(Scratch& x) {
   __syncthreads();
 }
 
+// The same among up to 64 tokens that x.few has.  Every wave ranks them, a lane each, by key, then place.  Returns what is kept.
+__device__ __forceinline__ u64 rank_few(uint32_t n, uint32_t above_cnt, u64 above_mass, bool by_mass, u64 want, Cut& cut, Scratch& x) {
+  __syncthreads();
+  const int lane = threadIdx.x & 63, mine = lane < (int)n ? lane : 0;
+  const uint32_t key = x.few_key[mine];
+  const int place = x.few_place[mine];
+  uint32_t rank = above_cnt;
+  u64 mass = above_mass;
+  for (int j = 0; j < (int)n; ++j) {
+    const bool ahead = x.few_key[j] > key || (x.few_key[j] == key && x.few_place[j] < place);
+    rank += ahead;
+    mass += ahead ? x.few_mass[j] : 0;
+  }
+  const u64 upto = mass + x.few_mass[mine];
+  const u64 is = __builtin_amdgcn_ballot_w64(lane < (int)n && (by_mass ? mass < want && want <= upto : rank + 1 == (uint32_t)want));
+  // (sums by bins and by tokens differ by roundings: a wanted weight past the last token's means the last)
+  const u64 last = __builtin_amdgcn_ballot_w64(lane < (int)n && rank + 1 == above_cnt + n);
+  const int l = __builtin_ctzll(is ? is : last);
+  cut.key = (uint32_t)__builtin_amdgcn_readlane((int)key, l);
+  cut.last = __builtin_amdgcn_readlane(place, l);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(upto >> 32), l), lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)upto, l);
+  return (u64)hi << 32 | lo;
+}
+
+// The cut among the tokens for which in(z) holds; above_cnt, above_mass: of those ahead of them all.  Their keys' range in kDigits equal
+// pieces, then the piece of the cut, until a piece is one key.  Returns what is kept.
+template <typename S, typename P>
+__device__ u64 select_digits(const S& src, const SampleRow& row, bool by_mass, u64 want, uint32_t above_cnt, u64 above_mass, P in_set, Cut& cut,
+                             Scratch& x) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t high = 0, low = ~0u;
+  src.each([&](int, float v, bool) {
+    if (v > -INFINITY && in_set(v)) {
+      const uint32_t k = key_of(v);
+      high = max(high, k);
+      low = min(low, k);
+    }
+  });
+  // (both at once as maxima)
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { high = max(high, (uint32_t)__shfl_xor((int)high, o, 64)); low = min(low, (uint32_t)__shfl_xor((int)low, o, 64)); }
+  __syncthreads();
+  if (lane == 0) x.wsum[wave] = (u64)high << 32 | low;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSampleWaves; ++w) { high = max(high, (uint32_t)(x.wsum[w] >> 32)); low = min(low, (uint32_t)x.wsum[w]); }
+  uint32_t span = high - low;   // of the keys from `high` down
+  for (;;) {
+    const int shift = max(0, 22 - __builtin_clz(span | 1));   // (span >> shift < kDigits)
+    clear_bins(x);
+    src.each([&](int, float v, bool) {
+      const uint32_t k = key_of(v);
+      if (v > -INFINITY && in_set(v) && k <= high && high - k <= span) {
+        const uint32_t b = (high - k) >> shift;
+        atomicAdd(&x.cnt[b], 1u);
+        atomicAdd(&x.mass[b], row.weight(v));
+      }
+    });
+    __syncthreads();
+    find_bin(by_mass, want, above_cnt, above_mass, x);
+    high -= x.found_bin << shift;
+    above_cnt = x.found_above_cnt;
+    above_mass = x.found_above_mass;
+    if (shift == 0) break;
+    span = (1u << shift) - 1;
+  }
+  const uint32_t prefix = high;
+  const u64 each = x.found_mass / x.found_cnt;   // (equal logits, equal weights)
+  const uint32_t ties = by_mass ? (uint32_t)((want - above_mass + each - 1) / each) : (uint32_t)want - above_cnt;
+  cut.key = prefix;
+  cut.last = INT_MAX;
+  if (ties < x.found_cnt) {   // the place of the last of them
+    uint32_t tied = 0;
+    src.each([&](int, float v, bool in) { tied += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && key_of(v) == prefix)); });
+    __syncthreads();
+    if (lane == 0) x.wcnt[wave] = tied;
+    __syncthreads();
+    uint32_t seen = 0;
+    for (int w = 0; w < wave; ++w) seen += x.wcnt[w];
+    if (seen < ties && ties <= seen + tied)
+      src.each([&](int place, float v, bool in) {
+        const u64 same = __builtin_amdgcn_ballot_w64(in && key_of(v) == prefix);
+        const uint32_t nth = seen + (uint32_t)__builtin_popcountll(same & ((2ull << lane) - 1));
+        if (in && key_of(v) == prefix && nth == ties) x.found_id = place;
+        seen += (uint32_t)__builtin_popcountll(same);
+      });
+    __syncthreads();
+    cut.last = x.found_id;
+  }
+  return above_mass + each * ties;
+}
+
 // The cut after which `want` tokens are kept (by_mass: after which what is kept first weighs `want` or more); there are as many.  Returns what is
-// kept.  First bins of equal width in z, 32 T in all; if up to 64 tokens share the one of the cut, a wave ranks them.  Otherwise digit
-// by digit of their keys: of those that begin like the cut, how many have each next digit and what they weigh.
+// kept.  First bins of equal width in z, 32 T in all; if up to 64 tokens share the one of the cut, a wave ranks them.
 template <typename S>
 __device__ u64 select_cut(const S& src, const SampleRow& row, bool by_mass, u64 want, Cut& cut, Scratch& x) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -204,67 +315,9 @@ __device__ u64 select_cut(const S& src, const SampleRow& row, bool by_mass, u64 
         x.few_mass[i] = row.weight(v);
       }
     });
-    __syncthreads();
-    // every wave ranks them: a lane each, by key, then place
-    const int mine = lane < (int)n ? lane : 0;
-    const uint32_t key = x.few_key[mine];
-    const int place = x.few_place[mine];
-    uint32_t rank = above_cnt;
-    u64 mass = above_mass;
-    for (int j = 0; j < (int)n; ++j) {
-      const bool ahead = x.few_key[j] > key || (x.few_key[j] == key && x.few_place[j] < place);
-      rank += ahead;
-      mass += ahead ? x.few_mass[j] : 0;
-    }
-    const u64 upto = mass + x.few_mass[mine];
-    const u64 is = __builtin_amdgcn_ballot_w64(lane < (int)n && (by_mass ? mass < want && want <= upto : rank + 1 == (uint32_t)want));
-    const int l = __builtin_ctzll(is);
-    cut.key = (uint32_t)__builtin_amdgcn_readlane((int)key, l);
-    cut.last = __builtin_amdgcn_readlane(place, l);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(upto >> 32), l), lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)upto, l);
-    return (u64)hi << 32 | lo;
+    return rank_few(n, above_cnt, above_mass, by_mass, want, cut, x);
   }
-  uint32_t prefix = 0;
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    clear_bins(x);
-    src.each([&](int, float v, bool) {
-      const uint32_t k = key_of(v);
-      if (v > -INFINITY && bin(v) == at && (pass == 0 || (k >> (shift + bits)) == prefix)) {
-        const uint32_t b = (1u << bits) - 1 - ((k >> shift) & ((1u << bits) - 1));   // (the largest digit first)
-        atomicAdd(&x.cnt[b], 1u);
-        atomicAdd(&x.mass[b], row.weight(v));
-      }
-    });
-    __syncthreads();
-    find_bin(by_mass, want, above_cnt, above_mass, x);
-    prefix = (prefix << bits) | ((1u << bits) - 1 - x.found_bin);
-    above_cnt = x.found_above_cnt;
-    above_mass = x.found_above_mass;
-  }
-  const u64 each = x.found_mass / x.found_cnt;   // (equal logits, equal weights)
-  const uint32_t ties = by_mass ? (uint32_t)((want - above_mass + each - 1) / each) : (uint32_t)want - above_cnt;
-  cut.key = prefix;
-  cut.last = INT_MAX;
-  if (ties < x.found_cnt) {   // the place of the last of them
-    uint32_t tied = 0;
-    src.each([&](int, float v, bool in) { tied += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in && key_of(v) == prefix)); });
-    __syncthreads();
-    if (lane == 0) x.wcnt[wave] = tied;
-    __syncthreads();
-    uint32_t seen = 0;
-    for (int w = 0; w < wave; ++w) seen += x.wcnt[w];
-    if (seen < ties && ties <= seen + tied)
-      src.each([&](int place, float v, bool in) {
-        const u64 same = __builtin_amdgcn_ballot_w64(in && key_of(v) == prefix);
-        const uint32_t nth = seen + (uint32_t)__builtin_popcountll(same & ((2ull << lane) - 1));
-        if (in && key_of(v) == prefix && nth == ties) x.found_id = place;
-        seen += (uint32_t)__builtin_popcountll(same);
-      });
-    __syncthreads();
-    cut.last = x.found_id;
-  }
-  return above_mass + each * ties;
+  return select_digits(src, row, by_mass, want, above_cnt, above_mass, [&](float v) { return bin(v) == at; }, cut, x);
 }
 
 // what the tokens before one have to weigh for it to go
@@ -365,7 +418,7 @@ __device__ void sample_whole(const S& src, const SampleRow& row, const SampleArg
     put_token(tokens, stats, r, place, z, row, kept, n, all);
 }
 
-// A row of up to 1024 NE logits: one block, which reads it once.
+// A row of up to 512 NE logits: one block, which reads it once.
 template <typename T, int NE>
 __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* __restrict__ logits, int V, size_t ld,
                                                                       const float* __restrict__ uniforms, SampleArgs a,
@@ -381,13 +434,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* _
   sample_whole(src, SampleRow{(double)m, a.scale}, a, uniforms[r], r, x, tokens, stats);
 }
 
-// ---- longer rows: parts of 1024 NE logits to a block --------------------------------------------------
+// ---- longer rows: parts of 512 NE logits to a block --------------------------------------------------
 // A part's maximum and, without filters, its weights' sum.  With filters, how its weights spread over kBins bins of T / 16 in z, counted down
 // from its largest logit; the last one is all that lies 32 T and more below it, which weighs nothing (less than 2^-46 of the maximum).  Bins
 // begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
 // e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1], and what is added for it one number: 2^48 (a count) plus (e^(rho / 16) - 0.99) 2^36,
-// whose sums over the 32768 logits of a part stay below 2^48.
-constexpr int kBins = 512, kList = 8192, kPartsMax = 40, kSampleBatch = 1024;
+// whose sums over the 16384 logits of a part stay below 2^48.
+constexpr int kBins = 512, kList = 5632, kPartsMax = 40, kSampleBatch = 1024;
+constexpr int kChunk = 1024, kChunksMax = 160;   // logits that a wave goes through at a time; of the longest row
 struct PartSum {
   float m;
   int count;   // -1: a NaN.  With filters: the logits of the last bin, -2 where logits are too large for the bins (2^16 T).  Without: all above -inf
@@ -483,305 +537,371 @@ __device__ __forceinline__ int join_parts(const PartSum* sums, int parts, float&
   return __builtin_amdgcn_ballot_w64(mine.count == -2) ? -2 : 0;
 }
 
-// What is known of a row once its bins are: the cut lies in bins lo .. hi, all above is kept and all below is not.  LISTED: bins 0 .. hi hold up to
-// kList tokens, and these are listed; CUT: the tokens of bins lo .. hi are; WHOLE: neither will do.
-enum { PLAN_NONE = 0, PLAN_LISTED = 1, PLAN_CUT = 2, PLAN_WHOLE = 3 };
-struct Plan {
-  float m;
-  int mode, listed, by_k, by_p;   // by_k, by_p: top-k, top-p cut within the bins
-  int fixed;                      // how many are kept, if that is known (else 0)
-  uint32_t above_cnt;
-  u64 all, above_mass;
-  u64 above[kPartsMax];           // of above_mass, in each part
+// LDS of a block that draws from a row whose parts are known
+struct RowScratch {
+  Scratch x;
+  u64 frac[kBins];
+  uint32_t cnt[kBins];
+  double unit[kBins];
+  int below[64], far[64];   // a part's bins lie so far below the row's (-1: it has none); logits in its last
+  int bin_k, bin_p;
+  u64 cum_mass[kBins + 1], part_kept[64];   // cum: of the bins above
+  uint32_t cum_cnt[kBins + 1];
+  int chunk_cnt[kChunksMax], chunk_at[kChunksMax], chunk_id[kChunksMax], listed;
+  int2 list[kList];         // logit and id
 };
 
-// Finds the bins of the cut and lists their tokens in the order of the ids.  One block a part; each of a row's blocks finds the same bins.
-template <typename T, int NE>
-__global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(const T* __restrict__ logits, int V, size_t ld, SampleArgs a,
-                                                                     const PartSum* __restrict__ sums, const Spread* __restrict__ spreads,
-                                                                     Plan* __restrict__ plans, int2* __restrict__ lists) {
-  __shared__ Scratch x;
-  __shared__ u64 frac[kBins];
-  __shared__ uint32_t cnt[kBins];
-  __shared__ double unit[kBins];
-  __shared__ int below[64], far[64];   // a part's bins lie so far below the row's; logits in its last
-  __shared__ int bin_k, bin_p, at_hi_cnt, at_lo_cnt;
-  __shared__ u64 at_lo_mass, above_s[kPartsMax];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int part = blockIdx.x, parts = gridDim.x, r = blockIdx.y, lo_id = part * (kSampleThreads * NE);
-  InRegisters<NE> src;
-  src.fetch(logits + (size_t)r * ld + lo_id, min(V - lo_id, kSampleThreads * NE));
-  Plan& plan = plans[r];
-  spreads += (size_t)r * parts;
-  float m;
-  PartSum mine;
-  const int state = join_parts(sums + (size_t)r * parts, parts, m, mine);
-  if (state) {
-    if (part == 0 && tid == 0) { plan.m = m; plan.mode = state == -1 ? PLAN_NONE : PLAN_WHOLE; }
-    return;
-  }
-  const float c = fminf((float)a.per_z, 1e30f), top = bin_of(m, c);
-  if (tid < kBins) { frac[tid] = 0; cnt[tid] = 0; unit[tid] = tid < kBins - 1 ? bin_unit(m, top, tid, a.per_z) : 0.0; }
-  if (tid < kPartsMax) above_s[tid] = 0;
-  if (tid < 64) {
-    below[tid] = tid < parts && mine.m > -INFINITY ? bins_below(top, bin_of(mine.m, c)) : -1;   // (-1: it has written none)
-    far[tid] = tid < parts ? mine.count : 0;
-  }
-  if (tid == 0) bin_k = bin_p = kBins;
-  __syncthreads();
-  auto sum_of = [&](int p, int b) { return below[p] >= 0 ? spreads[p][b] : 0ull; };
-  auto row_bin = [&](int p, int b) { return min(b + below[p], kBins - 1); };
-  constexpr u64 kFrac = (1ull << 48) - 1;
-  {
-    const int b = tid % kBins;   // two parts at a time, a thread a bin of each
-    for (int p0 = tid / kBins; p0 < parts; p0 += 8) {
-      u64 s[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = p0 + 2 * i < parts ? sum_of(p0 + 2 * i, b) : 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (s[i]) {
-          const int to = row_bin(p0 + 2 * i, b);
-          atomicAdd(&cnt[to], (uint32_t)(s[i] >> 48));
-          atomicAdd(&frac[to], s[i] & kFrac);
-        }
+// Bins lo .. hi hold the cut: all above is kept and all below is not.  LISTED: the tokens of bins 0 .. hi are listed, up to kList of them;
+// CUT: those of lo .. hi; WHOLE: neither will do.
+enum { PLAN_LISTED = 1, PLAN_CUT = 2, PLAN_WHOLE = 3 };
+
+// Lists the tokens of bins `from` .. `hi` in the order of the ids.  A wave takes a chunk at a time, of the parts that reach so high; its
+// tokens go to wherever the list has got to, and once all are there a chunk's are moved to behind those of the chunks before it.
+template <typename T>
+__device__ __forceinline__ void list_bins(const T* z, int V, int part_size, float c, float top, int from, int hi, RowScratch& y) {
+  constexpr int E = kChunk / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (V + kChunk - 1) / kChunk;
+  static_assert(kChunksMax <= 192, "three waves have a chunk a lane");
+  // The lowest logit of bin hi, the highest of bin `from`: bins go with the logits' order, so bisect it.
+  auto logit_of = [](uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); };
+  uint32_t least = 0x00800000u, most = 0xff7fffffu;   // (keys of the lowest and the highest finite value)
+  auto bin_of_key = [&](uint32_t k) { return bins_below(top, bin_of(logit_of(k), c)); };
+  // first key of bin b or above it: a few keys around where it should be, or bisected
+  auto first_key = [&](int b) {
+    const uint32_t guess = min(max(key_of((top - (float)b) / c), 0x00800020u), 0xff7fffdfu) - 32;
+    const u64 yes = __builtin_amdgcn_ballot_w64(bin_of_key(guess + lane) <= b);
+    if (yes && !(yes & 1)) return guess + (uint32_t)__builtin_ctzll(yes);
+    uint32_t i = 0x00800000u, j = 0xff7fffffu;
+    while (i < j) {
+      const uint32_t mid = i + (j - i) / 2;
+      if (bin_of_key(mid) <= b) j = mid; else i = mid + 1;
     }
-    if (tid < parts && far[tid] > 0) atomicAdd(&cnt[kBins - 1], (uint32_t)far[tid]);
+    return i;
+  };
+  if (hi < kBins - 1) least = first_key(hi);
+  if (from > 0) most = first_key(from - 1) - 1;
+  const float vmin = logit_of(least), vmax = logit_of(most);
+  // the chunks to go through, a lane each
+  u64 n = tid < chunks && y.below[tid * kChunk / part_size] >= 0 && y.below[tid * kChunk / part_size] <= hi;
+  u64 before = 0;
+  if (wave < 3) {
+    before = wave_before_u64(n);
+    if (lane == 63) y.x.wcnt[wave] = (uint32_t)(before + n);
   }
   __syncthreads();
-  // a bin a thread, the largest logits first
-  const uint32_t n = tid < kBins ? cnt[tid] : 0;
-  const u64 s = tid < kBins ? bin_mass(n, frac[tid], unit[tid]) : 0;
-  u64 cb = wave_before_u64(n), mb = wave_before_u64(s);
-  if (lane == 63) { x.wcnt[wave] = (uint32_t)cb + n; x.wsum[wave] = mb + s; }
+  if (wave < 3) {
+    for (int w = 0; w < wave; ++w) before += y.x.wcnt[w];
+    if (n) y.chunk_id[before] = tid;
+    if (tid < chunks) y.chunk_cnt[tid] = 0;
+  }
+  const int active = (int)(y.x.wcnt[0] + y.x.wcnt[1] + y.x.wcnt[2]);
   __syncthreads();
-  u64 all = 0, finite = 0;
+  auto fetch = [&](float (&v)[E], int i) {
+    const int first = (i < active ? y.chunk_id[i] : 0) * kChunk + lane;
 #pragma unroll
-  for (int w = 0; w < kSampleWaves; ++w) {
-    if (w < wave) { cb += x.wcnt[w]; mb += x.wsum[w]; }
-    finite += x.wcnt[w];
-    all += x.wsum[w];
-  }
-  bool by_k = a.top_k > 0 && (u64)a.top_k < finite;
-  if (by_k && cb < (u64)a.top_k && (u64)a.top_k <= cb + n) bin_k = tid;
-  __syncthreads();
-  // Top-k that ends among tokens of no weight takes nothing from the others: all that it says is how many are kept, if nothing else does.
-  const int fixed = by_k && bin_k == kBins - 1 && a.top_p >= 1.0 && a.min_weight == 0 ? a.top_k : 0;
-  const int k_at = by_k && bin_k < kBins - 1 ? bin_k : kBins;
-  by_k = k_at < kBins;
-  const bool by_p = a.top_p < 1.0;
-  const u64 want = by_p ? mass_wanted(a.top_p, all) : 0;
-  if (by_p && !by_k && mb < want && want <= mb + s) bin_p = tid;
-  __syncthreads();
-  // kBins: no cut.  (The bin of min_p's border is known up to the rounding of its logarithm.  Where top-p goes by the sum of the top-k, these
-  // have to be there.)
-  int lo = min(k_at, bin_p), hi = lo;
-  if (a.min_weight > 0 && !(by_k && by_p)) {
-    const double border = log2((double)a.min_weight * 0x1p-46) / a.scale;   // (z of the border less the maximum: <= 0)
-    const int bm = (int)fmax(fmin((double)top - floor(((double)m + border) * a.per_z), (double)kBins), 0.0);
-    lo = min(lo, max(bm - 1, 0));
-    hi = min(hi, bm + 1);
-  }
-  if (lo < kBins) hi = min(hi, kBins - 1);
-  if (tid == 0) { at_hi_cnt = (int)finite; at_lo_cnt = (int)finite; at_lo_mass = all; }
-  __syncthreads();
-  if (tid == lo) { at_lo_cnt = (int)cb; at_lo_mass = mb; }
-  if (tid == hi) at_hi_cnt = (int)cb + (int)n;
-  __syncthreads();
-  int mode = PLAN_WHOLE;
-  if (lo < kBins && at_hi_cnt <= kList) mode = PLAN_LISTED;
-  else if (!(by_k && by_p) && at_hi_cnt - at_lo_cnt <= kList) mode = PLAN_CUT;
-  const int from = mode == PLAN_LISTED ? 0 : lo;
-  if (mode != PLAN_WHOLE && lo < kBins) {
-    uint32_t have = 0;
-    u64 has[NE], sum = 0;
-    int e = 0;
-    src.each([&](int, float v, bool) {
-      const int b = v > -INFINITY ? bins_below(top, bin_of(v, c)) : -1;
-      has[e] = __builtin_amdgcn_ballot_w64(b >= from && b <= hi);
-      have += (uint32_t)__builtin_popcountll(has[e++]);
-    });
-    // those of the parts before this one
-    for (int i = tid; i < part * kBins; i += kSampleThreads) {
-      const u64 v = sum_of(i / kBins, i % kBins);
-      const int to = row_bin(i / kBins, i % kBins);
-      sum += to >= from && to <= hi ? v >> 48 : 0;
+    for (int e = 0; e < E; ++e) v[e] = load_f32(z + min(first + e * 64, V - 1));
+  };
+  auto put = [&](float (&v)[E], int i) {
+    const int ch = y.chunk_id[i];
+    if ((ch + 1) * kChunk > V)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = ch * kChunk + e * 64 + lane < V ? v[e] : -INFINITY;
+    u64 has[E];
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      has[e] = __builtin_amdgcn_ballot_w64(v[e] >= vmin && v[e] <= vmax);
+      n += __builtin_popcountll(has[e]);
     }
-    if (hi == kBins - 1 && tid < part) sum += far[tid];
-    const uint32_t before = (uint32_t)block_sum_u64(sum, x);
-    __syncthreads();
-    if (lane == 0) x.wcnt[wave] = have;
-    __syncthreads();
-    uint32_t at = before;
-    for (int w = 0; w < wave; ++w) at += x.wcnt[w];
-    int2* list = lists + (size_t)r * kList;
-    e = 0;
-    src.each([&](int place, float v, bool) {
-      const u64 h = has[e++];
-      const uint32_t to = at + (uint32_t)__builtin_popcountll(h & ((1ull << lane) - 1));
-      if ((h >> lane & 1) && to < (uint32_t)kList) list[to] = make_int2(__float_as_int(v), lo_id + place);
-      at += (uint32_t)__builtin_popcountll(h);
-    });
-  }
-  if (part == 0) {
-    if (mode == PLAN_CUT) {
-      for (int i = tid; i < parts * kBins; i += kSampleThreads) {
-        const int p = i / kBins, to = row_bin(p, i % kBins);
-        const u64 v = to < lo && to < kBins - 1 ? sum_of(p, i % kBins) : 0;
-        if (v) atomicAdd(&above_s[p], bin_mass(v >> 48, v & kFrac, unit[to]));
+    if (!n) return;
+    int at = 0;
+    if (lane == 0) {
+      at = atomicAdd(&y.listed, n);
+      y.chunk_cnt[ch] = n;
+      y.chunk_at[ch] = at;
+    }
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (has[e]) {
+        const int to = at + __builtin_popcountll(has[e] & ((1ull << lane) - 1));
+        if ((has[e] >> lane & 1) && to < kList) y.list[to] = make_int2(__float_as_int(v[e]), ch * kChunk + e * 64 + lane);
+        at += __builtin_popcountll(has[e]);
       }
-      __syncthreads();
-      if (tid < parts) plan.above[tid] = above_s[tid];
-    }
-    if (tid == 0) {
-      plan.m = m;
-      plan.mode = mode;
-      plan.listed = mode == PLAN_LISTED ? at_hi_cnt : at_hi_cnt - at_lo_cnt;
-      plan.by_k = by_k && k_at <= hi;
-      plan.fixed = fixed;
-      plan.by_p = by_p && (by_k || bin_p <= hi);
-      plan.above_cnt = mode == PLAN_LISTED ? 0 : (uint32_t)at_lo_cnt;
-      plan.above_mass = mode == PLAN_LISTED ? 0 : at_lo_mass;
-      plan.all = all;
-    }
+  };
+  float v[E], w[E];   // (one chunk on its way while the other is gone through)
+  fetch(v, wave);
+  for (int i = wave; i < active; i += 2 * kSampleWaves) {
+    fetch(w, i + kSampleWaves);
+    put(v, i);
+    fetch(v, i + 2 * kSampleWaves);
+    if (i + kSampleWaves < active) put(w, i + kSampleWaves);
+  }
+  __syncthreads();
+  // where each chunk's tokens go
+  if (wave < 3) {
+    n = tid < chunks ? y.chunk_cnt[tid] : 0;
+    before = wave_before_u64(n);
+    if (lane == 63) y.x.wcnt[wave] = (uint32_t)(before + n);
+  }
+  int2 mine[kList / kSampleThreads];
+  static_assert(kList % kSampleThreads == 0, "whole rounds");
+  const int listed = min(y.listed, kList);
+#pragma unroll
+  for (int e = 0; e < kList / kSampleThreads; ++e)
+    if (e * kSampleThreads < listed) mine[e] = y.list[min(e * kSampleThreads + tid, kList - 1)];
+  __syncthreads();
+  if (tid < chunks && n) {
+    for (int w = 0; w < wave; ++w) before += y.x.wcnt[w];
+    y.chunk_cnt[tid] = (int)before - y.chunk_at[tid];   // how far they move
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kList / kSampleThreads; ++e) {
+    const int at = e * kSampleThreads + tid;
+    if (at < listed) y.list[at + y.chunk_cnt[mine[e].y / kChunk]] = mine[e];
   }
 }
 
-// The token of a row whose parts are known.  One block a row.
+// The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the row is read
+// once more for the tokens of these, which are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
+// which part the token is, and only that is read.
 template <typename T, bool FILTERS>
 __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
-                                                                     const PartSum* __restrict__ sums, const Plan* __restrict__ plans,
-                                                                     const int2* __restrict__ lists, int* __restrict__ tokens,
-                                                                     float4* __restrict__ stats) {
-  __shared__ Scratch x;
-  __shared__ u64 part_kept[kPartsMax];
-  const int r = blockIdx.x, tid = threadIdx.x;
+                                                                     const PartSum* __restrict__ sums, const Spread* __restrict__ spreads,
+                                                                     int* __restrict__ tokens, float4* __restrict__ stats) {
+  extern __shared__ char lds_[];
+  RowScratch& y = *(RowScratch*)lds_;
+  Scratch& x = y.x;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float u = uniforms[r];
   const T* z = logits + (size_t)r * ld;
+  spreads += (size_t)r * parts;
   Cut cut;
   u64 all = 0;
   uint32_t count = 0;
   float m;
+  PartSum mine;
+  const int state = join_parts(sums + (size_t)r * parts, parts, m, mine);
+  if (state == -1) { no_token(tokens, stats, r); return; }
+  const SampleRow row = {(double)m, a.scale};
   if constexpr (FILTERS) {
-    const Plan& plan = plans[r];
-    const int mode = plan.mode;
-    if (mode == PLAN_NONE) { no_token(tokens, stats, r); return; }
-    m = plan.m;
-    const SampleRow row = {(double)m, a.scale};
+    const float c = fminf((float)a.per_z, 1e30f), top = bin_of(m, c);
+    int mode = PLAN_WHOLE, lo = 0, hi = 0, fixed = 0;
+    bool by_k = false, by_p = a.top_p < 1.0;
+    if (state == 0) {
+      static_assert(kSampleThreads == kBins, "a thread a bin");
+      y.frac[tid] = 0;
+      y.cnt[tid] = 0;
+      y.unit[tid] = tid < kBins - 1 ? bin_unit(m, top, tid, a.per_z) : 0.0;
+      if (tid < 64) {
+        y.below[tid] = tid < parts && mine.m > -INFINITY ? bins_below(top, bin_of(mine.m, c)) : -1;   // (-1: it has written none)
+        y.far[tid] = tid < parts ? mine.count : 0;
+        y.part_kept[tid] = 0;
+      }
+      if (tid == 0) { y.bin_k = y.bin_p = kBins; y.listed = 0; }
+      __syncthreads();
+      auto row_bin = [&](int p, int b) { return min(b + y.below[p], kBins - 1); };
+      constexpr u64 kFrac = (1ull << 48) - 1;
+      // a thread a bin of each part, eight loads on their way
+      for (int p0 = 0; p0 < parts; p0 += 8) {
+        u64 s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = p0 + i < parts && y.below[p0 + i] >= 0 ? spreads[p0 + i][tid] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (s[i]) {
+            const int to = row_bin(p0 + i, tid);
+            atomicAdd(&y.cnt[to], (uint32_t)(s[i] >> 48));
+            atomicAdd(&y.frac[to], s[i] & kFrac);
+          }
+      }
+      if (tid < parts && y.far[tid] > 0) atomicAdd(&y.cnt[kBins - 1], (uint32_t)y.far[tid]);
+      __syncthreads();
+      // a bin a thread, the largest logits first
+      const uint32_t n = y.cnt[tid];
+      const u64 s = bin_mass(n, y.frac[tid], y.unit[tid]);
+      u64 cb = wave_before_u64(n), mb = wave_before_u64(s);
+      if (lane == 63) { x.wcnt[wave] = (uint32_t)cb + n; x.wsum[wave] = mb + s; }
+      __syncthreads();
+      u64 finite = 0;
+#pragma unroll
+      for (int w = 0; w < kSampleWaves; ++w) {
+        if (w < wave) { cb += x.wcnt[w]; mb += x.wsum[w]; }
+        finite += x.wcnt[w];
+        all += x.wsum[w];
+      }
+      by_k = a.top_k > 0 && (u64)a.top_k < finite;
+      if (by_k && cb < (u64)a.top_k && (u64)a.top_k <= cb + n) y.bin_k = tid;
+      __syncthreads();
+      // Top-k that ends among tokens of no weight takes nothing from the others: all that it says is how many are kept, if nothing else does.
+      const int bin_k = y.bin_k;
+      fixed = by_k && bin_k == kBins - 1 && !by_p && a.min_weight == 0 ? a.top_k : 0;
+      by_k = by_k && bin_k < kBins - 1;
+      const u64 want = by_p ? mass_wanted(a.top_p, all) : 0;
+      if (by_p && !by_k && mb < want && want <= mb + s) y.bin_p = tid;
+      __syncthreads();
+      // kBins: no cut.  (The bin of min_p's border is known up to the rounding of its logarithm.  Where top-p goes by the sum of the top-k,
+      // these have to be there.)
+      const int k_at = by_k ? bin_k : kBins, p_at = y.bin_p;
+      lo = hi = min(k_at, p_at);
+      if (a.min_weight > 0 && !(by_k && by_p)) {
+        const double border = log2((double)a.min_weight * 0x1p-46) / a.scale;   // (z of the border less the maximum: <= 0)
+        const int bm = (int)fmax(fmin((double)top - floor(((double)m + border) * a.per_z), (double)kBins), 0.0);
+        lo = min(lo, max(bm - 1, 0));
+        hi = min(hi, bm + 1);
+      }
+      if (lo < kBins) hi = min(hi, kBins - 1);
+      y.cum_cnt[tid] = (uint32_t)cb;
+      y.cum_mass[tid] = mb;
+      if (tid == 0) { y.cum_cnt[kBins] = (uint32_t)finite; y.cum_mass[kBins] = all; }
+      __syncthreads();
+      // (hi < kBins wherever lo is)
+      const int upto_hi = (int)y.cum_cnt[min(hi + 1, kBins)];
+      if (lo < kBins && upto_hi <= kList) mode = PLAN_LISTED;
+      else if (!(by_k && by_p) && upto_hi - (int)y.cum_cnt[lo] <= kList) mode = PLAN_CUT;
+      by_k = by_k && k_at <= hi;
+      by_p = by_p && (by_k || p_at <= hi);
+      if (mode == PLAN_CUT) {
+        // what lies above the bins, part by part
+        for (int p0 = 0; p0 < parts; p0 += 8) {
+          u64 v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int to = p0 + i < parts && y.below[p0 + i] >= 0 ? row_bin(p0 + i, tid) : kBins;
+            v[i] = to < lo && to < kBins - 1 ? spreads[p0 + i][tid] : 0;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (p0 + i < parts) {
+              const u64 sum = wave_sum_u64(v[i] ? bin_mass(v[i] >> 48, v[i] & kFrac, y.unit[row_bin(p0 + i, tid)]) : 0);
+              if (lane == 0 && sum) atomicAdd(&y.part_kept[p0 + i], sum);
+            }
+        }
+      }
+    }
     if (mode == PLAN_WHOLE) {
       InMemory<T> src;
       src.fetch(z, V);
       sample_whole(src, row, a, u, r, x, tokens, stats);
       return;
     }
-    all = plan.all;
-    const int2* list = lists + (size_t)r * kList;
-    InRegisters<kList / kSampleThreads> src;
-    src.n = plan.listed;
-    src.first = (tid >> 6) * kList / kSampleWaves + (tid & 63);
-#pragma unroll
-    for (int e = 0; e < kList / kSampleThreads; ++e) {
-      const int at = src.first + e * 64;
-      src.v[e] = at < src.n ? __int_as_float(list[at].x) : -INFINITY;
-    }
-    const u64 listed = sum_weights(src, row, x);   // (may differ from the bins' by roundings)
-    u64 of_k = mode == PLAN_LISTED ? all : 0;
+    if (lo < kBins) list_bins(z, V, part_size, c, top, mode == PLAN_LISTED ? 0 : lo, hi, y);
+    __syncthreads();
+    InList src;
+    src.fetch(y.list, lo < kBins ? y.listed : 0);
+    u64 of_k = all;
     for (int by_mass = 0; by_mass < 2; ++by_mass) {
-      u64 want;
-      if (by_mass) {
-        if (!plan.by_p) continue;
-        want = min(mode == PLAN_LISTED ? mass_wanted(a.top_p, of_k) : mass_wanted(a.top_p, all) - plan.above_mass, listed);
-      } else {
-        if (!plan.by_k) continue;
-        want = a.top_k - (int)plan.above_cnt;
-        if (want >= (u64)src.n) { of_k = listed; continue; }
+      if (!(by_mass ? by_p : by_k)) continue;
+      const u64 want = by_mass ? mass_wanted(a.top_p, of_k) : (u64)a.top_k;
+      int at = by_mass ? y.bin_p : y.bin_k;
+      if (by_mass && by_k) {   // (the sum of the top-k is known only now)
+        __syncthreads();
+        if (y.cum_mass[tid] < want && want <= y.cum_mass[tid + 1]) y.bin_p = tid;
+        __syncthreads();
+        at = y.bin_p;
       }
-      of_k = select_cut(src, row, by_mass, want, cut, x);
+      const uint32_t n = y.cnt[at];
+      if (n <= 64) {
+        if (tid == 0) x.n_few = 0;
+        __syncthreads();
+        src.each([&](int place, float v, bool in) {
+          if (in && bins_below(top, bin_of(v, c)) == at) {
+            const uint32_t i = atomicAdd(&x.n_few, 1u);
+            x.few_key[i & 63] = key_of(v);
+            x.few_place[i & 63] = place;
+            x.few_mass[i & 63] = row.weight(v);
+          }
+        });
+        of_k = rank_few(n, y.cum_cnt[at], y.cum_mass[at], by_mass, want, cut, x);
+      } else {
+        // (the weights of the bin's tokens, and their sum there, differ by roundings)
+        u64 of_bin = 0;
+        auto in_bin = [&](float v) { return bins_below(top, bin_of(v, c)) == at; };
+        src.each([&](int, float v, bool) { of_bin += v > -INFINITY && in_bin(v) ? row.weight(v) : 0; });
+        of_bin = block_sum_u64(of_bin, x);
+        of_k = select_digits(src, row, by_mass, by_mass ? min(want, y.cum_mass[at] + of_bin) : want, y.cum_cnt[at], y.cum_mass[at], in_bin, cut, x);
+      }
     }
     if (mode == PLAN_LISTED) {
       u64 kept;
       int place;
       float v;
       if (draw_place(src, row, cut, 0, a.min_weight, x, kept, count, [&](u64 k) { return draw_at(u, k); }, place, v))
-        put_token(tokens, stats, r, list[place].y, v, row, kept, count, all);
+        put_token(tokens, stats, r, y.list[place].y, v, row, kept, count, all);
       return;
     }
     // what is kept of each part: all above the bins, and some of the list
-    if (tid < kPartsMax) part_kept[tid] = tid < parts ? plan.above[tid] : 0;
-    __syncthreads();
     u64 n = 0;
     src.each([&](int at, float v, bool) {
       const u64 w = row.weight(v);
       if (v > -INFINITY && w >= a.min_weight && cut.keeps(key_of(v), at)) {
         ++n;
-        atomicAdd(&part_kept[list[at].y / part_size], w);
+        atomicAdd(&y.part_kept[y.list[at].y / part_size], w);
       }
     });
-    count = plan.above_cnt + (uint32_t)block_sum_u64(n, x);
-    if (plan.fixed) count = plan.fixed;
-    if (cut.last != INT_MAX) cut.last = list[cut.last].y;
+    count = y.cum_cnt[lo] + (uint32_t)block_sum_u64(n, x);
+    if (fixed) count = fixed;
+    if (cut.last != INT_MAX) cut.last = y.list[cut.last].y;
   } else {
-    PartSum mine;
-    if (join_parts(sums + (size_t)r * parts, parts, m, mine)) { no_token(tokens, stats, r); return; }
-    const bool some = (tid & 63) < parts && mine.m > -INFINITY;
-    if (tid < kPartsMax)   // (the part's sum, seen from the row's maximum)
-      part_kept[tid] = some ? (u64)((double)mine.sum * (exp2_times_2to46(((double)mine.m - (double)m) * a.scale) * 0x1p-46) + 0.5) : 0;
+    const bool some = lane < parts && mine.m > -INFINITY;
+    if (tid < 64)   // (the part's sum, seen from the row's maximum)
+      y.part_kept[tid] = some ? (u64)((double)mine.sum * (exp2_times_2to46(((double)mine.m - (double)m) * a.scale) * 0x1p-46) + 0.5) : 0;
     count = (uint32_t)wave_sum_u64(some ? (u64)mine.count : 0);
   }
   __syncthreads();
-  const SampleRow row = {(double)m, a.scale};
-  const u64 kept = wave_sum_u64((tid & 63) < parts ? part_kept[tid & 63] : 0);
+  const u64 kept = wave_sum_u64(y.part_kept[lane]);
   if constexpr (!FILTERS) all = kept;
   // The part of the token, then the token.  The part's own weights, seen from the row's maximum, may come to a little less than its sum did, to
   // nothing where each rounds to 0: then the next part's first.
   const u64 want = draw_at(u, kept);
-  u64 base = 0;
-  int p = 0;
-  while (p + 1 < parts && base + part_kept[p] < want) base += part_kept[p++];
+  u64 base = wave_before_u64(y.part_kept[lane]);
+  int p = __builtin_ctzll(__builtin_amdgcn_ballot_w64(base + y.part_kept[lane] >= want));
+  {
+    const uint32_t bhi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(base >> 32), p), blo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)base, p);
+    base = (u64)bhi << 32 | blo;
+  }
   for (int tried = 0; tried <= parts; ++tried, p = p + 1 < parts ? p + 1 : 0) {
-    const int lo = p * part_size;
+    const int first = p * part_size;
     InMemory<T> src;
-    src.fetch(z + lo, min(V - lo, part_size));
+    src.fetch(z + first, min(V - first, part_size));
     u64 here;
     uint32_t n;
     int place;
     float v;
-    const bool mine = draw_place(src, row, cut, lo, a.min_weight, x, here, n,
-                                 [&](u64 k) { return tried ? min((u64)1, k) : min(want - base, k); }, place, v);
-    if (mine) put_token(tokens, stats, r, lo + place, v, row, kept, count, all);
+    const bool found = draw_place(src, row, cut, first, a.min_weight, x, here, n,
+                                  [&](u64 k) { return tried ? min((u64)1, k) : min(want - base, k); }, place, v);
+    if (found) put_token(tokens, stats, r, first + place, v, row, kept, count, all);
     if (here > 0) break;   // (the same for all threads)
   }
 }
 
 // ---- launchers ------------------------------------------------------------------------------------
 struct SamplePlanSizes { int ne, parts; };
-// Logits to a thread: the fewest with which a batch of rows makes about two blocks of 1024 threads for each compute unit.
+// Logits to a thread: the fewest with which a batch of rows makes no more than four blocks for each compute unit.
+constexpr int kSampleBlocks = 1024;
 static SamplePlanSizes sample_sizes(int rows, int V) {
-  for (const int ne : {4, 8, 16, 32}) {
+  for (const int ne : {8, 16, 32}) {
     const int parts = (V + kSampleThreads * ne - 1) / (kSampleThreads * ne);
-    if (ne == 32 || (long)rows * parts <= 512) return {ne, parts};
+    if (ne == 32 || (long)rows * parts <= kSampleBlocks) return {ne, parts};
   }
   return {32, 1};
 }
 constexpr int kSampleSmall = 16384;   // logits of a row that one block holds in registers
-struct SampleBytes { size_t sums, spreads, plans, lists, all; };
+struct SampleBytes { size_t sums, all; };
 static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) { b.all = 256; return b; }
   if (rows > kSampleBatch) rows = kSampleBatch;
   size_t most = 0;   // (fewer rows may have more parts between them)
-  for (const int ne : {4, 8, 16, 32}) {
+  for (const int ne : {8, 16, 32}) {
     const size_t parts = (V + kSampleThreads * ne - 1) / (kSampleThreads * ne);
-    const size_t n = parts * (ne == 32 ? rows : rows * parts <= 512 ? rows : 512 / parts);
+    const size_t n = parts * (ne == 32 ? rows : rows * parts <= kSampleBlocks ? rows : kSampleBlocks / parts);
     if (n > most) most = n;
   }
-  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  b.sums = up(most * sizeof(PartSum));
-  b.spreads = up(most * sizeof(Spread));
-  b.plans = up(rows * sizeof(Plan));
-  b.lists = up((size_t)rows * kList * sizeof(int2));
-  b.all = b.sums + b.spreads + b.plans + b.lists;
+  b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
+  b.all = b.sums + most * sizeof(Spread);
   return b;
 }
 size_t sample_workspace(int rows, int V) { return sample_bytes(rows, V).all; }
@@ -791,16 +911,18 @@ static void launch_sample_ne(const T* logits, int rows, int parts, int V, size_t
                              float4* stats, char* ws, const SampleBytes& b, hipStream_t s) {
   PartSum* sums = (PartSum*)ws;
   Spread* spreads = (Spread*)(ws + b.sums);
-  Plan* plans = (Plan*)(ws + b.sums + b.spreads);
-  int2* lists = (int2*)(ws + b.sums + b.spreads + b.plans);
   const dim3 grid(parts, rows);
   if (a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0) {
+    static const hipError_t once = hipFuncSetAttribute((const void*)sample_draw_kernel<T, true>,
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(RowScratch));
+    (void)once;
     sample_parts_kernel<T, NE, true><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    sample_list_kernel<T, NE><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a, sums, spreads, plans, lists);
-    sample_draw_kernel<T, true><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, parts, kSampleThreads * NE, uniforms, a, sums, plans, lists, tokens, stats);
+    sample_draw_kernel<T, true><<<rows, kSampleThreads, sizeof(RowScratch), s>>>(logits, V, ld, parts, kSampleThreads * NE, uniforms, a, sums,
+                                                                                 spreads, tokens, stats);
   } else {
     sample_parts_kernel<T, NE, false><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    sample_draw_kernel<T, false><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, parts, kSampleThreads * NE, uniforms, a, sums, plans, lists, tokens, stats);
+    sample_draw_kernel<T, false><<<rows, kSampleThreads, offsetof(RowScratch, list), s>>>(logits, V, ld, parts, kSampleThreads * NE, uniforms, a,
+                                                                                          sums, spreads, tokens, stats);
   }
 }
 
@@ -808,9 +930,9 @@ template <typename T>
 static void launch_sample_t(const T* logits, int rows, int V, size_t ld, const float* uniforms, const SampleArgs& a, int* tokens,
                             float4* stats, void* workspace, hipStream_t s) {
   if (V <= kSampleSmall) {
-    if (V <= 1024) sample_small_kernel<T, 1><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
-    else if (V <= 4096) sample_small_kernel<T, 4><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
-    else sample_small_kernel<T, 16><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
+    if (V <= 1024) sample_small_kernel<T, 2><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
+    else if (V <= 4096) sample_small_kernel<T, 8><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
+    else sample_small_kernel<T, 32><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
     return;
   }
   const SampleBytes b = sample_bytes(rows, V);
@@ -819,7 +941,6 @@ static void launch_sample_t(const T* logits, int rows, int V, size_t ld, const f
     const SamplePlanSizes w = sample_sizes(n, V);
     const T* z = logits + (size_t)r * ld;
     switch (w.ne) {
-      case 4: launch_sample_ne<T, 4>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
       case 8: launch_sample_ne<T, 8>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
       case 16: launch_sample_ne<T, 16>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
       default: launch_sample_ne<T, 32>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
