@@ -282,7 +282,7 @@ __device__ u64 select_digits(const S& src, const SampleRow& row, bool by_mass, u
 // kept.  First bins of equal width in z, 32 T in all; if up to 64 tokens share the one of the cut, a wave ranks them.
 template <typename S>
 __device__ u64 select_cut(const S& src, const SampleRow& row, bool by_mass, u64 want, Cut& cut, Scratch& x) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   // (a fixed order of operations on one logit: it falls into the same bin each time, and a larger one into none behind it)
   const float m = (float)row.m, wide = fminf((float)(row.scale * (kDigits / (32 * 1.4426950408889634))), 1e30f);
   auto bin = [&](float v) { return (int)fminf((m - v) * wide, (float)(kDigits - 1)); };
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* _
 // begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
 // e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1], and what is added for it one number: 2^48 (a count) plus (e^(rho / 16) - 0.99) 2^36,
 // whose sums over the 16384 logits of a part stay below 2^48.
-constexpr int kBins = 512, kList = 5632, kPartsMax = 40, kSampleBatch = 1024;
+constexpr int kBins = 512, kList = 5632, kListShort = 3072, kPartsMax = 40, kSampleBatch = 1024;
 constexpr int kChunk = 1024, kChunksMax = 160;   // logits that a wave goes through at a time; of the longest row
 struct PartSum {
   float m;
@@ -537,28 +537,30 @@ __device__ __forceinline__ int join_parts(const PartSum* sums, int parts, float&
   return __builtin_amdgcn_ballot_w64(mine.count == -2) ? -2 : 0;
 }
 
-// LDS of a block that draws from a row whose parts are known
-struct RowScratch {
-  Scratch x;
-  u64 frac[kBins];
+// LDS of a block that draws from a row whose parts are known, up to LIST tokens among which the cut is
+template <int LIST> struct RowScratch {
+  union {
+    Scratch x;               // (of its arrays, mass is used only once these two are not)
+    struct { u64 frac[kBins]; double unit[kBins]; } bins;
+  };
   uint32_t cnt[kBins];
-  double unit[kBins];
   int below[64], far[64];   // a part's bins lie so far below the row's (-1: it has none); logits in its last
   int bin_k, bin_p;
   u64 cum_mass[kBins + 1], part_kept[64];   // cum: of the bins above
   uint32_t cum_cnt[kBins + 1];
   int chunk_cnt[kChunksMax], chunk_at[kChunksMax], chunk_id[kChunksMax], listed;
-  int2 list[kList];         // logit and id
+  int2 list[LIST];          // logit and id
 };
+static_assert(offsetof(Scratch, mass) == 0 && sizeof(Scratch::mass) >= kBins * 16, "frac and unit lie over mass");
 
-// Bins lo .. hi hold the cut: all above is kept and all below is not.  LISTED: the tokens of bins 0 .. hi are listed, up to kList of them;
+// Bins lo .. hi hold the cut: all above is kept and all below is not.  LISTED: the tokens of bins 0 .. hi are listed, up to LIST of them;
 // CUT: those of lo .. hi; WHOLE: neither will do.
 enum { PLAN_LISTED = 1, PLAN_CUT = 2, PLAN_WHOLE = 3 };
 
 // Lists the tokens of bins `from` .. `hi` in the order of the ids.  A wave takes a chunk at a time, of the parts that reach so high; its
 // tokens go to wherever the list has got to, and once all are there a chunk's are moved to behind those of the chunks before it.
-template <typename T>
-__device__ __forceinline__ void list_bins(const T* z, int V, int part_size, float c, float top, int from, int hi, RowScratch& y) {
+template <typename T, int LIST>
+__device__ __forceinline__ void list_bins(const T* z, int V, int part_size, float c, float top, int from, int hi, RowScratch<LIST>& y) {
   constexpr int E = kChunk / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (V + kChunk - 1) / kChunk;
   static_assert(kChunksMax <= 192, "three waves have a chunk a lane");
@@ -609,10 +611,12 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
     u64 has[E];
     int n = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      has[e] = __builtin_amdgcn_ballot_w64(v[e] >= vmin && v[e] <= vmax);
-      n += __builtin_popcountll(has[e]);
-    }
+    for (int e = 0; e < E; ++e) has[e] = __builtin_amdgcn_ballot_w64(v[e] >= vmin);
+    if (from)
+#pragma unroll
+      for (int e = 0; e < E; ++e) has[e] &= __builtin_amdgcn_ballot_w64(v[e] <= vmax);
+#pragma unroll
+    for (int e = 0; e < E; ++e) n += __builtin_popcountll(has[e]);
     if (!n) return;
     int at = 0;
     if (lane == 0) {
@@ -624,8 +628,8 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (has[e]) {
-        const int to = at + __builtin_popcountll(has[e] & ((1ull << lane) - 1));
-        if ((has[e] >> lane & 1) && to < kList) y.list[to] = make_int2(__float_as_int(v[e]), ch * kChunk + e * 64 + lane);
+        const int to = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has[e], 0));
+        if ((has[e] >> lane & 1) && to < LIST) y.list[to] = make_int2(__float_as_int(v[e]), ch * kChunk + e * 64 + lane);
         at += __builtin_popcountll(has[e]);
       }
   };
@@ -644,12 +648,12 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
     before = wave_before_u64(n);
     if (lane == 63) y.x.wcnt[wave] = (uint32_t)(before + n);
   }
-  int2 mine[kList / kSampleThreads];
-  static_assert(kList % kSampleThreads == 0, "whole rounds");
-  const int listed = min(y.listed, kList);
+  int2 mine[LIST / kSampleThreads];
+  static_assert(LIST % kSampleThreads == 0, "whole rounds");
+  const int listed = min(y.listed, LIST);
 #pragma unroll
-  for (int e = 0; e < kList / kSampleThreads; ++e)
-    if (e * kSampleThreads < listed) mine[e] = y.list[min(e * kSampleThreads + tid, kList - 1)];
+  for (int e = 0; e < LIST / kSampleThreads; ++e)
+    if (e * kSampleThreads < listed) mine[e] = y.list[min(e * kSampleThreads + tid, LIST - 1)];
   __syncthreads();
   if (tid < chunks && n) {
     for (int w = 0; w < wave; ++w) before += y.x.wcnt[w];
@@ -657,7 +661,7 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
   }
   __syncthreads();
 #pragma unroll
-  for (int e = 0; e < kList / kSampleThreads; ++e) {
+  for (int e = 0; e < LIST / kSampleThreads; ++e) {
     const int at = e * kSampleThreads + tid;
     if (at < listed) y.list[at + y.chunk_cnt[mine[e].y / kChunk]] = mine[e];
   }
@@ -666,13 +670,13 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
 // The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the row is read
 // once more for the tokens of these, which are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
 // which part the token is, and only that is read.
-template <typename T, bool FILTERS>
-__global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
+template <typename T, bool FILTERS, int LIST>
+__global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
                                                                      const PartSum* __restrict__ sums, const Spread* __restrict__ spreads,
                                                                      int* __restrict__ tokens, float4* __restrict__ stats) {
   extern __shared__ char lds_[];
-  RowScratch& y = *(RowScratch*)lds_;
+  RowScratch<LIST>& y = *(RowScratch<LIST>*)lds_;
   Scratch& x = y.x;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float u = uniforms[r];
@@ -683,6 +687,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
   uint32_t count = 0;
   float m;
   PartSum mine;
+  // (a thread a bin of each part; the first eight asked for ahead of everything else)
+  u64 s8[8];
+  if constexpr (FILTERS) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s8[i] = spreads[min(i, parts - 1)][tid];
+  }
   const int state = join_parts(sums + (size_t)r * parts, parts, m, mine);
   if (state == -1) { no_token(tokens, stats, r); return; }
   const SampleRow row = {(double)m, a.scale};
@@ -692,9 +702,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
     bool by_k = false, by_p = a.top_p < 1.0;
     if (state == 0) {
       static_assert(kSampleThreads == kBins, "a thread a bin");
-      y.frac[tid] = 0;
+      y.bins.frac[tid] = 0;
       y.cnt[tid] = 0;
-      y.unit[tid] = tid < kBins - 1 ? bin_unit(m, top, tid, a.per_z) : 0.0;
+      y.bins.unit[tid] = tid < kBins - 1 ? bin_unit(m, top, tid, a.per_z) : 0.0;
       if (tid < 64) {
         y.below[tid] = tid < parts && mine.m > -INFINITY ? bins_below(top, bin_of(mine.m, c)) : -1;   // (-1: it has written none)
         y.far[tid] = tid < parts ? mine.count : 0;
@@ -704,24 +714,26 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       __syncthreads();
       auto row_bin = [&](int p, int b) { return min(b + y.below[p], kBins - 1); };
       constexpr u64 kFrac = (1ull << 48) - 1;
-      // a thread a bin of each part, eight loads on their way
       for (int p0 = 0; p0 < parts; p0 += 8) {
-        u64 s[8];
+        u64 next[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = p0 + i < parts && y.below[p0 + i] >= 0 ? spreads[p0 + i][tid] : 0;
+        for (int i = 0; i < 8; ++i) next[i] = spreads[min(p0 + 8 + i, parts - 1)][tid];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (s[i]) {
-            const int to = row_bin(p0 + i, tid);
-            atomicAdd(&y.cnt[to], (uint32_t)(s[i] >> 48));
-            atomicAdd(&y.frac[to], s[i] & kFrac);
+        for (int i = 0; i < 8; ++i) {
+          const int p = min(p0 + i, parts - 1);
+          if (p0 + i < parts && y.below[p] >= 0 && s8[i]) {
+            const int to = row_bin(p, tid);
+            atomicAdd(&y.cnt[to], (uint32_t)(s8[i] >> 48));
+            atomicAdd(&y.bins.frac[to], s8[i] & kFrac);
           }
+          s8[i] = next[i];
+        }
       }
       if (tid < parts && y.far[tid] > 0) atomicAdd(&y.cnt[kBins - 1], (uint32_t)y.far[tid]);
       __syncthreads();
       // a bin a thread, the largest logits first
       const uint32_t n = y.cnt[tid];
-      const u64 s = bin_mass(n, y.frac[tid], y.unit[tid]);
+      const u64 s = bin_mass(n, y.bins.frac[tid], y.bins.unit[tid]);
       u64 cb = wave_before_u64(n), mb = wave_before_u64(s);
       if (lane == 63) { x.wcnt[wave] = (uint32_t)cb + n; x.wsum[wave] = mb + s; }
       __syncthreads();
@@ -759,8 +771,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       __syncthreads();
       // (hi < kBins wherever lo is)
       const int upto_hi = (int)y.cum_cnt[min(hi + 1, kBins)];
-      if (lo < kBins && upto_hi <= kList) mode = PLAN_LISTED;
-      else if (!(by_k && by_p) && upto_hi - (int)y.cum_cnt[lo] <= kList) mode = PLAN_CUT;
+      if (lo < kBins && upto_hi <= LIST) mode = PLAN_LISTED;
+      else if (!(by_k && by_p) && upto_hi - (int)y.cum_cnt[lo] <= LIST) mode = PLAN_CUT;
       by_k = by_k && k_at <= hi;
       by_p = by_p && (by_k || p_at <= hi);
       if (mode == PLAN_CUT) {
@@ -775,7 +787,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             if (p0 + i < parts) {
-              const u64 sum = wave_sum_u64(v[i] ? bin_mass(v[i] >> 48, v[i] & kFrac, y.unit[row_bin(p0 + i, tid)]) : 0);
+              const u64 sum = wave_sum_u64(v[i] ? bin_mass(v[i] >> 48, v[i] & kFrac, y.bins.unit[row_bin(p0 + i, tid)]) : 0);
               if (lane == 0 && sum) atomicAdd(&y.part_kept[p0 + i], sum);
             }
         }
@@ -878,15 +890,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
 }
 
 // ---- launchers ------------------------------------------------------------------------------------
-struct SamplePlanSizes { int ne, parts; };
-// Logits to a thread: the fewest with which a batch of rows makes no more than four blocks for each compute unit.
-constexpr int kSampleBlocks = 1024;
-static SamplePlanSizes sample_sizes(int rows, int V) {
-  for (const int ne : {8, 16, 32}) {
+struct SampleSizes { int ne, parts; };
+// Logits to a thread: the fewest with which a batch of rows makes no more than two blocks for each compute unit; four where nothing is
+// listed, as the part that the token is in is then read again.  us by trace, 32 rows of 126464 without filters, 31 parts and 16: 8.5 + 6.6, 7.9 +
+// 10.8; 34 rows of 152064 with top-p, 19 parts and 10: 10.4 + 25.1, 12.1 + 24.5, the call 37.9, 36.9.
+static SampleSizes sample_sizes(int rows, int V, bool filters) {
+  for (const int ne : {8, 16}) {
     const int parts = (V + kSampleThreads * ne - 1) / (kSampleThreads * ne);
-    if (ne == 32 || (long)rows * parts <= kSampleBlocks) return {ne, parts};
+    if ((long)rows * parts <= (filters ? 512 : 1024)) return {ne, parts};
   }
-  return {32, 1};
+  return {32, (V + kSampleThreads * 32 - 1) / (kSampleThreads * 32)};
 }
 constexpr int kSampleSmall = 16384;   // logits of a row that one block holds in registers
 struct SampleBytes { size_t sums, all; };
@@ -894,18 +907,26 @@ static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) { b.all = 256; return b; }
   if (rows > kSampleBatch) rows = kSampleBatch;
-  size_t most = 0;   // (fewer rows may have more parts between them)
-  for (const int ne : {8, 16, 32}) {
-    const size_t parts = (V + kSampleThreads * ne - 1) / (kSampleThreads * ne);
-    const size_t n = parts * (ne == 32 ? rows : rows * parts <= kSampleBlocks ? rows : kSampleBlocks / parts);
-    if (n > most) most = n;
-  }
+  // (with fewer than 32 logits to a thread there are at most 1024 parts, 512 of them with bins)
+  size_t most = (size_t)rows * ((V + kSampleThreads * 32 - 1) / (kSampleThreads * 32));
+  if (most < 1024) most = 1024;
   b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
   b.all = b.sums + most * sizeof(Spread);
   return b;
 }
 size_t sample_workspace(int rows, int V) { return sample_bytes(rows, V).all; }
 
+template <typename T, bool FILTERS, int LIST>
+static void launch_sample_draw(const T* logits, int rows, int parts, int V, size_t ld, int part_size, const float* uniforms,
+                               const SampleArgs& a, const PartSum* sums, const Spread* spreads, int* tokens, float4* stats, hipStream_t s) {
+  constexpr int smem = sizeof(RowScratch<LIST>);
+  static_assert(smem <= 80 * 1024 && sizeof(RowScratch<kListShort>) <= 160 * 1024 / 3, "two or three blocks to a compute unit");
+  static const hipError_t once = hipFuncSetAttribute((const void*)sample_draw_kernel<T, FILTERS, LIST>,
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  (void)once;
+  sample_draw_kernel<T, FILTERS, LIST><<<rows, kSampleThreads, smem, s>>>(logits, V, ld, parts, part_size, uniforms, a, sums, spreads, tokens,
+                                                                          stats);
+}
 template <typename T, int NE>
 static void launch_sample_ne(const T* logits, int rows, int parts, int V, size_t ld, const float* uniforms, const SampleArgs& a, int* tokens,
                              float4* stats, char* ws, const SampleBytes& b, hipStream_t s) {
@@ -913,16 +934,15 @@ static void launch_sample_ne(const T* logits, int rows, int parts, int V, size_t
   Spread* spreads = (Spread*)(ws + b.sums);
   const dim3 grid(parts, rows);
   if (a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0) {
-    static const hipError_t once = hipFuncSetAttribute((const void*)sample_draw_kernel<T, true>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(RowScratch));
-    (void)once;
     sample_parts_kernel<T, NE, true><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    sample_draw_kernel<T, true><<<rows, kSampleThreads, sizeof(RowScratch), s>>>(logits, V, ld, parts, kSampleThreads * NE, uniforms, a, sums,
-                                                                                 spreads, tokens, stats);
+    // (a few top-k fit a shorter list, and three blocks of it a compute unit instead of two)
+    if (a.top_k > 0 && a.top_k <= kListShort / 2)
+      launch_sample_draw<T, true, kListShort>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
+    else
+      launch_sample_draw<T, true, kList>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
   } else {
     sample_parts_kernel<T, NE, false><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    sample_draw_kernel<T, false><<<rows, kSampleThreads, offsetof(RowScratch, list), s>>>(logits, V, ld, parts, kSampleThreads * NE, uniforms, a,
-                                                                                          sums, spreads, tokens, stats);
+    launch_sample_draw<T, false, 1>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
   }
 }
 
@@ -938,7 +958,7 @@ static void launch_sample_t(const T* logits, int rows, int V, size_t ld, const f
   const SampleBytes b = sample_bytes(rows, V);
   for (int r = 0; r < rows; r += kSampleBatch) {
     const int n = rows - r < kSampleBatch ? rows - r : kSampleBatch;
-    const SamplePlanSizes w = sample_sizes(n, V);
+    const SampleSizes w = sample_sizes(n, V, a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0);
     const T* z = logits + (size_t)r * ld;
     switch (w.ne) {
       case 8: launch_sample_ne<T, 8>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
