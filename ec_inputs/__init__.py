@@ -37,6 +37,7 @@ class ModelCfg:
     logit_scale: float = 1.0
     # storage type of the weights: "f32", "bf16", or "fp8w" = matrices as 8-bit e4m3 codes with one
     # float32 scale per output row (QuantMatrix), everything else (embedding, norm gains) bfloat16.
+    # "mxfp4w": the matrices in microscaled 4-bit floating point (MxMatrix), everything else likewise.
     # The GPU's activations and KV cache are float32 for "f32" and bfloat16 otherwise.
     dtype: str = "f32"
 
@@ -118,6 +119,13 @@ WORKLOADS: Dict[str, Workload] = {
     "llada8b_fp8_l2": Workload("llada8b_fp8_l2", _llada(dtype="fp8w", n_layers=2),
                                DecodeCfg(gen_len=256, block=32, k_recent=2, tokens_per_step=1,
                                          tau=1.0), 512, 2),
+    # the same in microscaled 4-bit floating point: 4.25 bits an element to stream
+    "llada8b_mxfp4": Workload("llada8b_mxfp4", _llada(dtype="mxfp4w"),
+                              DecodeCfg(gen_len=256, block=32, k_recent=2, tokens_per_step=1, tau=1.0),
+                              512, 2),
+    "llada8b_mxfp4_l2": Workload("llada8b_mxfp4_l2", _llada(dtype="mxfp4w", n_layers=2),
+                                 DecodeCfg(gen_len=256, block=32, k_recent=2, tokens_per_step=1,
+                                           tau=1.0), 512, 2),
     # reduced-depth twins (same widths and vocabulary, 2 layers) for whole-generation parity
     "llada8b_l2": Workload("llada8b_l2", _llada(n_layers=2),
                            DecodeCfg(gen_len=256, block=32, k_recent=2, tokens_per_step=1,
@@ -180,6 +188,35 @@ def quantize_rows_e4m3(w: np.ndarray) -> QuantMatrix:
     return QuantMatrix(f32_to_e4m3_bits(w / scale[:, None]), scale)
 
 
+class MxMatrix:
+    """A matrix in microscaled 4-bit floating point: e2m1 codes [out, in / 2], two to a byte (an even column in the
+    low four bits), and a scale byte s to 32 columns, [out, in / 32]; value = 2^(s - 127) * e2m1(code)."""
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes: np.ndarray, scales: np.ndarray):
+        self.codes, self.scales = codes, scales
+
+    ndim = 2
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], 2 * self.codes.shape[1]
+
+
+def quantize_blocks_e2m1(w: np.ndarray) -> MxMatrix:
+    """Scale = the largest power of two that leaves a block's largest magnitude at 4 or more (at least 2^-127), codes =
+    nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with ties to the even code, saturating at 6.  Finite values only."""
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    v = w.reshape(w.shape[0], -1, 32)
+    amax = np.abs(v).max(axis=2)
+    e = np.where(amax > 0, np.frexp(amax)[1] - 3, -127)       # (frexp: a mantissa in [0.5, 1))
+    e = np.maximum(e, -127)
+    a = np.abs(np.ldexp(v.astype(np.float64), -e[:, :, None]))
+    code = np.where(a < 2, np.rint(2 * a), np.where(a < 4, np.rint(a) + 2, np.rint(a / 2) + 4))
+    code = (np.minimum(code, 7).astype(np.uint8) | (np.signbit(v).astype(np.uint8) << 3)).reshape(w.shape[0], -1, 2)
+    return MxMatrix(code[:, :, 0] | (code[:, :, 1] << 4), (e + 127).astype(np.uint8))
+
+
 # ----------------------------------------------------------------------------------------------
 # random draws
 # ----------------------------------------------------------------------------------------------
@@ -236,16 +273,19 @@ def make_weights(cfg: ModelCfg, seed: int, std: float = 0.02, gain_jitter: float
     """
     d, hq, hkv, hd, f, v = (cfg.d_model, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, cfg.d_ffn,
                             cfg.vocab)
-    quant = cfg.dtype == "fp8w"
-    dt = "bf16" if quant else cfg.dtype
+    quant, micro = cfg.dtype == "fp8w", cfg.dtype == "mxfp4w"
+    dt = "bf16" if quant or micro else cfg.dtype
     w: Dict[str, object] = {}
     with ThreadPoolExecutor(max_workers=max(1, threads)) as pool:
         def nt(name, shape):
-            if not quant:
+            if not quant and not micro:
                 return normal_tensor(seed, name, shape, std, dt, pool)
-            # the same float32 draws, then e4m3 codes with per-row scales (row blocks in parallel)
+            # the same float32 draws, then codes and scales (row blocks in parallel)
             x = normal_tensor(seed, name, shape, std, "f32", pool)
             step = max(1, (1 << 22) // shape[1])
+            if micro:
+                parts = list(pool.map(lambda lo: quantize_blocks_e2m1(x[lo:lo + step]), range(0, shape[0], step)))
+                return MxMatrix(np.concatenate([p.codes for p in parts]), np.concatenate([p.scales for p in parts]))
             parts = list(pool.map(lambda lo: quantize_rows_e4m3(x[lo:lo + step]),
                                   range(0, shape[0], step)))
             return QuantMatrix(np.concatenate([p.codes for p in parts]),
@@ -280,5 +320,5 @@ def weight_bytes(cfg: ModelCfg) -> int:
     d, hq, hkv, hd, f, v = (cfg.d_model, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, cfg.d_ffn,
                             cfg.vocab)
     per_layer = (hq + 2 * hkv) * hd * d + d * hq * hd + 3 * f * d
-    esz = {"bf16": 2, "fp8w": 1}.get(cfg.dtype, 4)
-    return (cfg.n_layers * per_layer + v * d) * esz
+    esz = {"bf16": 2, "fp8w": 1, "mxfp4w": 17 / 32}.get(cfg.dtype, 4)
+    return int((cfg.n_layers * per_layer + v * d) * esz)

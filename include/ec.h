@@ -28,11 +28,11 @@
  *  - batch sequences generate side by side and independently (own prompt, mask set, history,
  *    flag, block, cache): a step concatenates the rows each sequence recomputes, so the weights
  *    stream once for all of them; the results equal those of running each sequence alone.
- *    batch > 1 needs the bfloat16 path (EC_BF16 or EC_FP8W).  Per-sequence arguments and results are arrays of
+ *    batch > 1 needs the bfloat16 path (EC_BF16, EC_FP8W or EC_MXFP4W).  Per-sequence arguments and results are arrays of
  *    batch entries in sequence order.
  *  - All matrices are row-major [out_features, in_features] in the model's storage type
- *    (float32, bfloat16, or under EC_FP8W one e4m3 byte per element plus a float32 scale per
- *    row).  Norm gains and the embedding are float32 (EC_F32) or bfloat16.
+ *    (float32, bfloat16, under EC_FP8W one e4m3 byte per element plus a float32 scale per
+ *    row, or under EC_MXFP4W 4-bit codes plus a scale byte for 32).  Norm gains and the embedding are float32 (EC_F32) or bfloat16.
  */
 #ifndef EC_H
 #define EC_H
@@ -55,8 +55,11 @@ typedef struct ec_ctx ec_ctx; /* opaque */
  * float32 scale per output row - value = scale[row] * e4m3(code) - while the embedding, the norm
  * gains, the activations fed to GEMMs and the KV cache are bfloat16 as under EC_BF16.  It halves
  * the bytes a PARTIAL step streams; the arithmetic (bf16 MFMA on the exactly widened codes, fp32
- * accumulation, scales applied to the sums) is otherwise that of EC_BF16. */
-enum { EC_F32 = 0, EC_BF16 = 1, EC_FP8W = 2 };
+ * accumulation, scales applied to the sums) is otherwise that of EC_BF16.
+ * EC_MXFP4W: the same matrices in microscaled 4-bit floating point (EC_T_MXFP4 below, as ec_mx_quantize makes it), everything else as
+ * under EC_FP8W; 4.25 bits to stream an element.  Codes are widened to bf16 with their scale, exactly (a block of scale 253 or 254 may
+ * overflow). */
+enum { EC_F32 = 0, EC_BF16 = 1, EC_FP8W = 2, EC_MXFP4W = 3 };
 /* EC_AUTO: follow the flag set by the previous step; the first step is always FULL. */
 enum { EC_FULL = 0, EC_PARTIAL = 1, EC_AUTO = 2 };
 enum {
@@ -77,7 +80,8 @@ enum {
  * absolute positions, grouped-query attention without mask, SwiGLU MLP, no biases, untied
  * embedding and LM head.  logit_scale multiplies the LM-head output (1.0 = the model as is).
  * Supported (EC_ERR_CONFIG otherwise): head_dim 64 or 128; n_heads a multiple of n_kv_heads;
- * d_model and d_ffn multiples of 8 (bfloat16: of 32, EC_FP8W: of 64, and vocab a multiple of 16);
+ * d_model and d_ffn multiples of 8 (bfloat16: of 32, EC_FP8W: of 64, EC_MXFP4W: of 128, as n_heads *
+ * head_dim then, and vocab a multiple of 16);
  * vocab at most 163840; prompt + generation at most 15000 positions per sequence.
  * bfloat16 path: the sum of squares of a row of the residual stream is kept in 44.20 fixed point
  * (exact to 5e-7 per 16 features, which is all a row needs down to sums of squares of ~1e-3); it
@@ -86,7 +90,7 @@ enum {
 typedef struct {
   int32_t n_layers, d_model, n_heads, n_kv_heads, head_dim, d_ffn, vocab, mask_id;
   float rms_eps, rope_base, logit_scale;
-  int32_t dtype; /* EC_F32 | EC_BF16 | EC_FP8W */
+  int32_t dtype; /* EC_F32 | EC_BF16 | EC_FP8W | EC_MXFP4W */
 } ec_model_cfg;
 
 /* DEVICE pointers, BORROWED.  Per-layer entries are HOST arrays of n_layers DEVICE pointers. */
@@ -113,6 +117,16 @@ typedef struct {
   const float *const *w_gate_scale;   /* [L] of [d_ffn]             */
   const float *const *w_up_scale;
   const float *const *w_down_scale;   /* [L] of [d_model]           */
+  /* EC_MXFP4W only (not looked at otherwise): the scale bytes of the matrix of the same name, [out_features, in_features / 32]; the matrix
+   * itself is its codes, [out_features, in_features / 2], 16-byte aligned */
+  const uint8_t *lm_head_mx;
+  const uint8_t *const *wq_mx;
+  const uint8_t *const *wk_mx;
+  const uint8_t *const *wv_mx;
+  const uint8_t *const *wo_mx;
+  const uint8_t *const *w_gate_mx;
+  const uint8_t *const *w_up_mx;
+  const uint8_t *const *w_down_mx;
 } ec_weights;
 
 /* Decoding parameters: generation length N, block (window) size w, recent-token budget k,

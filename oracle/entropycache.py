@@ -9,7 +9,8 @@ fusion or reordering.  numpy's matmul / einsum serve as the contraction primitiv
 
 Only tests, the smoke check and the bench's cpu_baseline leg may import this module.  It shares
 no code with the HIP path.  Weights arrive in their storage type (float32, bfloat16 bit patterns
-as uint16, or 8-bit e4m3 codes with a float32 scale per row) and are up-cast exactly; all
+as uint16, 8-bit e4m3 codes with a float32 scale per row, or 4-bit e2m1 codes with a power of
+two to 32) and are up-cast exactly; all
 activations are float64.
 
 Readings taken where the paper is silent or inconsistent (each is listed in the design notes):
@@ -80,9 +81,28 @@ def e4m3_values() -> np.ndarray:
 _E4M3 = e4m3_values()
 
 
+def e2m1_values() -> np.ndarray:
+    """The 16 values of the 4-bit e2m1 format (1 sign bit, 2 exponent bits with bias 1, 1 mantissa bit; exponent 0 =
+    subnormals m/2; neither infinities nor NaN), written out from the format's definition."""
+    v = np.empty(16, dtype=np.float64)
+    for c in range(16):
+        sgn, e, m = c >> 3, (c >> 1) & 3, c & 1
+        x = m / 2.0 if e == 0 else (1.0 + m / 2.0) * 2.0 ** (e - 1)
+        v[c] = -x if sgn else x
+    return v
+
+
+_E2M1 = e2m1_values()
+
+
 def to_f64(w) -> np.ndarray:
     """Exact up-cast of a stored tensor: float32/float64 as is, uint16 = bfloat16 bit pattern, an
-    object with `codes` (uint8 e4m3) and `scale` (float32 per row) = scale[row] * e4m3(code)."""
+    object with `codes` (uint8 e4m3) and `scale` (float32 per row) = scale[row] * e4m3(code), one with `codes` (two e2m1
+    codes to a byte, the even column's in the low bits) and `scales` (a byte s to 32 columns) = 2^(s - 127) * e2m1(code)."""
+    if hasattr(w, "scales"):
+        v = np.empty((w.codes.shape[0], 2 * w.codes.shape[1]))
+        v[:, ::2], v[:, 1::2] = _E2M1[w.codes & 15], _E2M1[w.codes >> 4]
+        return v * np.repeat(2.0 ** (w.scales.astype(np.float64) - 127), 32, axis=1)
     if hasattr(w, "codes"):
         return _E4M3[w.codes] * w.scale.astype(np.float64)[:, None]
     if w.dtype == np.uint16:

@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(HERE, "libec.so")
 EC_MAX_N = 32
 EC_MAX_BLOCK = 128
 EC_MAX_BATCH = 64
-EC_F32, EC_BF16, EC_FP8W = 0, 1, 2
+EC_F32, EC_BF16, EC_FP8W, EC_MXFP4W = 0, 1, 2, 3
 EC_FULL, EC_PARTIAL, EC_AUTO = 0, 1, 2
 EC_GATE_MAX_ENTROPY, EC_GATE_ENTROPY_SUM, EC_GATE_MAX_CONFIDENCE = 0, 1, 2
 EC_SCHED_BLOCKS, EC_SCHED_SLIDING = 0, 1
@@ -54,7 +54,8 @@ class ec_weights(C.Structure):
                [(n, C.POINTER(C.c_void_p)) for n in ("attn_norm", "wq", "wk", "wv", "wo",
                                                       "mlp_norm", "w_gate", "w_up", "w_down")] + \
                [("lm_head_scale", C.c_void_p)] + \
-               [(n + "_scale", C.POINTER(C.c_void_p)) for n in QUANT_MATRICES]
+               [(n + "_scale", C.POINTER(C.c_void_p)) for n in QUANT_MATRICES] + \
+               [("lm_head_mx", C.c_void_p)] + [(n + "_mx", C.POINTER(C.c_void_p)) for n in QUANT_MATRICES]
 
 
 class ec_decode_cfg(C.Structure):
@@ -184,7 +185,8 @@ class EcError(RuntimeError):
 def model_cfg_struct(cfg) -> ec_model_cfg:
     return ec_model_cfg(cfg.n_layers, cfg.d_model, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim,
                         cfg.d_ffn, cfg.vocab, cfg.mask_id, cfg.rms_eps, cfg.rope_base,
-                        cfg.logit_scale, {"f32": EC_F32, "bf16": EC_BF16, "fp8w": EC_FP8W}[cfg.dtype])
+                        cfg.logit_scale, {"f32": EC_F32, "bf16": EC_BF16, "fp8w": EC_FP8W,
+                                          "mxfp4w": EC_MXFP4W}[cfg.dtype])
 
 
 def decode_cfg_struct(dec) -> ec_decode_cfg:
@@ -202,9 +204,10 @@ def _i32p(a: np.ndarray):
 
 
 def weights_to_device(cfg, w: Dict[str, object], device="cuda:0") -> Dict[str, object]:
-    """Uploads host weights (float32, uint16 bfloat16 bit patterns, or matrices as e4m3 codes +
-    float32 row scales) as torch device tensors; a quantised matrix `name` becomes the uint8 tensor
-    `name` and the float32 tensor `name_scale`."""
+    """Uploads host weights (float32, uint16 bfloat16 bit patterns, or matrices as codes and scales) as
+    torch device tensors; a matrix `name` in e4m3 becomes the uint8 tensor `name` and the float32 tensor
+    `name_scale`, one in 4 bits the uint8 tensors `name` and `name_mx`.  For a model whose `dtype` is "mxfp4w"
+    matrices that are still float32 or bfloat16 are brought to 4 bits on the device (mxfp4_quantize)."""
     import torch
 
     def up(a: np.ndarray):
@@ -215,7 +218,11 @@ def weights_to_device(cfg, w: Dict[str, object], device="cuda:0") -> Dict[str, o
     out: Dict[str, object] = {}
     for k, v in w.items():
         items = v if isinstance(v, list) else [v]
-        if hasattr(items[0], "codes"):
+        if cfg.dtype == "mxfp4w" and (k in QUANT_MATRICES or k == "lm_head"):
+            pairs = [(up(x.codes), up(x.scales)) if hasattr(x, "codes") else mxfp4_quantize(up(x)) for x in items]
+            out[k] = [c for c, _ in pairs] if isinstance(v, list) else pairs[0][0]
+            out[k + "_mx"] = [s for _, s in pairs] if isinstance(v, list) else pairs[0][1]
+        elif hasattr(items[0], "codes"):
             codes, scales = [up(x.codes) for x in items], [up(x.scale) for x in items]
             out[k] = codes if isinstance(v, list) else codes[0]
             out[k + "_scale"] = scales if isinstance(v, list) else scales[0]
@@ -504,12 +511,13 @@ class EntropyCache:
             arr = (C.c_void_p * L)(*[t.data_ptr() for t in dev_weights[name]])
             self._ptr_arrays[name] = arr
             setattr(ws, name, C.cast(arr, C.POINTER(C.c_void_p)))
-        if cfg.dtype == "fp8w":
-            ws.lm_head_scale = dev_weights["lm_head_scale"].data_ptr()
+        of_scales = {"fp8w": "_scale", "mxfp4w": "_mx"}.get(cfg.dtype)
+        if of_scales:
+            setattr(ws, "lm_head" + of_scales, dev_weights["lm_head" + of_scales].data_ptr())
             for name in QUANT_MATRICES:
-                arr = (C.c_void_p * L)(*[t.data_ptr() for t in dev_weights[name + "_scale"]])
-                self._ptr_arrays[name + "_scale"] = arr
-                setattr(ws, name + "_scale", C.cast(arr, C.POINTER(C.c_void_p)))
+                arr = (C.c_void_p * L)(*[t.data_ptr() for t in dev_weights[name + of_scales]])
+                self._ptr_arrays[name + of_scales] = arr
+                setattr(ws, name + of_scales, C.cast(arr, C.POINTER(C.c_void_p)))
         self._ws = ws
         plen = _i32(self.Ps)
         need = self.lib.ec_workspace_bytes(C.byref(self._mc), C.byref(self._dc), _i32p(plen))

@@ -2,6 +2,7 @@
 // per-step launch sequence (one denoising step of the appendix algorithm), result read-back.
 // All arithmetic of the step runs in the kernels; the host only chooses launch shapes.
 #include <chrono>
+#include <cstddef>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -38,6 +39,8 @@ struct PackedLayer {
   // EC_FP8W: the same matrices as e4m3 fragment pairs, and their row scales in packed row order
   uint8_t *qqkv = nullptr, *qo = nullptr, *qgu = nullptr, *qd = nullptr;
   float *sqkv = nullptr, *so = nullptr, *sgu = nullptr, *sd = nullptr;
+  // EC_MXFP4W: the q's are e2m1 fragments, and these their scale bytes in the same order
+  uint8_t *mqkv = nullptr, *mo = nullptr, *mgu = nullptr, *md = nullptr;
 };
 
 struct Buffers {
@@ -64,9 +67,10 @@ struct Buffers {
   int* attn_tickets;   // [256] arrival counters of the key slices, zero between launches
   std::vector<PackedLayer> pl; bf16_t* lm_head_p;
   uint8_t* lm_head_q = nullptr; float* lm_head_s = nullptr;  // EC_FP8W
+  uint8_t* lm_head_m = nullptr;                              // EC_MXFP4W (with lm_head_q)
 };
 
-// bytes of an activation / KV-cache element (EC_FP8W computes like EC_BF16)
+// bytes of an activation / KV-cache element (EC_FP8W and EC_MXFP4W compute like EC_BF16)
 size_t esize(int dtype) { return dtype == EC_F32 ? 4 : 2; }
 bool bf16_path(int dtype) { return dtype != EC_F32; }
 // keys held per cache slab: the packed bf16 cache is padded to whole 32-key blocks
@@ -172,7 +176,22 @@ void carve(Carver& c, const ec_model_cfg& m, const ec_decode_cfg& d, const Geome
         p.sd = c.take<float>(packed_elems(EPI_RESID, m.d_model, 1));
       }
     }
+    if (m.dtype == EC_MXFP4W)   // half a byte per element, a byte of scale to 32
+      for (PackedLayer& p : b.pl) {
+        auto take = [&](int epi, size_t N, size_t K, uint8_t*& q, uint8_t*& sc) {
+          q = c.take<uint8_t>(packed_elems(epi, N, K) / 2);
+          sc = c.take<uint8_t>(packed_elems(epi, N, K) / 32);
+        };
+        take(EPI_QKV, nq + 2 * nkv, m.d_model, p.qqkv, p.mqkv);
+        take(EPI_RESID, m.d_model, nq, p.qo, p.mo);
+        take(EPI_SWIGLU, 2 * m.d_ffn, m.d_model, p.qgu, p.mgu);
+        take(EPI_RESID, m.d_model, m.d_ffn, p.qd, p.md);
+      }
     b.lm_head_p = c.take<bf16_t>(packed_elems(EPI_LOGITS, m.vocab, m.d_model));
+    if (m.dtype == EC_MXFP4W) {
+      b.lm_head_q = c.take<uint8_t>(packed_elems(EPI_LOGITS, m.vocab, m.d_model) / 2);
+      b.lm_head_m = c.take<uint8_t>(packed_elems(EPI_LOGITS, m.vocab, m.d_model) / 32);
+    }
     if (m.dtype == EC_FP8W) {
       b.lm_head_q = c.take<uint8_t>(packed_elems(EPI_LOGITS, m.vocab, m.d_model));
       b.lm_head_s = c.take<float>(packed_elems(EPI_LOGITS, m.vocab, 1));
@@ -181,8 +200,8 @@ void carve(Carver& c, const ec_model_cfg& m, const ec_decode_cfg& d, const Geome
 }
 
 const char* check_config(const ec_model_cfg* m, const ec_decode_cfg* d, const int32_t* prompt_lens) {
-  if (m->dtype != EC_F32 && m->dtype != EC_BF16 && m->dtype != EC_FP8W)
-    return "dtype must be EC_F32, EC_BF16 or EC_FP8W";
+  if (m->dtype != EC_F32 && m->dtype != EC_BF16 && m->dtype != EC_FP8W && m->dtype != EC_MXFP4W)
+    return "dtype must be EC_F32, EC_BF16, EC_FP8W or EC_MXFP4W";
   if (m->n_layers < 1 || m->d_model < 1 || m->n_heads < 1 || m->n_kv_heads < 1 || m->d_ffn < 1 ||
       m->vocab < 2)
     return "model sizes must be positive";
@@ -199,6 +218,8 @@ const char* check_config(const ec_model_cfg* m, const ec_decode_cfg* d, const in
   }
   if (m->dtype == EC_FP8W && (m->d_model % 64 || m->d_ffn % 64))
     return "EC_FP8W: d_model and d_ffn must be multiples of 64";
+  if (m->dtype == EC_MXFP4W && (m->d_model % 128 || m->d_ffn % 128 || (long)m->n_heads * m->head_dim % 128))
+    return "EC_MXFP4W: d_model, d_ffn and n_heads * head_dim must be multiples of 128";
   if (d->batch < 1 || d->batch > EC_MAX_BATCH) return "batch must be in [1, EC_MAX_BATCH]";
   if (d->batch > 1 && !bf16_path(m->dtype)) return "batch > 1 needs the bfloat16 path";
   if (d->gen_len < 1) return "gen_len must be positive";
@@ -236,6 +257,7 @@ struct ec_ctx {
   ec_decode_cfg d;
   ec_weights w;  // device pointers; per-layer arrays copied into the vectors below
   std::vector<const void*> attn_norm, wq, wk, wv, wo, mlp_norm, w_gate, w_up, w_down;
+  std::vector<const uint8_t*> wq_m, wk_m, wv_m, wo_m, w_gate_m, w_up_m, w_down_m;  // EC_MXFP4W
   std::vector<const float*> wq_s, wk_s, wv_s, wo_s, w_gate_s, w_up_s, w_down_s;  // EC_FP8W
   Geometry g;
   int B, N;
@@ -502,7 +524,7 @@ int forward_bf16(ec_ctx* c, const StepPlan& sp) {
       GemmEpi e{}; e.M = M; e.MT = MT; e.sumsq_in = sums(2 * l); e.d_in = d; e.eps = m.rms_eps;
       e.sum_stride = b.sumsq_stride; e.rowinfo = b.rowinfo; e.cs = b.rope_cs; e.Hq = m.n_heads;
       e.Hkv = m.n_kv_heads; e.hd = hd; e.q_out = q; e.kc = kc; e.vc = vc;
-      e.w_grp = skinny_tiles_per_block(EPI_QKV, nqkv / 16); e.wscale = b.pl[l].sqkv;
+      e.w_grp = skinny_tiles_per_block(EPI_QKV, nqkv / 16); e.wscale = b.pl[l].sqkv; e.wmx = b.pl[l].mqkv;
       launch_gemm_bf16(EPI_QKV, u, R, b.pl[l].wqkv, b.pl[l].qqkv, nqkv, d, e, s); }
     { Scope p(c, EC_K_ATTN);
       launch_attention_mfma(q, kc, vc, R, b.rowinfo, sp.single ? nullptr : b.pairs + c->B + sp.npairs,
@@ -514,19 +536,19 @@ int forward_bf16(ec_ctx* c, const StepPlan& sp) {
       GemmEpi e{}; e.M = M; e.MT = MT; e.h = b.h; e.d = d; e.gain_next = G(c->mlp_norm[l]);
       e.a_next = u; e.sumsq_out = sums(2 * l + 1); e.sum_stride = b.sumsq_stride;
       splits(e, 2 * l);
-      e.w_grp = skinny_tiles_per_block(EPI_RESID, d / 16); e.wscale = b.pl[l].so;
+      e.w_grp = skinny_tiles_per_block(EPI_RESID, d / 16); e.wscale = b.pl[l].so; e.wmx = b.pl[l].mo;
       launch_gemm_bf16(EPI_RESID, attn, R, b.pl[l].wo, b.pl[l].qo, d, nq, e, s); }
     { Scope p(c, EC_K_GATEUP);
       GemmEpi e{}; e.M = M; e.MT = MT; e.sumsq_in = sums(2 * l + 1); e.d_in = d; e.eps = m.rms_eps;
       e.sum_stride = b.sumsq_stride; e.act = act;
-      e.w_grp = skinny_tiles_per_block(EPI_SWIGLU, 2 * F / 16); e.wscale = b.pl[l].sgu;
+      e.w_grp = skinny_tiles_per_block(EPI_SWIGLU, 2 * F / 16); e.wscale = b.pl[l].sgu; e.wmx = b.pl[l].mgu;
       launch_gemm_bf16(EPI_SWIGLU, u, R, b.pl[l].wgu, b.pl[l].qgu, 2 * F, d, e, s); }
     { Scope p(c, EC_K_DOWN);
       GemmEpi e{}; e.M = M; e.MT = MT; e.h = b.h; e.d = d;
       e.gain_next = G(l + 1 < L ? c->attn_norm[l + 1] : c->w.final_norm);
       e.a_next = u; e.sumsq_out = sums(2 * l + 2); e.sum_stride = b.sumsq_stride;
       splits(e, 2 * l + 1);
-      e.w_grp = skinny_tiles_per_block(EPI_RESID, d / 16); e.wscale = b.pl[l].sd;
+      e.w_grp = skinny_tiles_per_block(EPI_RESID, d / 16); e.wscale = b.pl[l].sd; e.wmx = b.pl[l].md;
       launch_gemm_bf16(EPI_RESID, act, R, b.pl[l].wd, b.pl[l].qd, d, F, e, s); }
   }
   // logits only for the blocks' masked rows: the LM head gathers them from `u`
@@ -534,7 +556,7 @@ int forward_bf16(ec_ctx* c, const StepPlan& sp) {
     GemmEpi e{}; e.M = sp.n_lm; e.MT = (sp.n_lm + 15) / 16; e.row_sel = b.lm_sel;
     e.sumsq_in = sums(2 * L); e.d_in = d; e.eps = m.rms_eps; e.sum_stride = b.sumsq_stride;
     e.scale = m.logit_scale; e.logits = b.logits; e.ldc = m.vocab;
-    e.w_grp = skinny_tiles_per_block(EPI_LOGITS, m.vocab / 16); e.wscale = b.lm_head_s;
+    e.w_grp = skinny_tiles_per_block(EPI_LOGITS, m.vocab / 16); e.wscale = b.lm_head_s; e.wmx = b.lm_head_m;
     if (sp.n_lm <= kLmSkinnyRows) {
       // the epilogue reduces the vocabulary itself; the logits go to memory only on request
       e.vparts = b.partials;
@@ -796,6 +818,21 @@ static int init_impl(ec_ctx** out, const ec_model_cfg* model, const ec_weights* 
           !weights->w_down_scale[l])
         return fail(nullptr, EC_ERR_ARG, "EC_FP8W: a per-layer scale pointer is NULL");
   }
+  if (model->dtype == EC_MXFP4W) {
+    if (!weights->lm_head_mx || !weights->wq_mx || !weights->wk_mx || !weights->wv_mx || !weights->wo_mx || !weights->w_gate_mx ||
+        !weights->w_up_mx || !weights->w_down_mx)
+      return fail(nullptr, EC_ERR_ARG, "EC_MXFP4W: a scale pointer is NULL");
+    for (int l = 0; l < model->n_layers; ++l)
+      if (!weights->wq_mx[l] || !weights->wk_mx[l] || !weights->wv_mx[l] || !weights->wo_mx[l] || !weights->w_gate_mx[l] ||
+          !weights->w_up_mx[l] || !weights->w_down_mx[l])
+        return fail(nullptr, EC_ERR_ARG, "EC_MXFP4W: a per-layer scale pointer is NULL");
+    const auto loose = [](const void* p) { return (uintptr_t)p % 16 != 0; };
+    bool off = loose(weights->lm_head);
+    for (int l = 0; l < model->n_layers; ++l)
+      off |= loose(weights->wq[l]) || loose(weights->wk[l]) || loose(weights->wv[l]) || loose(weights->wo[l]) ||
+             loose(weights->w_gate[l]) || loose(weights->w_up[l]) || loose(weights->w_down[l]);
+    if (off) return fail(nullptr, EC_ERR_ARG, "EC_MXFP4W: codes must be 16-byte aligned");
+  }
   size_t need = ec_workspace_bytes(model, decode, prompt_lens);
   if (!workspace) return fail(nullptr, EC_ERR_WORKSPACE, "workspace is NULL");
   if (((uintptr_t)workspace) % kAlign) return fail(nullptr, EC_ERR_WORKSPACE, "workspace is not 256-byte aligned");
@@ -807,7 +844,9 @@ static int init_impl(ec_ctx** out, const ec_model_cfg* model, const ec_weights* 
 
   ec_ctx* c = new (std::nothrow) ec_ctx();
   if (!c) return fail(nullptr, EC_ERR_ARG, "out of host memory");
-  c->m = *model; c->d = *decode; c->w = *weights;
+  c->m = *model; c->d = *decode;
+  // (a caller of other types may hold a structure without the fields at its end)
+  memcpy(&c->w, weights, model->dtype == EC_MXFP4W ? sizeof(ec_weights) : offsetof(ec_weights, lm_head_mx));
   const int L = model->n_layers, B = decode->batch;
   c->attn_norm.assign(weights->attn_norm, weights->attn_norm + L);
   c->wq.assign(weights->wq, weights->wq + L); c->wk.assign(weights->wk, weights->wk + L);
@@ -824,6 +863,13 @@ static int init_impl(ec_ctx** out, const ec_model_cfg* model, const ec_weights* 
     c->w_gate_s.assign(weights->w_gate_scale, weights->w_gate_scale + L);
     c->w_up_s.assign(weights->w_up_scale, weights->w_up_scale + L);
     c->w_down_s.assign(weights->w_down_scale, weights->w_down_scale + L);
+  }
+  if (model->dtype == EC_MXFP4W) {
+    c->wq_m.assign(weights->wq_mx, weights->wq_mx + L); c->wk_m.assign(weights->wk_mx, weights->wk_mx + L);
+    c->wv_m.assign(weights->wv_mx, weights->wv_mx + L); c->wo_m.assign(weights->wo_mx, weights->wo_mx + L);
+    c->w_gate_m.assign(weights->w_gate_mx, weights->w_gate_mx + L);
+    c->w_up_m.assign(weights->w_up_mx, weights->w_up_mx + L);
+    c->w_down_m.assign(weights->w_down_mx, weights->w_down_mx + L);
   }
   c->g = g; c->B = B; c->N = decode->gen_len;
   c->stream = (hipStream_t)hip_stream;
@@ -868,13 +914,27 @@ static int init_impl(ec_ctx** out, const ec_model_cfg* model, const ec_weights* 
     const int hd = c->m.head_dim;
     auto Bp = [](const void* p) { return (const bf16_t*)p; };
     auto Qp = [](const void* p) { return (const uint8_t*)p; };
-    const bool quant = c->m.dtype == EC_FP8W;
+    const bool quant = c->m.dtype == EC_FP8W, micro = c->m.dtype == EC_MXFP4W;
     const int glm = skinny_tiles_per_block(EPI_LOGITS, c->m.vocab / 16);
     for (int l = 0; l < L; ++l) {
       PackedLayer& p = c->b.pl[l];
       const int gq = skinny_tiles_per_block(EPI_QKV, (nq + 2 * nkv) / 16);
       const int go = skinny_tiles_per_block(EPI_RESID, d / 16);
       const int gg = skinny_tiles_per_block(EPI_SWIGLU, 2 * F / 16);
+      if (micro) {   // e2m1 codes and their scales for the weight-streaming kernels, exact bf16 fragments for the tiled ones
+        struct Part { const void* w; const uint8_t* sc; int N, K; uint8_t *q, *m; bf16_t* p; int mode, grp, row0; };
+        const Part parts[] = {
+            {c->wq[l], c->wq_m[l], nq, d, p.qqkv, p.mqkv, p.wqkv, REPACK_ROPE_HALVES, gq, 0},
+            {c->wk[l], c->wk_m[l], nkv, d, p.qqkv, p.mqkv, p.wqkv, REPACK_ROPE_HALVES, gq, nq},
+            {c->wv[l], c->wv_m[l], nkv, d, p.qqkv, p.mqkv, p.wqkv, REPACK_PLAIN, gq, nq + nkv},
+            {c->wo[l], c->wo_m[l], d, nq, p.qo, p.mo, p.wo, REPACK_PLAIN, go, 0},
+            {c->w_gate[l], c->w_gate_m[l], F, d, p.qgu, p.mgu, p.wgu, REPACK_LO8, gg, 0},
+            {c->w_up[l], c->w_up_m[l], F, d, p.qgu, p.mgu, p.wgu, REPACK_HI8, gg, 0},
+            {c->w_down[l], c->w_down_m[l], d, F, p.qd, p.md, p.wd, REPACK_PLAIN, go, 0}};
+        for (const Part& t : parts)
+          launch_repack_weight_e2m1(Qp(t.w), t.sc, t.N, t.K, t.q, t.m, t.p, t.mode, hd, t.grp, t.row0, c->stream);
+        continue;
+      }
       if (!quant) {
         launch_repack_weight(Bp(c->wq[l]), nq, d, p.wqkv, REPACK_ROPE_HALVES, hd, gq, 0, c->stream);
         launch_repack_weight(Bp(c->wk[l]), nkv, d, p.wqkv, REPACK_ROPE_HALVES, hd, gq, nq, c->stream);
@@ -901,7 +961,10 @@ static int init_impl(ec_ctx** out, const ec_model_cfg* model, const ec_weights* 
         launch_repack_rows_f32(t.sc, t.N, t.s, t.mode, hd, t.row0, c->stream);
       }
     }
-    if (!quant) {
+    if (micro) {
+      launch_repack_weight_e2m1(Qp(c->w.lm_head), c->w.lm_head_mx, c->m.vocab, d, c->b.lm_head_q, c->b.lm_head_m, c->b.lm_head_p,
+                                REPACK_PLAIN, hd, glm, 0, c->stream);
+    } else if (!quant) {
       launch_repack_weight(Bp(c->w.lm_head), c->m.vocab, d, c->b.lm_head_p, REPACK_PLAIN, hd, glm, 0,
                            c->stream);
     } else {

@@ -177,6 +177,7 @@ struct GemmEpi {
   int Hq, Hkv, hd;
   bf16_t* q_out;                  // [M, Hq*hd] row-major
   bf16_t* kc; bf16_t* vc;         // the layer's packed caches
+  const uint8_t* wmx;             // nullable: the matrix came as e2m1 codes; their scale bytes, [tile][128 k][lane] in the tiles' order
 };
 
 // First kernel of a step.  From the sequence table it writes the step's row list (rowinfo, one
@@ -231,6 +232,10 @@ bool gemm_bf16_block_shape(int epi, int M_src, int M, int N, int K, size_t piece
 // Wp the same values as bf16 fragments (exact); either may be NULL.  mode / hd / grp / row0 as
 // launch_repack_weight.
 void launch_repack_weight_e4m3(const uint8_t* W, int N, int K, uint8_t* Wq, bf16_t* Wp, int mode,
+                               int hd, int grp, int row0, hipStream_t s);
+// e2m1 source (codes [N, K/2], scales [N, K/32], K a multiple of 128): Wq receives the codes as 1 KiB fragments (128 k), Ws their scale
+// bytes in the same order, Wp the same values as bf16 fragments (exact)
+void launch_repack_weight_e2m1(const uint8_t* W, const uint8_t* scales, int N, int K, uint8_t* Wq, uint8_t* Ws, bf16_t* Wp, int mode,
                                int hd, int grp, int row0, hipStream_t s);
 // dst[row0 + packed row of n] = src[n]: a per-row vector in the packed matrix' row order
 void launch_repack_rows_f32(const float* src, int N, float* dst, int mode, int hd, int row0,

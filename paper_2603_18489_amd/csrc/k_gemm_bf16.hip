@@ -58,6 +58,15 @@ __device__ __forceinline__ bf16x8 e4m3x8_as_bf16x8(uint32_t a, uint32_t b) {
   c.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
   return c.v;
 }
+// 8 e2m1 codes (a dword, lowest four bits first) times the power of two whose exponent bits `scale` has -> 8 bf16 values, exactly
+__device__ __forceinline__ bf16x8 e2m1x8_as_bf16x8(uint32_t a, float scale) {
+  union { bf16x2_t h[4]; bf16x8 v; } c;
+  c.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 0);
+  c.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 1);
+  c.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 2);
+  c.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale, 3);
+  return c.v;
+}
 template <int N> __device__ __forceinline__ void wait_vmcnt() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
@@ -204,20 +213,25 @@ __device__ __forceinline__ void epi_qkv(const GemmEpi& e, int m, int vt, int q4,
 // ---------------------------------------------------------------------------------------------
 // skinny: grid = ceil(n-tiles / NTW) blocks of KS*64 threads
 // ---------------------------------------------------------------------------------------------
-// W8: the weights are e4m3 codes (k_common.h: packed_w8_index), one 1 KiB fragment pair covering
+// WF: how the weights come.  WF_E4M3: e4m3 codes (k_common.h: packed_w8_index), one 1 KiB fragment pair covering
 // 64 k per weight tile and k-step; a lane's 16 bytes are turned into two bf16 MFMA operands in
 // registers (exact), so a k-step is two MFMAs per (weight tile, m-tile) on two activation
 // fragments, KB counts 64-wide steps, and the per-row scales multiply the K-reduced sums.
+// WF_E2M1: e2m1 codes with a scale to 32 of a row's k, a 1 KiB fragment covering 128 k: a lane's 16 bytes are row r's k = 32 g .. 32 g + 31,
+// one scale.  MFMA h of a step takes codes 8 h .. 8 h + 7 of every lane, so that lane's activations are those of k-block g of the step, its
+// 16 bytes at place h.  KB counts 128-wide steps.
 // The LM head of up to 32 rows keeps to 256 registers, with one k-step to a register set: two blocks to a compute unit, one
 // streaming while the other is in its epilogue.  (8 tiles with two steps to a set take 264 and run alone, four rounds of
 // blocks one after the other.)  us by events: 32 rows, 4096 -> 126464 186 -> 179; 3584 -> 152064 207 -> 195.
-constexpr int skinny_waves(int epi, int MT) { return epi == EPI_LOGITS && MT <= 2 ? 2 : 1; }
-template <int EPI, int MT, int NTW, int KS, int U, bool W8 = false>
-__global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT)) void gemm_bf16_skinny_kernel(const u32x4* __restrict__ Ap,
+constexpr int skinny_waves(int epi, int MT, bool w4) { return epi == EPI_LOGITS && MT <= (w4 ? 1 : 2) ? 2 : 1; }
+enum { WF_BF16 = 0, WF_E4M3 = 1, WF_E2M1 = 2 };
+template <int EPI, int MT, int NTW, int KS, int U, int WF = WF_BF16>
+__global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT, WF == 2)) void gemm_bf16_skinny_kernel(const u32x4* __restrict__ Ap,
                                                                    const u32x4* __restrict__ Wp,
                                                                    int total_nt, int KB,
                                                                    int MT_src, GemmEpi e) {
-  constexpr int AW = W8 ? 2 : 1;   // activation fragments per k-step
+  constexpr bool W8 = WF == WF_E4M3, W4 = WF == WF_E2M1;
+  constexpr int AW = W4 ? 4 : W8 ? 2 : 1;   // activation fragments per k-step
   extern __shared__ float4 red[];  // [KS][NTW*MT][64]
   // the wave index is made a scalar so that everything derived from it (the K slice) is
   // provably wave-uniform: MFMA ignores the EXEC mask, so it must never sit under a condition
@@ -242,6 +256,12 @@ __global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT)) void gemm_bf16_skin
     wp[i] = Wp + packed_w_frag(nt, kb_lo, KB, grp) * 64 + lane;
   }
   const size_t wstep = (size_t)grp * 64;  // u32x4 per k-step
+  const uint8_t* sp[NTW];                 // W4: a byte of scale a lane beside its codes
+#pragma unroll
+  for (int i = 0; i < NTW; ++i) {
+    const int nt = nt0 + i < total_nt ? nt0 + i : 0;
+    sp[i] = W4 ? e.wmx + packed_w_frag(nt, kb_lo, KB, grp) * 64 + lane : nullptr;
+  }
   // activation rows may be gathered (LM head: only the block's masked rows)
   const u32x4* ap[MT];
 #pragma unroll
@@ -249,7 +269,8 @@ __global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT)) void gemm_bf16_skin
     int m = j * 16 + (lane & 15);
     int row = m < e.M ? m : 0;
     if constexpr (EPI == EPI_LOGITS) row = (m < e.M && e.row_sel) ? e.row_sel[m] : row;
-    ap[j] = Ap + ((size_t)kb_lo * AW * MT_src + (row >> 4)) * 64 + (lane >> 4) * 16 + (row & 15);
+    ap[j] = W4 ? Ap + ((size_t)(kb_lo * AW + (lane >> 4)) * MT_src + (row >> 4)) * 64 + (row & 15)
+               : Ap + ((size_t)kb_lo * AW * MT_src + (row >> 4)) * 64 + (lane >> 4) * 16 + (row & 15);
   }
 
   constexpr bool NORMED = (EPI == EPI_QKV || EPI == EPI_SWIGLU || EPI == EPI_LOGITS);
@@ -274,23 +295,34 @@ __global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT)) void gemm_bf16_skin
   const int last = nkb > 0 ? nkb - 1 : 0;
   const u32x4 zero4 = {0u, 0u, 0u, 0u};
   u32x4 wa[U][NTW], aa[U][MT * AW], wb[U][NTW], ab[U][MT * AW];
-#define EC_SK_LOAD(WSET, ASET, IT0)                                                        \
+  uint32_t sa[U][W4 ? NTW : 1], sb[U][W4 ? NTW : 1];
+#define EC_SK_LOAD(WSET, ASET, SSET, IT0)                                                        \
   _Pragma("unroll") for (int u = 0; u < U; ++u) {                                          \
     const int it_ = (IT0) + u < last ? (IT0) + u : last;                                   \
     _Pragma("unroll") for (int i = 0; i < NTW; ++i) WSET[u][i] = __builtin_nontemporal_load(&wp[i][(size_t)it_ * wstep]);  \
+    if constexpr (W4)                                                                      \
+      _Pragma("unroll") for (int i = 0; i < NTW; ++i) SSET[u][i] = sp[i][(size_t)it_ * grp * 64];  \
     _Pragma("unroll") for (int j = 0; j < MT; ++j)                                         \
       _Pragma("unroll") for (int h = 0; h < AW; ++h)                                       \
-        ASET[u][j * AW + h] = ap[j][((size_t)it_ * AW + h) * MT_src * 64];                 \
+        ASET[u][j * AW + h] = ap[j][W4 ? (size_t)it_ * AW * MT_src * 64 + h * 16 : ((size_t)it_ * AW + h) * MT_src * 64];  \
   }
 #define EC_SK_ZERO_TAIL(ASET, IT0)                                                         \
   _Pragma("unroll") for (int u = 0; u < U; ++u) {                                          \
     const bool in_ = (IT0) + u < nkb;                                                      \
     _Pragma("unroll") for (int j = 0; j < MT * AW; ++j) ASET[u][j] = in_ ? ASET[u][j] : zero4;  \
   }
-#define EC_SK_MMA(WSET, ASET)                                                              \
+#define EC_SK_MMA(WSET, ASET, SSET)                                                        \
   _Pragma("unroll") for (int u = 0; u < U; ++u)                                            \
     _Pragma("unroll") for (int i = 0; i < NTW; ++i) {                                      \
-      if constexpr (W8) {                                                                  \
+      if constexpr (W4) {                                                                  \
+        const float f_ = __uint_as_float(SSET[u][i] << 23);                                \
+        _Pragma("unroll") for (int h = 0; h < 4; ++h) {                                    \
+          const bf16x8 w_ = e2m1x8_as_bf16x8(WSET[u][i][h], f_);                           \
+          _Pragma("unroll") for (int j = 0; j < MT; ++j)                                   \
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(                           \
+                w_, v4_as_bf16x8(ASET[u][j * AW + (AW > 1 ? h : 0)]), acc[i][j], 0, 0, 0); \
+        }                                                                                  \
+      } else if constexpr (W8) {                                                                  \
         const bf16x8 lo_ = e4m3x8_as_bf16x8(WSET[u][i][0], WSET[u][i][1]);                 \
         const bf16x8 hi_ = e4m3x8_as_bf16x8(WSET[u][i][2], WSET[u][i][3]);                 \
         _Pragma("unroll") for (int j = 0; j < MT; ++j) {                                   \
@@ -305,7 +337,7 @@ __global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT)) void gemm_bf16_skin
               v4_as_bf16x8(WSET[u][i]), v4_as_bf16x8(ASET[u][j]), acc[i][j], 0, 0, 0);     \
       }                                                                                    \
     }
-  EC_SK_LOAD(wa, aa, 0)
+  EC_SK_LOAD(wa, aa, sa, 0)
   // The rows' sum-of-squares counters are fetched behind the first operand loads and turned
   // into 1/rms after the main loop, so neither the loop nor the epilogue waits on them.  All
   // threads load (those without a row of their own read row 0): no branch, so the compiler
@@ -347,22 +379,22 @@ __global__ __launch_bounds__(KS * 64, skinny_waves(EPI, MT)) void gemm_bf16_skin
   // use, which would leave nothing in flight during the MFMAs)
   int it0 = 0;
   for (; it0 + 2 * U < nkb; it0 += 2 * U) {
-    EC_SK_LOAD(wb, ab, it0 + U)
+    EC_SK_LOAD(wb, ab, sb, it0 + U)
     __builtin_amdgcn_sched_barrier(0);
-    EC_SK_MMA(wa, aa)
+    EC_SK_MMA(wa, aa, sa)
     __builtin_amdgcn_sched_barrier(0);
-    EC_SK_LOAD(wa, aa, it0 + 2 * U)
+    EC_SK_LOAD(wa, aa, sa, it0 + 2 * U)
     __builtin_amdgcn_sched_barrier(0);
-    EC_SK_MMA(wb, ab)
+    EC_SK_MMA(wb, ab, sb)
     __builtin_amdgcn_sched_barrier(0);
   }
   // last 1 .. 2U k-steps: nothing left to prefetch; only here can a k-step lie past the slice
-  EC_SK_LOAD(wb, ab, it0 + U)
+  EC_SK_LOAD(wb, ab, sb, it0 + U)
   __builtin_amdgcn_sched_barrier(0);
   EC_SK_ZERO_TAIL(aa, it0)
-  EC_SK_MMA(wa, aa)
+  EC_SK_MMA(wa, aa, sa)
   EC_SK_ZERO_TAIL(ab, it0 + U)
-  EC_SK_MMA(wb, ab)
+  EC_SK_MMA(wb, ab, sb)
 #undef EC_SK_ZERO_TAIL
 #undef EC_SK_LOAD
 #undef EC_SK_MMA
@@ -510,23 +542,23 @@ static void launch_resid_finish(GemmEpi e, int N, hipStream_t s) {
   resid_finish_kernel<<<grid, 256, 0, s>>>(e);
 }
 
-template <int EPI, int MT, int NTW, int KS, int U = 4, bool W8 = false>
+template <int EPI, int MT, int NTW, int KS, int U = 4, int WF = WF_BF16>
 static void launch_skinny_t(const bf16_t* Ap, int MT_src, const void* Wp, int total_nt, int KB,
                             GemmEpi e, hipStream_t s, int ksplit = 1) {
   dim3 grid((total_nt + NTW - 1) / NTW, ksplit);
   if (EPI == EPI_RESID) e.sum_cap = sumsq_cap(grid.x, NTW);
   size_t smem = (size_t)KS * NTW * MT * 64 * sizeof(float4) + MT * 16 * sizeof(float);
   if (EPI == EPI_LOGITS) smem += (size_t)NTW * MT * 16 * sizeof(float4);  // per-tile row tuples
-  if (W8) smem += NTW * 16 * sizeof(float);                               // weight scales
+  if (WF == WF_E4M3) smem += NTW * 16 * sizeof(float);                               // weight scales
   if (smem > 48 * 1024) {
     static bool once = false;
     if (!once) {
-      (void)hipFuncSetAttribute((const void*)gemm_bf16_skinny_kernel<EPI, MT, NTW, KS, U, W8>,
+      (void)hipFuncSetAttribute((const void*)gemm_bf16_skinny_kernel<EPI, MT, NTW, KS, U, WF>,
                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       once = true;
     }
   }
-  gemm_bf16_skinny_kernel<EPI, MT, NTW, KS, U, W8><<<grid, KS * 64, smem, s>>>(
+  gemm_bf16_skinny_kernel<EPI, MT, NTW, KS, U, WF><<<grid, KS * 64, smem, s>>>(
       (const u32x4*)Ap, (const u32x4*)Wp, total_nt, KB, MT_src, e);
 }
 
@@ -574,26 +606,56 @@ static void launch_skinny_mt_w8(const bf16_t* Ap, int MT_src, const void* Wq, in
                                 int KB, const GemmEpi& e, hipStream_t s) {
   if constexpr (EPI == EPI_LOGITS) {
     switch (lm_tiles(total_nt)) {
-      case 8: launch_skinny_t<EPI, MT, 8, 4, 1, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
-      case 4: launch_skinny_t<EPI, MT, 4, 4, 1, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
-      default: launch_skinny_t<EPI, MT, 2, 4, 1, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 8: launch_skinny_t<EPI, MT, 8, 4, 1, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 4: launch_skinny_t<EPI, MT, 4, 4, 1, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      default: launch_skinny_t<EPI, MT, 2, 4, 1, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
     }
   } else if constexpr (EPI == EPI_RESID) {
     if constexpr (MT > 1) {
       if (skinny_splits(MT, KB * 64, e)) {
-        launch_skinny_t<EPI_PARTIAL, MT, kSkinnySplit, 4, 1, true>(Ap, MT_src, Wq, total_nt, KB, e, s, kSkinnySplit);
+        launch_skinny_t<EPI_PARTIAL, MT, kSkinnySplit, 4, 1, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s, kSkinnySplit);
         launch_resid_finish(e, total_nt * 16, s);
         return;
       }
     }
-    launch_skinny_t<EPI, MT, 1, 8, (MT > 3 ? 1 : 2), true>(Ap, MT_src, Wq, total_nt, KB, e, s);
+    launch_skinny_t<EPI, MT, 1, 8, (MT > 3 ? 1 : 2), WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s);
   } else {
     constexpr int U6 = MT > 2 ? 1 : 2, U8 = MT > 3 ? 1 : 2;
     switch (skinny_tiles_per_block(EPI, total_nt)) {
-      case 6: launch_skinny_t<EPI, MT, 6, 4, U6, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
-      case 3: launch_skinny_t<EPI, MT, 3, 8, U8, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
-      case 2: launch_skinny_t<EPI, MT, 2, 8, U8, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
-      default: launch_skinny_t<EPI, MT, 1, 8, U8, true>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 6: launch_skinny_t<EPI, MT, 6, 4, U6, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 3: launch_skinny_t<EPI, MT, 3, 8, U8, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 2: launch_skinny_t<EPI, MT, 2, 8, U8, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      default: launch_skinny_t<EPI, MT, 1, 8, U8, WF_E4M3>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+    }
+  }
+}
+
+// e2m1 weights: KB counts 128-wide k-steps, of which a register set holds one (four activation fragments per m-tile)
+template <int EPI, int MT>
+static void launch_skinny_mt_w4(const bf16_t* Ap, int MT_src, const void* Wq, int total_nt,
+                                int KB, const GemmEpi& e, hipStream_t s) {
+  constexpr int K8 = MT > 2 ? 4 : 8;   // (eight waves have half the registers)
+  if constexpr (EPI == EPI_LOGITS) {
+    switch (lm_tiles(total_nt)) {
+      case 8: launch_skinny_t<EPI, MT, 8, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 4: launch_skinny_t<EPI, MT, 4, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      default: launch_skinny_t<EPI, MT, 2, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+    }
+  } else if constexpr (EPI == EPI_RESID) {
+    if constexpr (MT > 1) {
+      if (skinny_splits(MT, KB * 128, e)) {
+        launch_skinny_t<EPI_PARTIAL, MT, kSkinnySplit, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s, kSkinnySplit);
+        launch_resid_finish(e, total_nt * 16, s);
+        return;
+      }
+    }
+    launch_skinny_t<EPI, MT, 1, (MT > 4 ? 4 : 8), 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s);
+  } else {
+    switch (skinny_tiles_per_block(EPI, total_nt)) {
+      case 6: launch_skinny_t<EPI, MT, (MT > 5 ? 3 : 6), 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;   // (half a group: registers)
+      case 3: launch_skinny_t<EPI, MT, 3, K8, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      case 2: launch_skinny_t<EPI, MT, 2, K8, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      default: launch_skinny_t<EPI, MT, 1, K8, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
     }
   }
 }
@@ -1456,6 +1518,17 @@ template <int EPI>
 static void launch_epi(const bf16_t* Ap, int M_src, const bf16_t* Wp, const void* Wq, int N, int K,
                        const GemmEpi& e, hipStream_t s) {
   const int total_nt = N / 16, KB = K / 32, MT = (e.M + 15) / 16, MT_src = (M_src + 15) / 16;
+  if (Wq && e.wmx && streams_weights(EPI, MT)) {  // weight streaming from e2m1 codes
+    switch (MT) {
+      case 1: launch_skinny_mt_w4<EPI, 1>(Ap, MT_src, Wq, total_nt, K / 128, e, s); break;
+      case 2: launch_skinny_mt_w4<EPI, 2>(Ap, MT_src, Wq, total_nt, K / 128, e, s); break;
+      case 3: launch_skinny_mt_w4<EPI, 3>(Ap, MT_src, Wq, total_nt, K / 128, e, s); break;
+      case 4: launch_skinny_mt_w4<EPI, 4>(Ap, MT_src, Wq, total_nt, K / 128, e, s); break;
+      case 5: if constexpr (EPI != EPI_LOGITS) launch_skinny_mt_w4<EPI, 5>(Ap, MT_src, Wq, total_nt, K / 128, e, s); break;
+      default: if constexpr (EPI != EPI_LOGITS) launch_skinny_mt_w4<EPI, 6>(Ap, MT_src, Wq, total_nt, K / 128, e, s); break;
+    }
+    return;
+  }
   if (Wq && streams_weights(EPI, MT)) {  // weight streaming from e4m3 codes
     switch (MT) {
       case 1: launch_skinny_mt_w8<EPI, 1>(Ap, MT_src, Wq, total_nt, K / 64, e, s); break;

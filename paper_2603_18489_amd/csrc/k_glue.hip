@@ -203,6 +203,39 @@ void launch_repack_weight_e4m3(const uint8_t* W, int N, int K, uint8_t* Wq, bf16
                                                                             hd, grp, row0);
 }
 
+// The same from e2m1 codes with a scale to 32: a thread a block of 32.
+__global__ __launch_bounds__(256) void repack_weight_e2m1_kernel(const uint8_t* __restrict__ W, const uint8_t* __restrict__ scales, int N,
+                                                                 int K, uint8_t* __restrict__ Wq, uint8_t* __restrict__ Ws,
+                                                                 bf16_t* __restrict__ Wp, int mode, int hd, int grp, int row0) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (size_t)N * (K / 32)) return;
+  const int n = (int)(i / (K / 32)), b = (int)(i % (K / 32));
+  const int dn = row0 + repack_row(n, mode, hd);
+  const uint4 v = *(const uint4*)(W + i * 16);
+  const uint8_t sc = scales[i];
+  const size_t at = packed_w_frag(dn >> 4, b >> 2, K / 128, grp) * 64 + (b & 3) * 16 + (dn & 15);
+  *(uint4*)(Wq + at * 16) = v;
+  Ws[at] = sc;
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const float f = __uint_as_float((uint32_t)sc << 23);   // (the conversion takes the exponent bits alone; 255: NaN)
+  const uint32_t codes[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    union { bf16x2 p[4]; uint4 u; } o;
+    o.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[h], f, 0);
+    o.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[h], f, 1);
+    o.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[h], f, 2);
+    o.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[h], f, 3);
+    *(uint4*)(Wp + packed_w_index(dn, b * 32 + h * 8, K / 32, grp)) = o.u;
+  }
+}
+
+void launch_repack_weight_e2m1(const uint8_t* W, const uint8_t* scales, int N, int K, uint8_t* Wq, uint8_t* Ws, bf16_t* Wp, int mode,
+                               int hd, int grp, int row0, hipStream_t s) {
+  const size_t total = (size_t)N * (K / 32);
+  repack_weight_e2m1_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(W, scales, N, K, Wq, Ws, Wp, mode, hd, grp, row0);
+}
+
 __global__ __launch_bounds__(256) void repack_rows_f32_kernel(const float* __restrict__ src, int N,
                                                               float* __restrict__ dst, int mode,
                                                               int hd, int row0) {
