@@ -371,8 +371,9 @@ typedef struct {
  *  tokens     DEVICE int32 [rows]; written.  -1 for a row that holds a NaN or has no finite maximum (all -inf, a +inf)
  *  stats      DEVICE float32 [rows, 4], 16-byte aligned; written: the drawn token's probability among the kept tokens, its probability
  *             e / S among all, how many are kept, the share of S that they hold.  NaN where the token is -1
- *  workspace  DEVICE, 256-byte aligned, >= ec_row_sample_workspace_bytes(rows, vocab) (0 for arguments outside the limits); BORROWED for
- *             the call: calls that overlap in time, and captured graphs that may run side by side, need one each
+ *  workspace  DEVICE, 256-byte aligned, >= ec_row_sample_workspace_bytes(rows, vocab); BORROWED for the call: calls that overlap in time, and
+ *             captured graphs that may run side by side, need one each.  0 bytes: none is needed, and it may be NULL (rows of up to 16384
+ *             logits; also for arguments outside the limits, which the call refuses)
  * Enqueues on hip_stream (NULL = default stream) and returns without synchronising; may be captured into a graph.
  * Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP; ec_last_error(NULL) names the cause. */
 size_t ec_row_sample_workspace_bytes(int32_t rows, int32_t vocab);
@@ -403,7 +404,7 @@ int ec_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, 
  *  rows       0 .. 524288; n 1 .. 1048576; k a multiple of 32, at most 131072
  *  y          DEVICE [rows, n] of y_type (EC_T_F32 or EC_T_BF16), row stride ldy elements, aligned to its elements; written, columns past
  *             n are not
- *  workspace  DEVICE, 256-byte aligned, >= ec_mx_linear_workspace_bytes(x_type, rows, n, k); BORROWED for the call, as ec_row_sample's
+ *  workspace  DEVICE, 256-byte aligned, >= ec_mx_linear_workspace_bytes(x_type, rows, n, k); as ec_row_sample's (0 bytes for many shapes)
  * Enqueue on hip_stream and return without synchronising; may be captured.  Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP. */
 size_t ec_mx_packed_bytes(int32_t n, int32_t k);
 int ec_mx_pack(const uint8_t *codes, const uint8_t *scales, int32_t n, int32_t k, void *packed, size_t packed_bytes,

@@ -321,15 +321,19 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _place(stream, call, *tensors):
+def _place(stream, call, first, *others):
     """Runs call() where the tensors are: on their device, and on `stream` if one is given, whose pool then owns what it
     allocates and which is waited for (as row_entropy does); on the device's current stream otherwise."""
     import torch
-    dev = tensors[0].get_device()
-    _need(dev >= 0 and all(t.get_device() == dev for t in tensors), "tensors must be on one GPU")
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("tensors must be on one GPU")
+    for t in others:
+        if t.get_device() != dev:
+            raise ValueError("tensors must be on one GPU")
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
-            return _place(stream, call, *tensors)
+            return _place(stream, call, first, *others)
     if stream is None:
         return call(_raw_stream(torch, None, dev))
     here = torch.cuda.current_stream()
@@ -341,6 +345,14 @@ def _place(stream, call, *tensors):
             if hasattr(t, "record_stream"):
                 t.record_stream(here)    # the caller goes on with it there
     return out
+
+
+def _workspace(torch, size: int, device):
+    """Workspace and its address, which belong to the current stream; none where none is needed."""
+    if not size:
+        return None, None
+    ws = torch.empty((size,), dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr()
 
 
 def _done(lib, rc: int) -> None:
@@ -381,9 +393,9 @@ def row_sample(logits, uniforms, temperature: float = 1.0, top_k: int = 0, top_p
         tokens = torch.empty((rows,), dtype=torch.int32, device=logits.device)
         stats = torch.empty((rows, 4), dtype=torch.float32, device=logits.device)
         size = lib.ec_row_sample_workspace_bytes(rows, vocab)
-        ws = torch.empty((max(size, 256),), dtype=torch.uint8, device=logits.device)
+        ws, at = _workspace(torch, size, logits.device)
         _done(lib, lib.ec_row_sample(logits.data_ptr(), kind, rows, vocab, ld, uniforms.data_ptr(), C.byref(cfg),
-                                     tokens.data_ptr(), stats.data_ptr(), ws.data_ptr(), size, raw))
+                                     tokens.data_ptr(), stats.data_ptr(), at, size, raw))
         return tokens, stats
     return _place(stream, call, logits, uniforms)
 
@@ -476,9 +488,9 @@ def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
     def call(raw):
         y = torch.empty((rows, w.n), dtype=dtype, device=w.data.device)
         size = lib.ec_mx_linear_workspace_bytes(x_kind, rows, w.n, k)
-        ws = torch.empty((max(size, 256),), dtype=torch.uint8, device=w.data.device)
+        ws, at = _workspace(torch, size, w.data.device)
         _done(lib, lib.ec_mx_linear(tensors[0].data_ptr(), x_scales, x_kind, rows, ld, w.data.data_ptr(), w.n, k,
-                                    y.data_ptr(), kind, w.n, ws.data_ptr(), size, raw))
+                                    y.data_ptr(), kind, w.n, at, size, raw))
         return y
     return _place(stream, call, *tensors)
 

@@ -64,10 +64,10 @@ int ec_row_sample(const void* logits, int32_t type, int32_t rows, int32_t vocab,
   if (!aligned(stats, 16)) return op_fail(EC_ERR_ARG, "stats must be 16-byte aligned");
   if (!aligned(logits, type_bytes(type)) || !aligned(uniforms, 4) || !aligned(tokens, 4))
     return op_fail(EC_ERR_ARG, "logits, uniforms and tokens must be aligned to their elements");
-  if (!workspace || !aligned(workspace, 256))
-    return op_fail(EC_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
-  if (workspace_bytes < ec_row_sample_workspace_bytes(rows, vocab))
-    return op_fail(EC_ERR_WORKSPACE, "workspace smaller than ec_row_sample_workspace_bytes()");
+  if (const size_t need = ec_row_sample_workspace_bytes(rows, vocab)) {
+    if (!workspace || !aligned(workspace, 256)) return op_fail(EC_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
+    if (workspace_bytes < need) return op_fail(EC_ERR_WORKSPACE, "workspace smaller than ec_row_sample_workspace_bytes()");
+  }
   const bool greedy = cfg->temperature == 0.f;
   SampleArgs a;
   a.scale = 1.4426950408889634 / (greedy ? 1.0 : (double)cfg->temperature);
@@ -152,10 +152,10 @@ int ec_mx_linear(const void* x, const uint8_t* x_scales, int32_t x_type, int64_t
     return op_fail(EC_ERR_ARG, "x's row stride must be a multiple of 8 elements, k or more");
   if (ldy < (size_t)n) return op_fail(EC_ERR_ARG, "y's row stride is smaller than n");
   if (!aligned(y, type_bytes(y_type))) return op_fail(EC_ERR_ARG, "y must be aligned to its elements");
-  if (!workspace || !aligned(workspace, 256))
-    return op_fail(EC_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
-  if (workspace_bytes < ec_mx_linear_workspace_bytes(x_type, rows, n, k))
-    return op_fail(EC_ERR_WORKSPACE, "workspace smaller than ec_mx_linear_workspace_bytes()");
+  if (const size_t need = ec_mx_linear_workspace_bytes(x_type, rows, n, k)) {
+    if (!workspace || !aligned(workspace, 256)) return op_fail(EC_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
+    if (workspace_bytes < need) return op_fail(EC_ERR_WORKSPACE, "workspace smaller than ec_mx_linear_workspace_bytes()");
+  }
   launch_mx_linear(x, x_type == EC_T_MXFP4 ? x_scales : nullptr, rows, ld, (const uint8_t*)packed, n, k / 32, y,
                    y_type == EC_T_BF16, ldy, workspace, (hipStream_t)hip_stream);
   return op_done("product kernel");

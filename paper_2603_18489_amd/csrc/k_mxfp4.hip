@@ -30,53 +30,74 @@ __device__ __forceinline__ float mx_to_codes(uint32_t s) {
 // 2^(s - 127) as the conversion from codes takes it: the exponent bits alone; NaN for 255
 __device__ __forceinline__ float mx_to_values(uint32_t s) { return __uint_as_float(s << 23); }
 
-template <typename T>
+// A lane takes 8 values of a block, so that a wave reads 512 neighbours and writes 256 bytes; the block's four lanes find its largest
+// together.  WIDE: rows lie so that 16 bytes can be read at a time.
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const T* __restrict__ x, long rows, int kb, size_t ld,
                                                           uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;   // a block of 32 values
-  if (i >= rows * kb) return;
-  const long row = i / kb;
-  const T* p = x + (size_t)row * ld + (size_t)(i - row * kb) * 32;
-  float v[32], amax = 0.f;
-  bool finite = true;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;   // eight values: four of these are a block
+  if (i >= rows * kb * 4) return;                        // (the lanes of a block go together)
+  const long row = i / (kb * 4);
+  const T* p = x + (size_t)row * ld + (size_t)(i - row * (kb * 4)) * 8;
+  float v[8];
+  if constexpr (!WIDE) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    v[j] = load_f32(p + j);
-    finite &= fabsf(v[j]) < INFINITY;
-    amax = fmaxf(amax, fabsf(v[j]));
+    for (int j = 0; j < 8; ++j) v[j] = load_f32(p + j);
+  } else if constexpr (sizeof(T) == 4) {
+    const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+    const u32x4 a = *(const u32x4*)p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(a[j] << 16); v[2 * j + 1] = __uint_as_float(a[j] & 0xffff0000u); }
   }
-  const uint32_t s = finite ? mx_scale(amax) : 255u;
+  // (as integers, magnitudes order themselves and everything that is not finite is largest)
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  top = max(top, (uint32_t)dpp_i<0xB1>((int)top));
+  top = max(top, (uint32_t)dpp_i<0x4E>((int)top));
+  const bool finite = top < 0x7f800000u;
+  const uint32_t s = finite ? mx_scale(__uint_as_float(top)) : 255u;
   const float f = mx_to_codes(s);
-  uint32_t out[4];
-#pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * d] * f, v[8 * d + 1] * f, 1.f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * d + 2] * f, v[8 * d + 3] * f, 1.f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * d + 4] * f, v[8 * d + 5] * f, 1.f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[8 * d + 6] * f, v[8 * d + 7] * f, 1.f, 3);
-    out[d] = finite ? c : 0u;
-  }
-  *(uint4*)(codes + (size_t)i * 16) = make_uint4(out[0], out[1], out[2], out[3]);
-  scales[i] = (uint8_t)s;
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * f, v[1] * f, 1.f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * f, v[3] * f, 1.f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * f, v[5] * f, 1.f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * f, v[7] * f, 1.f, 3);
+  ((uint32_t*)codes)[i] = finite ? c : 0u;
+  if ((i & 3) == 0) scales[i >> 2] = (uint8_t)s;
 }
 
-template <typename T>
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                             long rows, int kb, T* __restrict__ out, size_t ld) {
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;   // 8 values
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;   // eight values
   if (i >= rows * kb * 4) return;
   const long row = i / (kb * 4);
-  const int at = (int)(i - row * kb * 4);
-  const uint32_t c = *(const uint32_t*)(codes + (size_t)i * 4);
-  const float s = mx_to_values(scales[(size_t)row * kb + (at >> 2)]);
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
-  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
-  const float v[8] = {a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
-  T* p = out + (size_t)row * ld + (size_t)at * 8;
+  const uint32_t c = ((const uint32_t*)codes)[i];
+  const float s = mx_to_values(scales[i >> 2]);
+  T* p = out + (size_t)row * ld + (size_t)(i - row * (kb * 4)) * 8;
+  if constexpr (sizeof(T) == 2 && WIDE) {
+    union { bf16x2 h[4]; uint4 u; } o;
+    o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0);
+    o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1);
+    o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2);
+    o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3);
+    *(uint4*)p = o.u;
+  } else {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+    const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+    if constexpr (WIDE) {
+      *(float4*)p = make_float4(a[0], a[1], b[0], b[1]);
+      *(float4*)(p + 4) = make_float4(d[0], d[1], e[0], e[1]);
+    } else {
+      const float v[8] = {a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) store_f32(p + j, v[j]);
+      for (int j = 0; j < 8; ++j) store_f32(p + j, v[j]);
+    }
+  }
 }
 
 // one thread a block of 32 of the packed matrix; past the matrix' rows and k: zeros
@@ -106,7 +127,7 @@ struct MxProduct {
   const uint8_t* w;          // packed
   int M, N, kb;              // rows of x and of W; blocks of 32 along k
   void* y; size_t ldy;
-  int wide;                  // y takes the four features of a lane in one store
+  int wide, wide16;          // y takes the four features of a lane in one store; 16 bytes of bf16
   uint8_t* spread;           // room for the scales of 4-bit rows in whole dwords
   float* parts; int part_ld; // where K is split over blocks: their sums, [ranges][M][part_ld]; else NULL
 };
@@ -327,6 +348,16 @@ __global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
   }
 }
 
+// Which block of the result: an XCD takes a run of the blocks in an order that goes down 8 blocks of rows, then on along the features, so
+// that what its 32 compute units work on at a time shares rows and features.
+__device__ __forceinline__ void mx_block_xy(int gx, int gy, int& bx, int& by) {
+  const int nb = gx * gy, xcd = blockIdx.x & 7;
+  const int j = xcd * (nb >> 3) + min(xcd, nb & 7) + (int)(blockIdx.x >> 3);
+  const int panel = j / (8 * gx), high = min(8, gy - panel * 8), in = j - panel * 8 * gx;
+  by = panel * 8 + in % high;
+  bx = in / high;
+}
+
 // Many rows: 8 waves (WM x WN), a wave WTM tiles of 16 rows x 64 features.  QS steps of 128 k are a stage; S stages are in LDS, brought there by direct
 // loads, one barrier a stage.  W lies there as it is packed.  Rows of bf16 (256 bytes a step) and of codes (128 bytes, two steps)
 // have their 16-byte chunks at their number XOR the row, so that rows read at the same k hit all banks; the scales of 4-bit rows go
@@ -347,16 +378,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int wm = wave / WN, wn = wave % WN;
   const int kq = mx_tiles_of_k(p.kb), groups = (p.N + 63) / 64;
   const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
-  // An XCD takes a run of the blocks in an order that goes down 8 blocks of rows, then on along the features: what its 32 compute
-  // units work on at a time shares rows and features.
   int bx, by;
-  {
-    const int nb = gx * gy, xcd = blockIdx.x & 7;
-    const int j = xcd * (nb >> 3) + min(xcd, nb & 7) + (blockIdx.x >> 3);
-    const int panel = j / (8 * gx), high = min(8, gy - panel * 8), in = j - panel * 8 * gx;
-    by = panel * 8 + in % high;
-    bx = in / high;
-  }
+  mx_block_xy(gx, gy, bx, by);
   const int m0 = by * T::BM, group0 = bx * WN;
   const int st_all = (kq + QS - 1) / QS;
   const int st_lo = (int)((long)blockIdx.y * st_all / gridDim.y), ns = (int)((long)(blockIdx.y + 1) * st_all / gridDim.y) - st_lo;
@@ -498,6 +521,197 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 }
 
+// Many rows in 4 bits.  As above, with v_mfma_scale_f32_32x32x64 (6.9 PFLOP/s from registers with random operands against 4.5 to 5.7 of
+// 16x16x128, whose instructions one wave cannot issue often enough): 64 k a step, in which a lane has one block of 32 of one of 32 rows, 16
+// bytes, and its scale.  A wave has MF x NF tiles of 32 x 32.  Four steps are a stage, two stages are in LDS.  The operands of a step are
+// read while the step before it is multiplied; at a stage's last step the waves meet, behind which the next stage has landed and this
+// one's place is free for the one after.
+template <int WM, int WN, int MF, int NF> struct MxTile4 {
+  static constexpr int BM = WM * MF * 32, BN = WN * NF * 32;
+  static constexpr int XB = BM * 128, SB = BM * 8, WB = BN / 64 * 2 * (int)kMxGroupBytes, STAGE = XB + SB + WB;
+};
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// y in 16 bytes a lane where it can: lanes l and l + 32 hold row m, features 8 j + 4 (l >> 5) + 0 .. 3 of 32 from n on
+template <typename TY>
+__device__ __forceinline__ void mx_store32(const MxProduct& p, int m, int n, const f32x16& v, bool valid) {
+  const bool hi = (threadIdx.x & 32) != 0;
+  if constexpr (sizeof(TY) == 2) {
+    if (p.wide16) {
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {   // the lower lane ends with both halves of eight features, the upper with those of the next eight
+        const uint32_t a0 = pack2_bf16(v[4 * j], v[4 * j + 1]), a1 = pack2_bf16(v[4 * j + 2], v[4 * j + 3]);
+        const uint32_t b0 = pack2_bf16(v[4 * j + 4], v[4 * j + 5]), b1 = pack2_bf16(v[4 * j + 6], v[4 * j + 7]);
+        const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+        const int f = n + 8 * (j + hi);
+        if (valid && f < p.N) *(uint4*)((bf16_t*)p.y + (size_t)m * p.ldy + f) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+      }
+      return;
+    }
+  }
+  if (valid)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mx_store<TY>(p, m, n + 8 * j + (hi ? 4 : 0), (f32x4){v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]});
+}
+
+template <typename TY, int WM, int WN, int MF, int NF>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void mx_tiled4_kernel(MxProduct p) {
+  typedef MxTile4<WM, WN, MF, NF> T;
+  static_assert(WM * WN == 8 && T::BN % 64 == 0 && T::BM % 64 == 0, "eight waves, whole groups");
+  extern __shared__ char lds_[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, r32 = lane & 31;
+  const int wm = wave / WN, wn = wave % WN;
+  const int kq = mx_tiles_of_k(p.kb), groups = (p.N + 63) / 64;
+  const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
+  int bx, by;
+  mx_block_xy(gx, gy, bx, by);
+  const int m0 = by * T::BM, group0 = bx * (T::BN / 64);
+  const int st_all = (kq + 1) / 2;
+  const int st_lo = (int)((long)blockIdx.y * st_all / gridDim.y), ns = (int)((long)(blockIdx.y + 1) * st_all / gridDim.y) - st_lo;
+
+  // loads of a stage, 16 bytes a lane: rows, W, and what of W is left over, which several waves bring
+  constexpr int XL = T::XB / 8192, WU = T::WB / 16, WL = WU / 512, RL = (WU % 512 + 63) / 64;
+  static_assert(T::XB % 8192 == 0, "whole loads");
+  const char* xsrc[XL];
+  int xchunk[XL];
+#pragma unroll
+  for (int i = 0; i < XL; ++i) {
+    const int u = (i * 8 + wave) * 64 + lane, row = u >> 3;
+    xchunk[i] = (u & 7) ^ (row & 7);
+    xsrc[i] = (const char*)p.x + (size_t)min(m0 + row, p.M - 1) * p.kb * 16;
+  }
+  const char* wsrc[WL + (RL > 0)];
+  int wq[WL + (RL > 0)], wat[WL + (RL > 0)];
+#pragma unroll
+  for (int i = 0; i < WL + (RL > 0); ++i) {
+    wat[i] = i < WL ? i * 8 + wave : WL * 8 + wave % (RL ? RL : 1);
+    const int u = min(wat[i] * 64 + lane, WU - 1), gr = u / 544, off = u - gr * 544, group = group0 + gr < groups ? group0 + gr : 0;
+    wq[i] = off >= 272;
+    wsrc[i] = (const char*)p.w + (size_t)group * kq * kMxGroupBytes + (size_t)(off - wq[i] * 272) * 16;
+  }
+  const bool rest_in = WU % 64 == 0 || wat[WL + (RL > 0) - 1] * 64 + lane < WU;
+  constexpr int SLOADS = T::BM / 32, SL = (SLOADS + 7) / 8;
+  const uint8_t* ssrc[SL];
+  int sat[SL];
+#pragma unroll
+  for (int i = 0; i < SL; ++i) {
+    sat[i] = (i * 8 + wave) % SLOADS;
+    ssrc[i] = p.x_scales + (size_t)min(m0 + (sat[i] % (T::BM / 64)) * 64 + lane, p.M - 1) * p.scale_ld;
+  }
+  auto load = [&](int stage) {
+    const int q0 = (st_lo + min(stage, ns - 1)) * 2;
+    char* to = lds_ + (stage & 1) * T::STAGE;
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+      const int b = q0 * 4 + xchunk[i];   // (past K: codes that are there, times codes of W that are 0)
+      __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(xsrc[i] + (size_t)(b < p.kb ? b : q0 * 4) * 16),
+                                       (void __attribute__((address_space(3)))*)(to + (i * 8 + wave) * 1024), 16, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < SL; ++i)
+      __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(ssrc[i] + (size_t)min(q0 + sat[i] / (T::BM / 64), kq - 1) * 4),
+                                       (void __attribute__((address_space(3)))*)(to + T::XB + sat[i] * 256), 4, 0, 0);
+#pragma unroll
+    for (int i = 0; i < WL + (RL > 0); ++i) {
+      const char* from = wsrc[i] + (size_t)min(q0 + wq[i], kq - 1) * kMxGroupBytes;
+      const auto slot = (void __attribute__((address_space(3)))*)(to + T::XB + T::SB + wat[i] * 1024);
+      if (i < WL || rest_in) __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)from, slot, 16, 0, 0);
+    }
+  };
+
+  f32x16 acc[NF][MF];
+#pragma unroll
+  for (int i = 0; i < NF; ++i)
+#pragma unroll
+    for (int j = 0; j < MF; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  struct Step {
+    u32x4 w[NF], x[MF];
+    int ws[NF], xs[MF];
+  } a, b;
+  // step t of a stage: 64 k, blocks 2 (t & 1) and 2 (t & 1) + 1 of 128 k number t >> 1.  The scales of both steps of these lie in a dword, the
+  // odd step's two bytes up.
+  auto read = [&](Step& s, int stage, int t) {
+    const char* at = lds_ + (stage & 1) * T::STAGE;
+    const int q = t >> 1, blk = 2 * (t & 1) + half;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const int pair = wn * NF + i;   // 32 features: two tiles of a group
+      const char* g = at + T::XB + T::SB + ((pair >> 1) * 2 + q) * (int)kMxGroupBytes;
+      const int place = blk * 16 + (r32 & 15);
+      s.w[i] = *(const u32x4*)(g + (2 * (pair & 1) + (r32 >> 4)) * 1024 + place * 16);
+      s.ws[i] = *(const int*)(g + 4096 + place * 4);
+    }
+#pragma unroll
+    for (int j = 0; j < MF; ++j) {
+      const int row = (wm * MF + j) * 32 + r32;
+      s.x[j] = *(const u32x4*)(at + row * 128 + (((q * 4 + blk) ^ (row & 7)) * 16));
+      s.xs[j] = *(const int*)(at + T::XB + (q * T::BM + row) * 4);
+    }
+  };
+  auto mma = [&](Step& s, bool odd) {
+    // (the scales are shifted here and not where they are read, which would wait for them)
+#pragma unroll
+    for (int i = 0; i < NF; ++i) s.ws[i] >>= 16 * ((wn * NF + i) & 1) + 8 * (r32 >> 4);
+#pragma unroll
+    for (int j = 0; j < MF; ++j) s.xs[j] >>= 8 * half;
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+      for (int j = 0; j < MF; ++j)
+        acc[i][j] = odd ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(s.w[i]), mx_operand(s.x[j]), acc[i][j], 4, 4, 0, s.ws[i], 2, s.xs[j])
+                        : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_operand(s.w[i]), mx_operand(s.x[j]), acc[i][j], 4, 4, 0, s.ws[i], 0, s.xs[j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // (an odd number of 128 k: the last stage's second half is 0)
+  const bool short_end = (kq & 1) && blockIdx.y == gridDim.y - 1;
+  load(0);
+  load(1);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(XL + SL + WL + (RL > 0)) : "memory");
+  block_barrier_nofence();
+  read(a, 0, 0);
+  for (int s = 0; s < ns; ++s) {
+    const bool half_stage = short_end && s == ns - 1;
+    read(b, s, 1);
+    mma(a, false);
+    if (!half_stage) {
+      read(a, s, 2);
+      mma(b, true);
+      read(b, s, 3);
+      mma(a, false);
+    }
+    // the next stage is there for every wave, and this one has been read by all
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    block_barrier_nofence();
+    load(s + 2);
+    read(a, s + 1, 0);
+    mma(b, true);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the last loads, asked for but not used)
+#pragma unroll
+  for (int j = 0; j < MF; ++j) {
+    const int m = m0 + (wm * MF + j) * 32 + r32;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const int n = group0 * 64 + (wn * NF + i) * 32;
+      if (p.parts) {
+        if (m < p.M)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int f = n + 8 * e + 4 * half;
+            if (f < p.N)
+              *(f32x4*)(p.parts + ((size_t)blockIdx.y * p.M + m) * p.part_ld + f) =
+                  (f32x4){acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+          }
+      } else {
+        mx_store32<TY>(p, m, n, acc[i][j], m < p.M);
+      }
+    }
+  }
+}
+
 // scales of 4-bit rows with whole dwords a row: [M][kq][4], 127 past K
 __global__ __launch_bounds__(256) void mx_spread_scales_kernel(const uint8_t* __restrict__ scales, long total, int kb, int kq,
                                                                uint32_t* __restrict__ out) {
@@ -529,17 +743,27 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxProduct p, int parts) {
 // ---- launchers ------------------------------------------------------------------------------------
 size_t mx_packed_bytes(int n, int kb) { return (size_t)((n + 63) / 64) * mx_tiles_of_k(kb) * kMxGroupBytes; }
 
+template <typename T>
+static void launch_quantize_t(const T* x, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const unsigned grid = (unsigned)((rows * kb * 4 + 255) / 256);
+  if ((uintptr_t)x % 16 == 0 && (ld * sizeof(T)) % 16 == 0) mx_quantize_kernel<T, true><<<grid, 256, 0, s>>>(x, rows, kb, ld, codes, scales);
+  else mx_quantize_kernel<T, false><<<grid, 256, 0, s>>>(x, rows, kb, ld, codes, scales);
+}
 void launch_mx_quantize(const void* x, bool bf16, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s) {
-  const unsigned grid = (unsigned)((rows * kb + 255) / 256);
-  if (bf16) mx_quantize_kernel<<<grid, 256, 0, s>>>((const bf16_t*)x, rows, kb, ld, codes, scales);
-  else mx_quantize_kernel<<<grid, 256, 0, s>>>((const float*)x, rows, kb, ld, codes, scales);
+  if (bf16) launch_quantize_t((const bf16_t*)x, rows, kb, ld, codes, scales, s);
+  else launch_quantize_t((const float*)x, rows, kb, ld, codes, scales, s);
 }
 
+template <typename T>
+static void launch_dequantize_t(const uint8_t* codes, const uint8_t* scales, long rows, int kb, T* out, size_t ld, hipStream_t s) {
+  const unsigned grid = (unsigned)((rows * kb * 4 + 255) / 256);
+  if ((uintptr_t)out % 16 == 0 && (ld * sizeof(T)) % 16 == 0) mx_dequantize_kernel<T, true><<<grid, 256, 0, s>>>(codes, scales, rows, kb, out, ld);
+  else mx_dequantize_kernel<T, false><<<grid, 256, 0, s>>>(codes, scales, rows, kb, out, ld);
+}
 void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows, int kb, void* out, bool bf16, size_t ld,
                           hipStream_t s) {
-  const unsigned grid = (unsigned)((rows * kb * 4 + 255) / 256);
-  if (bf16) mx_dequantize_kernel<<<grid, 256, 0, s>>>(codes, scales, rows, kb, (bf16_t*)out, ld);
-  else mx_dequantize_kernel<<<grid, 256, 0, s>>>(codes, scales, rows, kb, (float*)out, ld);
+  if (bf16) launch_dequantize_t(codes, scales, rows, kb, (bf16_t*)out, ld, s);
+  else launch_dequantize_t(codes, scales, rows, kb, (float*)out, ld, s);
 }
 
 void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, uint8_t* packed, hipStream_t s) {
@@ -614,22 +838,39 @@ static void launch_tiled_t(const MxProduct& p, int parts, hipStream_t s) {
   if (parts > 1) mx_join_kernel<TY><<<dim3((p.N + 1023) / 1024, p.M), 256, 0, s>>>(p, parts);
 }
 
+template <typename TY, int WM, int WN, int MF, int NF>
+static void launch_tiled4_t(const MxProduct& p, int parts, hipStream_t s) {
+  typedef MxTile4<WM, WN, MF, NF> T;
+  constexpr int smem = T::STAGE * 2;
+  static_assert(smem <= 160 * 1024, "the stages fit the LDS");
+  static const hipError_t once = hipFuncSetAttribute((const void*)mx_tiled4_kernel<TY, WM, WN, MF, NF>,
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+  (void)once;
+  MxProduct q = p;
+  if (parts == 1) q.parts = nullptr;
+  const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
+  mx_tiled4_kernel<TY, WM, WN, MF, NF><<<dim3(gx * gy, parts), 512, smem, s>>>(q);
+  if (parts > 1) mx_join_kernel<TY><<<dim3((p.N + 1023) / 1024, p.M), 256, 0, s>>>(p, parts);
+}
+
 // Rows x features of a block and ranges of K, by what its rounds of 256 blocks take.  us a stage (128 k of bf16 rows, 256 k of 4-bit ones) and beside
 // the stages, from whole products of K 4096:
-//   bf16   128 x 256 1.65   64 x 256 1.05   128 x 128 1.05   (256 x 128 1.9: never the least)
-//   4 bits 128 x 256 1.60   64 x 256 1.00   128 x 128 1.00   256 x 256 2.75
+//   bf16   128 x 256 1.65 + 3   64 x 256 1.05 + 3   128 x 128 1.05 + 3
+//   4 bits 64 x 256 1.00 + 3    128 x 128 1.00 + 3  (16x16x128: quicker to start)
+//          256 x 256 2.50 + 4.5 192 x 384 2.90 + 4.5  128 x 256 1.40 + 4.5  192 x 256 2.00 + 4.5  (32x32x64)
+enum { MX_128x256, MX_64x256, MX_128x128, MX_256x256_4, MX_192x384_4, MX_128x256_4, MX_192x256_4, MX_SHAPES };
 struct MxTiledShape { int shape, parts; };
 static MxTiledShape pick_tiled(bool x4, int M, int N, int kb) {
-  static const int bm[4] = {128, 64, 128, 256}, bn[4] = {256, 256, 128, 256};
-  static const double stage_us[2][4] = {{1.65, 1.05, 1.05, 1e9}, {1.6, 1.0, 1.0, 2.75}};
+  static const int bm[MX_SHAPES] = {128, 64, 128, 256, 192, 128, 192}, bn[MX_SHAPES] = {256, 256, 128, 256, 384, 256, 256};
+  static const double us16[MX_SHAPES] = {1.65, 1.05, 1.05}, us4[MX_SHAPES] = {0, 1.0, 1.0, 2.5, 2.9, 1.4, 2.0};
   const int stages = x4 ? (mx_tiles_of_k(kb) + 1) / 2 : mx_tiles_of_k(kb);
-  MxTiledShape best = {0, 1};
+  MxTiledShape best = {MX_128x128, 1};
   double least = 1e30;
-  for (int shape = 0; shape < (x4 ? 4 : 3); ++shape)
+  for (int shape = x4 ? 1 : 0; shape < (x4 ? MX_SHAPES : 3); ++shape)
     for (const int parts : {1, 2, 4}) {
       if (parts > 1 && (M > kMxSplitRows || stages < 4 * parts)) continue;
       const long blocks = (long)((M + bm[shape] - 1) / bm[shape]) * ((N + bn[shape] - 1) / bn[shape]) * parts;
-      const double us = (double)((blocks + 255) / 256) * (((stages + parts - 1) / parts) * stage_us[x4][shape] + 3) +
+      const double us = (double)((blocks + 255) / 256) * (((stages + parts - 1) / parts) * (x4 ? us4 : us16)[shape] + (shape < 3 ? 3 : 4.5)) +
                         (parts > 1 ? 4 + (parts + 1) * 4.0 * M * N / 4e6 : 0);
       if (us < least) { least = us; best = {shape, parts}; }
     }
@@ -638,10 +879,13 @@ static MxTiledShape pick_tiled(bool x4, int M, int N, int kb) {
 template <bool X4, typename TY>
 static void launch_tiled(const MxProduct& p, hipStream_t s) {
   const MxTiledShape w = pick_tiled(X4, p.M, p.N, p.kb);
-  if (w.shape == 0) launch_tiled_t<X4, TY, 2, 4, 4>(p, w.parts, s);
-  else if (w.shape == 1) launch_tiled_t<X4, TY, 2, 4, 2>(p, w.parts, s);
-  else if (w.shape == 2) launch_tiled_t<X4, TY, 4, 2, 2>(p, w.parts, s);
-  else if constexpr (X4) launch_tiled_t<X4, TY, 2, 4, 8>(p, w.parts, s);
+  if (w.shape == MX_64x256) { launch_tiled_t<X4, TY, 2, 4, 2>(p, w.parts, s); return; }
+  if (w.shape == MX_128x128) { launch_tiled_t<X4, TY, 4, 2, 2>(p, w.parts, s); return; }
+  if constexpr (!X4) launch_tiled_t<false, TY, 2, 4, 4>(p, w.parts, s);
+  else if (w.shape == MX_256x256_4) launch_tiled4_t<TY, 2, 4, 4, 2>(p, w.parts, s);
+  else if (w.shape == MX_192x384_4) launch_tiled4_t<TY, 2, 4, 3, 3>(p, w.parts, s);
+  else if (w.shape == MX_128x256_4) launch_tiled4_t<TY, 2, 4, 2, 2>(p, w.parts, s);
+  else launch_tiled4_t<TY, 2, 4, 3, 2>(p, w.parts, s);
 }
 
 constexpr int kMxFewRows = 64;   // up to here W is streamed past all rows at once
@@ -667,20 +911,22 @@ static void launch_linear_t(const MxProduct& p, hipStream_t s) {
   }
 }
 
-// parts' sums [ranges][M][N], then the scales of 4-bit rows in whole dwords
-static size_t mx_parts_bytes(long M, int N) {
-  if (M > kMxSplitRows) return 0;
-  return ((size_t)kMxParts * M * ((N + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256;
+// parts' sums [ranges][M][N], then the scales of 4-bit rows in whole dwords.  (These may be wanted for scales that begin at any byte, which is not
+// known here.)
+static size_t mx_parts_bytes(bool x4, long M, int N, int kb) {
+  if (M <= 0) return 0;
+  const int parts = M <= kMxFewRows ? pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts;
+  return parts > 1 ? ((size_t)parts * M * ((N + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256 : 0;
 }
 size_t mx_linear_workspace(bool x4, long M, int N, int kb) {
-  const size_t need = mx_parts_bytes(M, N) + (x4 && M > kMxFewRows ? (size_t)M * mx_tiles_of_k(kb) * 4 : 0);
-  return need < 256 ? 256 : need;
+  return mx_parts_bytes(x4, M, N, kb) + (x4 && M > kMxFewRows ? (size_t)M * mx_tiles_of_k(kb) * 4 : 0);
 }
 
 void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,
                       bool y_bf16, size_t ldy, void* workspace, hipStream_t s) {
   const int wide = N % 4 == 0 && ldy % 4 == 0 && (uintptr_t)y % (y_bf16 ? 8 : 16) == 0;
-  const MxProduct p = {x, x_scales, ld, kb, packed, (int)M, N, kb, y, ldy, wide, (uint8_t*)workspace + mx_parts_bytes(M, N), (float*)workspace, (N + 3) / 4 * 4};
+  const int wide16 = N % 8 == 0 && ldy % 8 == 0 && (uintptr_t)y % 16 == 0;
+  const MxProduct p = {x, x_scales, ld, kb, packed, (int)M, N, kb, y, ldy, wide, wide16, (uint8_t*)workspace + mx_parts_bytes(x_scales != nullptr, M, N, kb), (float*)workspace, (N + 3) / 4 * 4};
   if (x_scales) {
     if (y_bf16) launch_linear_t<true, bf16_t>(p, s);
     else launch_linear_t<true, float>(p, s);

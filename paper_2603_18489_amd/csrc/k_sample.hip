@@ -905,7 +905,7 @@ constexpr int kSampleSmall = 16384;   // logits of a row that one block holds in
 struct SampleBytes { size_t sums, all; };
 static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
-  if (rows <= 0 || V <= kSampleSmall) { b.all = 256; return b; }
+  if (rows <= 0 || V <= kSampleSmall) return b;
   if (rows > kSampleBatch) rows = kSampleBatch;
   // (with fewer than 32 logits to a thread there are at most 1024 parts, 512 of them with bins)
   size_t most = (size_t)rows * ((V + kSampleThreads * 32 - 1) / (kSampleThreads * 32));

@@ -17,7 +17,7 @@ def lib():
 
 
 def sample(lib, logits=P, type=0, rows=4, vocab=100, ld=100, uniforms=P, cfg=(1.0, 0, 1.0, 0.0), tokens=P, stats=P, ws=P, size=None):
-    size = max(lib.ec_row_sample_workspace_bytes(rows, vocab), 256) if size is None else size
+    size = lib.ec_row_sample_workspace_bytes(rows, vocab) if size is None else size
     return lib.ec_row_sample(logits, type, rows, vocab, ld, uniforms, binding.ec_sample_cfg(*cfg) if cfg else None, tokens, stats,
                              ws, size, None)
 
@@ -35,10 +35,11 @@ def test_sample_refuses(lib, bad):
 
 
 def test_sample_workspace(lib):
-    assert sample(lib, ws=None) == sample(lib, ws=P + 128) == ec.EC_ERR_WORKSPACE
-    need = lib.ec_row_sample_workspace_bytes(4, 100)
-    assert need > 0 and sample(lib, size=need - 1) == ec.EC_ERR_WORKSPACE
-    for rows, vocab in ((-1, 100), (65536, 100), (4, 1), (4, 163841)):
+    big = dict(vocab=40000, ld=40000)
+    assert sample(lib, ws=None, **big) == sample(lib, ws=P + 128, **big) == ec.EC_ERR_WORKSPACE
+    need = lib.ec_row_sample_workspace_bytes(4, 40000)
+    assert need > 0 and sample(lib, size=need - 1, **big) == ec.EC_ERR_WORKSPACE
+    for rows, vocab in ((-1, 40000), (65536, 40000), (4, 1), (4, 163841), (4, 16384), (0, 40000)):
         assert lib.ec_row_sample_workspace_bytes(rows, vocab) == 0
     assert sample(lib, rows=0, logits=None, uniforms=None, tokens=None, stats=None, ws=None) == ec.EC_OK
 
@@ -98,12 +99,11 @@ def test_linear_refuses(lib, bad):
 
 
 def test_linear_workspace(lib):
-    assert linear(lib, ws=None) == linear(lib, ws=P + 16) == ec.EC_ERR_WORKSPACE
-    for x_type in (ec.EC_T_BF16, ec.EC_T_MXFP4):
-        for rows, n, k in ((1, 1, 32), (34, 24576, 4096), (2 ** 19, 1000, 64)):
-            need = lib.ec_mx_linear_workspace_bytes(x_type, rows, n, k)
-            assert need > 0
-            assert linear(lib, x_type=x_type, rows=rows, n=n, k=k, ld=k, ldy=n, size=need - 1) == ec.EC_ERR_WORKSPACE
+    for x_type, rows, n, k in ((1, 34, 4096, 12288), (2, 34, 4096, 12288), (1, 128, 4096, 4096), (2, 128, 4096, 4096), (2, 2 ** 19, 1000, 64)):
+        need = lib.ec_mx_linear_workspace_bytes(x_type, rows, n, k)
+        size = dict(x_type=x_type, rows=rows, n=n, k=k, ld=k, ldy=n)
+        assert need > 0
+        assert linear(lib, size=need - 1, **size) == linear(lib, ws=None, **size) == linear(lib, ws=P + 16, **size) == ec.EC_ERR_WORKSPACE
     for args in ((0, 4, 20, 64), (1, -1, 20, 64), (1, 2 ** 19 + 1, 20, 64), (1, 4, 0, 64), (1, 4, 20, 40)):
         assert lib.ec_mx_linear_workspace_bytes(*args) == 0
     assert linear(lib, rows=0, x=None, packed=None, y=None, ws=None) == ec.EC_OK
