@@ -36,6 +36,9 @@ __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
   v += halves(v, other_row);
   return v + halves(v, other_half);
 }
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v) {   // (as wave_min_dpp, of unsigned numbers)
+  return (uint32_t)wave_min_dpp((int)(v ^ 0x80000000u)) ^ 0x80000000u;
+}
 // sum of the lanes below this one: inside rows of 16, then the rows' last lanes to the rows behind them
 template <int CTRL, int ROWS> __device__ __forceinline__ u64 dpp_rows_u64(u64 v) {
   const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
@@ -63,6 +66,11 @@ template <int NE> struct InRegisters {
   template <typename T> __device__ __forceinline__ void fetch(const T* z, int count) {
     n = count;
     first = (threadIdx.x >> 6) * (64 * NE) + (threadIdx.x & 63);
+    if (n == kSampleThreads * NE) {
+#pragma unroll
+      for (int e = 0; e < NE; ++e) v[e] = load_f32(z + first + e * 64);
+      return;
+    }
 #pragma unroll
     for (int e = 0; e < NE; ++e) v[e] = load_f32(z + min(first + e * 64, n - 1));
 #pragma unroll
@@ -165,8 +173,15 @@ __device__ __forceinline__ void find_bin(bool by_mass, u64 want, uint32_t above_
   __syncthreads();
   cx += above_cnt;
   mx += above_mass;
+  u64 total = above_mass;
 #pragma unroll
-  for (int w = 0; w < kSampleWaves; ++w) { cx += w < wave ? x.wcnt[w] : 0u; mx += w < wave ? x.wsum[w] : 0ull; }
+  for (int w = 0; w < kSampleWaves; ++w) {
+    const u64 s = x.wsum[w];
+    cx += w < wave ? x.wcnt[w] : 0u;
+    mx += w < wave ? s : 0ull;
+    total += s;
+  }
+  if (by_mass) want = min(want, total);   // (sums by other bins and by tokens differ by roundings)
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t c = h ? c1 : c0;
@@ -224,9 +239,8 @@ __device__ u64 select_digits(const S& src, const SampleRow& row, bool by_mass, u
       low = min(low, k);
     }
   });
-  // (both at once as maxima)
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { high = max(high, (uint32_t)__shfl_xor((int)high, o, 64)); low = min(low, (uint32_t)__shfl_xor((int)low, o, 64)); }
+  high = ~(uint32_t)wave_min_u32(~high);
+  low = wave_min_u32(low);
   __syncthreads();
   if (lane == 0) x.wsum[wave] = (u64)high << 32 | low;
   __syncthreads();
@@ -254,7 +268,7 @@ __device__ u64 select_digits(const S& src, const SampleRow& row, bool by_mass, u
   }
   const uint32_t prefix = high;
   const u64 each = x.found_mass / x.found_cnt;   // (equal logits, equal weights)
-  const uint32_t ties = by_mass ? (uint32_t)((want - above_mass + each - 1) / each) : (uint32_t)want - above_cnt;
+  const uint32_t ties = by_mass ? min((uint32_t)((want - above_mass + each - 1) / each), x.found_cnt) : (uint32_t)want - above_cnt;
   cut.key = prefix;
   cut.last = INT_MAX;
   if (ties < x.found_cnt) {   // the place of the last of them
@@ -446,6 +460,7 @@ struct PartSum {
   float m;
   int count;   // -1: a NaN.  With filters: the logits of the last bin, -2 where logits are too large for the bins (2^16 T).  Without: all above -inf
   u64 sum;     // (without filters)
+  float of_wave[kSampleWaves];   // the largest of each 64 NE logits in a row, NaN aside
 };
 typedef u64 Spread[kBins];
 
@@ -524,14 +539,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_parts_kernel(const T* _
 #pragma unroll
     for (int w = 0; w < kSampleWaves; ++w) { sum += wsum[w]; count += wcnt[w]; }
   }
-  if (threadIdx.x == 0) sums[out] = PartSum{m, count, sum};
+  if (lane == 0) sums[out].of_wave[wave] = wmax[wave];
+  if (threadIdx.x == 0) { sums[out].m = m; sums[out].count = count; sums[out].sum = sum; }
 }
 
 // Maximum of a row from its parts (a lane each); 0 as it should be, -1: none, or a NaN, -2: too large for bins.
-__device__ __forceinline__ int join_parts(const PartSum* sums, int parts, float& m, PartSum& mine) {
+struct PartHead { float m; int count; u64 sum; };   // (what every kernel wants of a PartSum)
+__device__ __forceinline__ int join_parts(const PartSum* sums, int parts, float& m, PartHead& mine) {
   const int lane = threadIdx.x & 63;
   static_assert(kPartsMax <= 64, "a lane a part");
-  mine = sums[min(lane, parts - 1)];
+  mine = *(const PartHead*)&sums[min(lane, parts - 1)];
   m = wave_max_dpp(mine.m);
   if (__builtin_amdgcn_ballot_w64(mine.count == -1) || !(fabsf(m) < INFINITY)) return -1;
   return __builtin_amdgcn_ballot_w64(mine.count == -2) ? -2 : 0;
@@ -557,10 +574,11 @@ static_assert(offsetof(Scratch, mass) == 0 && sizeof(Scratch::mass) >= kBins * 1
 // CUT: those of lo .. hi; WHOLE: neither will do.
 enum { PLAN_LISTED = 1, PLAN_CUT = 2, PLAN_WHOLE = 3 };
 
-// Lists the tokens of bins `from` .. `hi` in the order of the ids.  A wave takes a chunk at a time, of the parts that reach so high; its
+// Lists the tokens of bins `from` .. `hi` in the order of the ids.  A wave takes a chunk at a time, of those that reach so high; its
 // tokens go to wherever the list has got to, and once all are there a chunk's are moved to behind those of the chunks before it.
 template <typename T, int LIST>
-__device__ __forceinline__ void list_bins(const T* z, int V, int part_size, float c, float top, int from, int hi, RowScratch<LIST>& y) {
+__device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums, int part_size, float c, float top, int from, int hi,
+                                          RowScratch<LIST>& y) {
   constexpr int E = kChunk / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (V + kChunk - 1) / kChunk;
   static_assert(kChunksMax <= 192, "three waves have a chunk a lane");
@@ -584,7 +602,11 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
   if (from > 0) most = first_key(from - 1) - 1;
   const float vmin = logit_of(least), vmax = logit_of(most);
   // the chunks to go through, a lane each
-  u64 n = tid < chunks && y.below[tid * kChunk / part_size] >= 0 && y.below[tid * kChunk / part_size] <= hi;
+  u64 n = 0;
+  if (tid < chunks) {
+    const int part = tid * kChunk / part_size, in = tid * kChunk - part * part_size, per = part_size / kSampleWaves;
+    for (int w = in / per; w <= (in + kChunk - 1) / per; ++w) n |= sums[part].of_wave[w] >= vmin;
+  }
   u64 before = 0;
   if (wave < 3) {
     before = wave_before_u64(n);
@@ -598,16 +620,18 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
   }
   const int active = (int)(y.x.wcnt[0] + y.x.wcnt[1] + y.x.wcnt[2]);
   __syncthreads();
+  // (the last chunk begins early, so that all read whole chunks: rows here have more than one)
+  auto begin = [&](int ch) { return min(ch * kChunk, V - kChunk); };
   auto fetch = [&](float (&v)[E], int i) {
-    const int first = (i < active ? y.chunk_id[i] : 0) * kChunk + lane;
+    const T* from = z + begin(__builtin_amdgcn_readfirstlane(i < active ? y.chunk_id[i] : 0)) + lane;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = load_f32(z + min(first + e * 64, V - 1));
+    for (int e = 0; e < E; ++e) v[e] = load_f32(from + e * 64);
   };
   auto put = [&](float (&v)[E], int i) {
-    const int ch = y.chunk_id[i];
-    if ((ch + 1) * kChunk > V)
+    const int ch = __builtin_amdgcn_readfirstlane(y.chunk_id[i]), first = begin(ch);
+    if (first < ch * kChunk)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = ch * kChunk + e * 64 + lane < V ? v[e] : -INFINITY;
+      for (int e = 0; e < E; ++e) v[e] = first + e * 64 + lane >= ch * kChunk ? v[e] : -INFINITY;
     u64 has[E];
     int n = 0;
 #pragma unroll
@@ -629,7 +653,7 @@ __device__ __forceinline__ void list_bins(const T* z, int V, int part_size, floa
     for (int e = 0; e < E; ++e)
       if (has[e]) {
         const int to = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has[e], 0));
-        if ((has[e] >> lane & 1) && to < LIST) y.list[to] = make_int2(__float_as_int(v[e]), ch * kChunk + e * 64 + lane);
+        if ((has[e] >> lane & 1) && to < LIST) y.list[to] = make_int2(__float_as_int(v[e]), first + e * 64 + lane);
         at += __builtin_popcountll(has[e]);
       }
   };
@@ -686,7 +710,7 @@ __global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T*
   u64 all = 0;
   uint32_t count = 0;
   float m;
-  PartSum mine;
+  PartHead mine;
   // (a thread a bin of each part; the first eight asked for ahead of everything else)
   u64 s8[8];
   if constexpr (FILTERS) {
@@ -799,7 +823,7 @@ __global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T*
       sample_whole(src, row, a, u, r, x, tokens, stats);
       return;
     }
-    if (lo < kBins) list_bins(z, V, part_size, c, top, mode == PLAN_LISTED ? 0 : lo, hi, y);
+    if (lo < kBins) list_bins(z, V, sums + (size_t)r * parts, part_size, c, top, mode == PLAN_LISTED ? 0 : lo, hi, y);
     __syncthreads();
     InList src;
     src.fetch(y.list, lo < kBins ? y.listed : 0);
@@ -828,12 +852,8 @@ __global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T*
         });
         of_k = rank_few(n, y.cum_cnt[at], y.cum_mass[at], by_mass, want, cut, x);
       } else {
-        // (the weights of the bin's tokens, and their sum there, differ by roundings)
-        u64 of_bin = 0;
-        auto in_bin = [&](float v) { return bins_below(top, bin_of(v, c)) == at; };
-        src.each([&](int, float v, bool) { of_bin += v > -INFINITY && in_bin(v) ? row.weight(v) : 0; });
-        of_bin = block_sum_u64(of_bin, x);
-        of_k = select_digits(src, row, by_mass, by_mass ? min(want, y.cum_mass[at] + of_bin) : want, y.cum_cnt[at], y.cum_mass[at], in_bin, cut, x);
+        of_k = select_digits(src, row, by_mass, want, y.cum_cnt[at], y.cum_mass[at],
+                             [&](float v) { return bins_below(top, bin_of(v, c)) == at; }, cut, x);
       }
     }
     if (mode == PLAN_LISTED) {
