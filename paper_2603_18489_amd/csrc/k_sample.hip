@@ -454,8 +454,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* _
 // begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
 // e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1], and what is added for it one number: 2^48 (a count) plus (e^(rho / 16) - 0.99) 2^36,
 // whose sums over the 16384 logits of a part stay below 2^48.
-constexpr int kBins = 512, kList = 5632, kListShort = 3072, kPartsMax = 40, kSampleBatch = 1024;
-constexpr int kChunk = 1024, kChunksMax = 160;   // logits that a wave goes through at a time; of the longest row
+constexpr int kBins = 512, kList = 5632, kPartsMax = 40, kSampleBatch = 1024;
+constexpr int kChunk = 1024, kChunksMax = 192;   // logits that a wave goes through at a time; of the longest row
 struct PartSum {
   float m;
   int count;   // -1: a NaN.  With filters: the logits of the last bin, -2 where logits are too large for the bins (2^16 T).  Without: all above -inf
@@ -581,7 +581,8 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
                                           RowScratch<LIST>& y) {
   constexpr int E = kChunk / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (V + kChunk - 1) / kChunk;
-  static_assert(kChunksMax <= 192, "three waves have a chunk a lane");
+  constexpr int CW = kChunksMax / 64;   // waves with a chunk a lane
+  static_assert(kChunksMax % 64 == 0 && CW <= kSampleWaves, "a lane a chunk");
   // The lowest logit of bin hi, the highest of bin `from`: bins go with the logits' order, so bisect it.
   auto logit_of = [](uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); };
   uint32_t least = 0x00800000u, most = 0xff7fffffu;   // (keys of the lowest and the highest finite value)
@@ -608,17 +609,19 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
     for (int w = in / per; w <= (in + kChunk - 1) / per; ++w) n |= sums[part].of_wave[w] >= vmin;
   }
   u64 before = 0;
-  if (wave < 3) {
+  if (wave < CW) {
     before = wave_before_u64(n);
     if (lane == 63) y.x.wcnt[wave] = (uint32_t)(before + n);
   }
   __syncthreads();
-  if (wave < 3) {
+  if (wave < CW) {
     for (int w = 0; w < wave; ++w) before += y.x.wcnt[w];
     if (n) y.chunk_id[before] = tid;
     if (tid < chunks) y.chunk_cnt[tid] = 0;
   }
-  const int active = (int)(y.x.wcnt[0] + y.x.wcnt[1] + y.x.wcnt[2]);
+  int active = 0;
+#pragma unroll
+  for (int w = 0; w < CW; ++w) active += (int)y.x.wcnt[w];
   __syncthreads();
   // (the last chunk begins early, so that all read whole chunks: rows here have more than one)
   auto begin = [&](int ch) { return min(ch * kChunk, V - kChunk); };
@@ -667,7 +670,7 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
   }
   __syncthreads();
   // where each chunk's tokens go
-  if (wave < 3) {
+  if (wave < CW) {
     n = tid < chunks ? y.chunk_cnt[tid] : 0;
     before = wave_before_u64(n);
     if (lane == 63) y.x.wcnt[wave] = (uint32_t)(before + n);
@@ -695,7 +698,7 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
 // once more for the tokens of these, which are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
 // which part the token is, and only that is read.
 template <typename T, bool FILTERS, int LIST>
-__global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
+__global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
                                                                      const PartSum* __restrict__ sums, const Spread* __restrict__ spreads,
                                                                      int* __restrict__ tokens, float4* __restrict__ stats) {
@@ -711,11 +714,11 @@ __global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T*
   uint32_t count = 0;
   float m;
   PartHead mine;
-  // (a thread a bin of each part; the first eight asked for ahead of everything else)
-  u64 s8[8];
+  // (a thread a bin of each part; the first four asked for ahead of everything else)
+  u64 s4[4];
   if constexpr (FILTERS) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s8[i] = spreads[min(i, parts - 1)][tid];
+    for (int i = 0; i < 4; ++i) s4[i] = spreads[min(i, parts - 1)][tid];
   }
   const int state = join_parts(sums + (size_t)r * parts, parts, m, mine);
   if (state == -1) { no_token(tokens, stats, r); return; }
@@ -738,19 +741,19 @@ __global__ __launch_bounds__(kSampleThreads, 4) void sample_draw_kernel(const T*
       __syncthreads();
       auto row_bin = [&](int p, int b) { return min(b + y.below[p], kBins - 1); };
       constexpr u64 kFrac = (1ull << 48) - 1;
-      for (int p0 = 0; p0 < parts; p0 += 8) {
-        u64 next[8];
+      for (int p0 = 0; p0 < parts; p0 += 4) {
+        u64 next[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) next[i] = spreads[min(p0 + 8 + i, parts - 1)][tid];
+        for (int i = 0; i < 4; ++i) next[i] = spreads[min(p0 + 4 + i, parts - 1)][tid];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
           const int p = min(p0 + i, parts - 1);
-          if (p0 + i < parts && y.below[p] >= 0 && s8[i]) {
+          if (p0 + i < parts && y.below[p] >= 0 && s4[i]) {
             const int to = row_bin(p, tid);
-            atomicAdd(&y.cnt[to], (uint32_t)(s8[i] >> 48));
-            atomicAdd(&y.bins.frac[to], s8[i] & kFrac);
+            atomicAdd(&y.cnt[to], (uint32_t)(s4[i] >> 48));
+            atomicAdd(&y.bins.frac[to], s4[i] & kFrac);
           }
-          s8[i] = next[i];
+          s4[i] = next[i];
         }
       }
       if (tid < parts && y.far[tid] > 0) atomicAdd(&y.cnt[kBins - 1], (uint32_t)y.far[tid]);
@@ -915,11 +918,9 @@ struct SampleSizes { int ne, parts; };
 // listed, as the part that the token is in is then read again.  us by trace, 32 rows of 126464 without filters, 31 parts and 16: 8.5 + 6.6, 7.9 +
 // 10.8; 34 rows of 152064 with top-p, 19 parts and 10: 10.4 + 25.1, 12.1 + 24.5, the call 37.9, 36.9.
 static SampleSizes sample_sizes(int rows, int V, bool filters) {
-  for (const int ne : {8, 16}) {
-    const int parts = (V + kSampleThreads * ne - 1) / (kSampleThreads * ne);
-    if ((long)rows * parts <= (filters ? 512 : 1024)) return {ne, parts};
-  }
-  return {32, (V + kSampleThreads * 32 - 1) / (kSampleThreads * 32)};
+  const int parts = (V + kSampleThreads * 8 - 1) / (kSampleThreads * 8);
+  if ((long)rows * parts <= (filters ? 512 : 1024)) return {8, parts};
+  return {16, (V + kSampleThreads * 16 - 1) / (kSampleThreads * 16)};
 }
 constexpr int kSampleSmall = 16384;   // logits of a row that one block holds in registers
 struct SampleBytes { size_t sums, all; };
@@ -928,7 +929,7 @@ static SampleBytes sample_bytes(int rows, int V) {
   if (rows <= 0 || V <= kSampleSmall) return b;
   if (rows > kSampleBatch) rows = kSampleBatch;
   // (with fewer than 32 logits to a thread there are at most 1024 parts, 512 of them with bins)
-  size_t most = (size_t)rows * ((V + kSampleThreads * 32 - 1) / (kSampleThreads * 32));
+  size_t most = (size_t)rows * ((V + kSampleThreads * 16 - 1) / (kSampleThreads * 16));
   if (most < 1024) most = 1024;
   b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
   b.all = b.sums + most * sizeof(Spread);
@@ -940,7 +941,7 @@ template <typename T, bool FILTERS, int LIST>
 static void launch_sample_draw(const T* logits, int rows, int parts, int V, size_t ld, int part_size, const float* uniforms,
                                const SampleArgs& a, const PartSum* sums, const Spread* spreads, int* tokens, float4* stats, hipStream_t s) {
   constexpr int smem = sizeof(RowScratch<LIST>);
-  static_assert(smem <= 80 * 1024 && sizeof(RowScratch<kListShort>) <= 160 * 1024 / 3, "two or three blocks to a compute unit");
+  static_assert(smem <= 80 * 1024, "two blocks to a compute unit");
   static const hipError_t once = hipFuncSetAttribute((const void*)sample_draw_kernel<T, FILTERS, LIST>,
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, smem);
   (void)once;
@@ -955,11 +956,7 @@ static void launch_sample_ne(const T* logits, int rows, int parts, int V, size_t
   const dim3 grid(parts, rows);
   if (a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0) {
     sample_parts_kernel<T, NE, true><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    // (a few top-k fit a shorter list, and three blocks of it a compute unit instead of two)
-    if (a.top_k > 0 && a.top_k <= kListShort / 2)
-      launch_sample_draw<T, true, kListShort>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
-    else
-      launch_sample_draw<T, true, kList>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
+    launch_sample_draw<T, true, kList>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
   } else {
     sample_parts_kernel<T, NE, false><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
     launch_sample_draw<T, false, 1>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
@@ -980,11 +977,8 @@ static void launch_sample_t(const T* logits, int rows, int V, size_t ld, const f
     const int n = rows - r < kSampleBatch ? rows - r : kSampleBatch;
     const SampleSizes w = sample_sizes(n, V, a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0);
     const T* z = logits + (size_t)r * ld;
-    switch (w.ne) {
-      case 8: launch_sample_ne<T, 8>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
-      case 16: launch_sample_ne<T, 16>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
-      default: launch_sample_ne<T, 32>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s); break;
-    }
+    if (w.ne == 8) launch_sample_ne<T, 8>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s);
+    else launch_sample_ne<T, 16>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s);
   }
 }
 void launch_sample_rows(const void* logits, bool bf16, int rows, int V, size_t ld, const float* uniforms, const SampleArgs& a,
