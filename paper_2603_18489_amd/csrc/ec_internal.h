@@ -3,10 +3,21 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/ec.h"
 #include "k_common.h"
 
 namespace ec {
+
+// The dynamic LDS that a kernel is launched with, allowed once on each device that launches it; `done` is that kernel's own set of devices.
+inline void allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int device = 0;
+  if (hipGetDevice(&device) != hipSuccess) return;   // (the launch reports it)
+  const uint64_t bit = 1ull << (device & 63);
+  if (done.load(std::memory_order_acquire) & bit) return;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+}
 
 // Device-resident scalar state of one sequence (the algorithm's t, flag, counters, block).
 struct DevState {

@@ -174,13 +174,17 @@ enum { MX_RING = 0, MX_REGS = 1, MX_X4 = 2 };   // where a wave's rows go: bf16 
 // waves share that out, and their sums meet in LDS in the order of the waves.  What a wave multiplies next is on its way while
 // it multiplies: R sets of operands, W in registers, bf16 rows by direct loads to a ring in LDS of the wave's own (which takes no
 // registers and no barrier): rows of 256 bytes, their 16-byte chunks at their number XOR the row, so that 16 rows read at the same k hit all banks.
-template <int XF, typename TY, int MT, int NTW, int KS>
-__global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
+// NW > 1 is for many features: NW waves with tiles of their own share a ring, each bringing its part of the rows, and a barrier a step.  The rows then pass
+// into LDS once for NW * NTW tiles, and the short sums let several blocks lie on a compute unit, whose waves together keep HBM busy.
+template <int XF, typename TY, int MT, int NTW, int KS, int NW>
+__global__ __launch_bounds__(KS * NW * 64) void mx_rows_kernel(MxProduct p) {
   constexpr int R = 2;
+  static_assert(NW == 1 || XF == MX_RING, "waves that share their rows");
   constexpr bool X4 = XF == MX_X4, RING = XF == MX_RING;
   extern __shared__ f32x4 red[];   // the rings; then [KS][NTW * MT][64]
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
-  const int kq = mx_tiles_of_k(p.kb), groups = (p.N + 63) / 64, tile0 = blockIdx.x * NTW;
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave_all / NW, wn = wave_all % NW;
+  const int kq = mx_tiles_of_k(p.kb), groups = (p.N + 63) / 64, tile0 = (blockIdx.x * NW + wn) * NTW;
   const int klo = (int)((long)blockIdx.y * kq / gridDim.y), kn = (int)((long)(blockIdx.y + 1) * kq / gridDim.y) - klo;
   const int lo = klo + (int)((long)wave * kn / KS), n = klo + (int)((long)(wave + 1) * kn / KS) - lo;
   const uint8_t* wp[NTW];
@@ -190,7 +194,7 @@ __global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
     wp[i] = p.w + ((size_t)(t >> 2) * kq + lo) * kMxGroupBytes + (t & 3) * 1024 + lane * 16;
   }
   // A tile's scale is the byte of its number in its group's dword; NTW tiles lie in GW groups.
-  constexpr int GW = NTW == 1 ? 1 : (NTW + 5) / 4 < (NTW + 3) / 4 ? 1 : NTW % 4 ? (NTW + 5) / 4 : NTW / 4;
+  constexpr int GW = NTW > 4 ? 2 : 1;
   static_assert(NTW == 1 || NTW == 2 || NTW == 4 || NTW == 6 || NTW == 8, "the bytes below");
   const uint8_t* sp[GW];
 #pragma unroll
@@ -201,11 +205,11 @@ __global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
   const int first_byte = tile0 & 3;
   // To registers: the lane's own row of each tile.  To LDS: the row of which the lane brings 16 bytes, four rows a load.
   constexpr int XL = RING ? MT * 4 : MT, XN = X4 ? 1 : 4;
-  const char* xp[XL];
+  const char* xp[XL / NW];
   const uint8_t* xs[MT];
 #pragma unroll
-  for (int j = 0; j < XL; ++j) {
-    const int row = RING ? j * 4 + g : j * 16 + r, m = row < p.M ? row : 0;
+  for (int j = 0; j < XL / NW; ++j) {
+    const int row = RING ? (j * NW + wn) * 4 + g : j * 16 + r, m = row < p.M ? row : 0;
     xp[j] = X4 ? (const char*)p.x + (size_t)m * p.kb * 16 : (const char*)p.x + (size_t)m * p.ld * 2;
     if constexpr (X4) xs[j] = p.x_scales + (size_t)m * p.scale_ld;
   }
@@ -235,10 +239,11 @@ __global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < XL; ++j) {
+      for (int j0 = 0; j0 < XL; j0 += NW) {   // (waves with the same rows bring every NW-th)
+        const int j = j0 + wn;
         int c = r ^ ((j * 4 + g) & 15);
         c = q * 4 + (c >> 2) < p.kb ? c : 0;
-        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(xp[j] + (size_t)q * 256 + c * 16),
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)(xp[j0 / NW] + (size_t)q * 256 + c * 16),
                                          (void __attribute__((address_space(3)))*)(ring + s * (MT * 4096) + j * 1024), 16, 0, 0);
       }
     }
@@ -303,7 +308,23 @@ __global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
       }
     }
   };
-  if (n > 0) {
+  if constexpr (NW > 1) {
+    // The waves that share a ring meet at each step, behind which its rows are there for both and the other place is free.
+    const int most = (kn + KS - 1) / KS;
+    if (n > 0) load(0, 0);
+    for (int it = 0; it < most; it += 2) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (it + s < most) {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          block_barrier_nofence();
+          if (it + s + 1 < n) load(s ^ 1, it + s + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          if (it + s < n) mma(s, it + s);
+        }
+      }
+    }
+  } else if (n > 0) {
 #pragma unroll
     for (int s = 0; s < R - 1; ++s) load(s, s);
     for (int it = 0;; it += R) {
@@ -331,13 +352,14 @@ __global__ __launch_bounds__(KS * 64) void mx_rows_kernel(MxProduct p) {
 #pragma unroll
   for (int i = 0; i < NTW; ++i)
 #pragma unroll
-    for (int j = 0; j < MT; ++j) red[(wave * UNITS + i * MT + j) * 64 + lane] = acc[i][j];
+    for (int j = 0; j < MT; ++j) red[(wave_all * UNITS + i * MT + j) * 64 + lane] = acc[i][j];
   __syncthreads();
-  for (int o = threadIdx.x; o < UNITS * 64; o += KS * 64) {
+  for (int o = threadIdx.x; o < NW * UNITS * 64; o += KS * NW * 64) {
     f32x4 v = red[o];
 #pragma unroll
-    for (int w = 1; w < KS; ++w) v += red[w * UNITS * 64 + o];
-    const int l = o & 63, unit = o >> 6, i = unit / MT, m = (unit - i * MT) * 16 + (l & 15), f = (tile0 + i) * 16 + (l >> 4) * 4;
+    for (int w = 1; w < KS; ++w) v += red[w * NW * UNITS * 64 + o];
+    const int l = o & 63, unit = o >> 6, i = unit / MT, m = (unit - i * MT) * 16 + (l & 15);
+    const int f = (blockIdx.x * NW * NTW + i) * 16 + (l >> 4) * 4;
     if (m < p.M) {
       if (p.parts) {
         if (f < p.N) *(f32x4*)(p.parts + ((size_t)blockIdx.y * p.M + m) * p.part_ld + f) = v;
@@ -771,23 +793,22 @@ void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, 
   mx_pack_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(codes, scales, n, kb, total, packed);
 }
 
-constexpr int mx_rows_lds(int xf, int mt, int ntw, int ks) {
-  const int ring = xf == MX_RING ? ks * 2 * mt * 4096 : 0, sums = ks * ntw * mt * 1024;
+constexpr int mx_rows_lds(int xf, int mt, int ntw, int ks, int nw = 1) {
+  const int ring = xf == MX_RING ? ks * 2 * mt * 4096 : 0, sums = ks * nw * ntw * mt * 1024;
   return ring > sums ? ring : sums;
 }
-template <int XF, typename TY, int MT, int NTW, int KS>
+template <int XF, typename TY, int MT, int NTW, int KS, int NW = 1>
 static void launch_rows_t(const MxProduct& p, int parts, hipStream_t s) {
-  constexpr int smem = mx_rows_lds(XF, MT, NTW, KS);
+  constexpr int smem = mx_rows_lds(XF, MT, NTW, KS, NW);
   static_assert(smem <= 160 * 1024, "the rings and the waves' sums fit the LDS");
   if constexpr (smem > 48 * 1024) {
-    static const hipError_t once = hipFuncSetAttribute((const void*)mx_rows_kernel<XF, TY, MT, NTW, KS>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    (void)once;
+    static std::atomic<uint64_t> done{0};
+    allow_lds((const void*)mx_rows_kernel<XF, TY, MT, NTW, KS, NW>, smem, done);
   }
   const int tiles = (p.N + 15) / 16;
   MxProduct q = p;
   if (parts == 1) q.parts = nullptr;
-  mx_rows_kernel<XF, TY, MT, NTW, KS><<<dim3((tiles + NTW - 1) / NTW, parts), KS * 64, smem, s>>>(q);
+  mx_rows_kernel<XF, TY, MT, NTW, KS, NW><<<dim3((tiles + NW * NTW - 1) / (NW * NTW), parts), KS * NW * 64, smem, s>>>(q);
   if (parts > 1) mx_join_kernel<TY><<<dim3((p.N + 1023) / 1024, p.M), 256, 0, s>>>(p, parts);
 }
 
@@ -808,8 +829,34 @@ static MxRowsShape pick_rows(bool x4, int M, int N, int kb) {
     }
   return best;
 }
+// Where waves share their rows: from more features on than 256 blocks of 128 give each compute unit one (512 for up to 16 rows, whose share of the traffic is
+// small).  Blocks of 256 features once there would be more than three blocks of 128 a unit, of which two share K where the registers let two blocks lie on a
+// unit (up to 32 rows) and each unit has its two.  us at K 4096, f32 results, for 16 / 32 / 48 / 64 rows (256 features without / with halves of K):
+//   features   alone            128 shared     256 shared     256 in halves
+//     40960    21  47  57  66   26 27 31 34    36 40 43 49    30 33  38  42
+//     65536    28  39  45  52   27 30 35 41    38 42 45 51    33 36  40  45
+//     98304    41  57  66  75   38 45 52 68    45 51 59 72    43 46  75  83
+//    131072    54  79  89 100   50 65 75 81    48 56 66 79    47 53  82  88
+//    262144   113 149 170 196  102 125 135 160  93 117 134 155  99 109 157 171
+enum { MX_ALONE, MX_SHARED_128, MX_SHARED_256, MX_SHARED_256_HALVES };
+static int pick_shared(int M, int N) {
+  const int tiles = (N + 15) / 16, blocks128 = (tiles + 7) / 8, blocks256 = (tiles + 15) / 16;
+  if (blocks128 <= (M <= 16 ? 512 : 256)) return MX_ALONE;
+  if (blocks128 <= 768) return MX_SHARED_128;
+  return M <= 32 && blocks256 <= 512 ? MX_SHARED_256_HALVES : MX_SHARED_256;
+}
 template <int XF, typename TY, int MT>
 static void launch_rows_mt(const MxProduct& p, hipStream_t s) {
+  if constexpr (XF == MX_RING) {
+    switch (pick_shared(p.M, p.N)) {
+      case MX_SHARED_128: launch_rows_t<XF, TY, MT, 4, 2, 2>(p, 1, s); return;
+      case MX_SHARED_256: launch_rows_t<XF, TY, MT, 4, 1, 4>(p, 1, s); return;
+      case MX_SHARED_256_HALVES:
+        if constexpr (MT <= 2) { launch_rows_t<XF, TY, MT, 4, 2, 4>(p, 1, s); return; }
+        break;
+      default: break;
+    }
+  }
   const MxRowsShape w = pick_rows(XF == MX_X4, p.M, p.N, p.kb);
   // (eight waves where a compute unit has one block, and LDS for it)
   const bool eight = MT == 1 && ((p.N + 15) / 16 + w.ntw - 1) / w.ntw * w.parts <= 256;
@@ -828,9 +875,8 @@ static void launch_tiled_t(const MxProduct& p, int parts, hipStream_t s) {
   typedef MxTile<X4, WM, WN, WTM> T;
   constexpr int smem = T::STAGE * T::S;
   static_assert(smem <= 160 * 1024, "the stages fit the LDS");
-  static const hipError_t once = hipFuncSetAttribute((const void*)mx_tiled_kernel<X4, TY, WM, WN, WTM>,
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  (void)once;
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)mx_tiled_kernel<X4, TY, WM, WN, WTM>, smem, done);
   MxProduct q = p;
   if (parts == 1) q.parts = nullptr;
   const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
@@ -843,9 +889,8 @@ static void launch_tiled4_t(const MxProduct& p, int parts, hipStream_t s) {
   typedef MxTile4<WM, WN, MF, NF> T;
   constexpr int smem = T::STAGE * 2;
   static_assert(smem <= 160 * 1024, "the stages fit the LDS");
-  static const hipError_t once = hipFuncSetAttribute((const void*)mx_tiled4_kernel<TY, WM, WN, MF, NF>,
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  (void)once;
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)mx_tiled4_kernel<TY, WM, WN, MF, NF>, smem, done);
   MxProduct q = p;
   if (parts == 1) q.parts = nullptr;
   const int gx = (p.N + T::BN - 1) / T::BN, gy = (p.M + T::BM - 1) / T::BM;
@@ -915,7 +960,7 @@ static void launch_linear_t(const MxProduct& p, hipStream_t s) {
 // known here.)
 static size_t mx_parts_bytes(bool x4, long M, int N, int kb) {
   if (M <= 0) return 0;
-  const int parts = M <= kMxFewRows ? pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts;
+  const int parts = M <= kMxFewRows ? !x4 && pick_shared((int)M, N) != MX_ALONE ? 1 : pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts;
   return parts > 1 ? ((size_t)parts * M * ((N + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256 : 0;
 }
 size_t mx_linear_workspace(bool x4, long M, int N, int kb) {

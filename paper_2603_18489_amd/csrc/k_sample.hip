@@ -942,9 +942,8 @@ static void launch_sample_draw(const T* logits, int rows, int parts, int V, size
                                const SampleArgs& a, const PartSum* sums, const Spread* spreads, int* tokens, float4* stats, hipStream_t s) {
   constexpr int smem = sizeof(RowScratch<LIST>);
   static_assert(smem <= 80 * 1024, "two blocks to a compute unit");
-  static const hipError_t once = hipFuncSetAttribute((const void*)sample_draw_kernel<T, FILTERS, LIST>,
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-  (void)once;
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)sample_draw_kernel<T, FILTERS, LIST>, smem, done);
   sample_draw_kernel<T, FILTERS, LIST><<<rows, kSampleThreads, smem, s>>>(logits, V, ld, parts, part_size, uniforms, a, sums, spreads, tokens,
                                                                           stats);
 }

@@ -147,6 +147,13 @@ def test_linear_at_the_models_sizes(m, n, k, pad, act):
     check_linear(m, n, k, act, "bf16", pad=pad)
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(17, 32900, 96), (33, 40001, 160), (64, 49160, 32), (16, 70001, 128), (48, 70004, 480), (5, 98320, 64),
+                                   (32, 100100, 224), (9, 131073, 32), (50, 98321, 160), (64, 140001, 96)])
+def test_linear_with_few_rows_and_many_features(m, n, k, out):
+    check_linear(m, n, k, "bf16", out)
+
+
 @pytest.mark.parametrize("act", ["bf16", "mxfp4"])
 @pytest.mark.parametrize("m", [1, 20, 130])
 def test_blocks_that_are_none_and_wide_scales(m, act):
