@@ -765,11 +765,23 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxProduct p, int parts) {
 // ---- launchers ------------------------------------------------------------------------------------
 size_t mx_packed_bytes(int n, int kb) { return (size_t)((n + 63) / 64) * mx_tiles_of_k(kb) * kMxGroupBytes; }
 
+// A launch takes fewer than 2^32 threads: rows of more go in several, each of up to 2^31 threads (`per_row` of them a row).
+template <typename F> static void in_slices(long rows, long per_row, F launch) {
+  const long most = (1l << 31) / per_row;   // (8192 and more)
+  for (long r = 0; r < rows; r += most) {
+    const long n = rows - r < most ? rows - r : most;
+    launch(r, n, (unsigned)((n * per_row + 255) / 256));
+  }
+}
 template <typename T>
 static void launch_quantize_t(const T* x, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s) {
-  const unsigned grid = (unsigned)((rows * kb * 4 + 255) / 256);
-  if ((uintptr_t)x % 16 == 0 && (ld * sizeof(T)) % 16 == 0) mx_quantize_kernel<T, true><<<grid, 256, 0, s>>>(x, rows, kb, ld, codes, scales);
-  else mx_quantize_kernel<T, false><<<grid, 256, 0, s>>>(x, rows, kb, ld, codes, scales);
+  const bool wide = (uintptr_t)x % 16 == 0 && (ld * sizeof(T)) % 16 == 0;
+  in_slices(rows, kb * 4, [&](long r, long n, unsigned grid) {
+    const T* from = x + (size_t)r * ld;
+    uint8_t *c = codes + (size_t)r * kb * 16, *e = scales + (size_t)r * kb;
+    if (wide) mx_quantize_kernel<T, true><<<grid, 256, 0, s>>>(from, n, kb, ld, c, e);
+    else mx_quantize_kernel<T, false><<<grid, 256, 0, s>>>(from, n, kb, ld, c, e);
+  });
 }
 void launch_mx_quantize(const void* x, bool bf16, long rows, int kb, size_t ld, uint8_t* codes, uint8_t* scales, hipStream_t s) {
   if (bf16) launch_quantize_t((const bf16_t*)x, rows, kb, ld, codes, scales, s);
@@ -778,9 +790,13 @@ void launch_mx_quantize(const void* x, bool bf16, long rows, int kb, size_t ld, 
 
 template <typename T>
 static void launch_dequantize_t(const uint8_t* codes, const uint8_t* scales, long rows, int kb, T* out, size_t ld, hipStream_t s) {
-  const unsigned grid = (unsigned)((rows * kb * 4 + 255) / 256);
-  if ((uintptr_t)out % 16 == 0 && (ld * sizeof(T)) % 16 == 0) mx_dequantize_kernel<T, true><<<grid, 256, 0, s>>>(codes, scales, rows, kb, out, ld);
-  else mx_dequantize_kernel<T, false><<<grid, 256, 0, s>>>(codes, scales, rows, kb, out, ld);
+  const bool wide = (uintptr_t)out % 16 == 0 && (ld * sizeof(T)) % 16 == 0;
+  in_slices(rows, kb * 4, [&](long r, long n, unsigned grid) {
+    const uint8_t *c = codes + (size_t)r * kb * 16, *e = scales + (size_t)r * kb;
+    T* to = out + (size_t)r * ld;
+    if (wide) mx_dequantize_kernel<T, true><<<grid, 256, 0, s>>>(c, e, n, kb, to, ld);
+    else mx_dequantize_kernel<T, false><<<grid, 256, 0, s>>>(c, e, n, kb, to, ld);
+  });
 }
 void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows, int kb, void* out, bool bf16, size_t ld,
                           hipStream_t s) {
@@ -789,8 +805,11 @@ void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows
 }
 
 void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, uint8_t* packed, hipStream_t s) {
-  const long total = (long)((n + 63) / 64) * mx_tiles_of_k(kb) * 256;
-  mx_pack_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(codes, scales, n, kb, total, packed);
+  const int kq = mx_tiles_of_k(kb);
+  in_slices((n + 63) / 64, kq * 256l, [&](long g, long count, unsigned grid) {   // groups of 64 rows
+    mx_pack_kernel<<<grid, 256, 0, s>>>(codes + (size_t)g * 64 * kb * 16, scales + (size_t)g * 64 * kb, (int)(n - g * 64), kb, count * kq * 256,
+                                        packed + (size_t)g * kq * kMxGroupBytes);
+  });
 }
 
 constexpr int mx_rows_lds(int xf, int mt, int ntw, int ks, int nw = 1) {
@@ -812,24 +831,8 @@ static void launch_rows_t(const MxProduct& p, int parts, hipStream_t s) {
   if (parts > 1) mx_join_kernel<TY><<<dim3((p.N + 1023) / 1024, p.M), 256, 0, s>>>(p, parts);
 }
 
-// Tiles of features to a block and ranges of K.  A compute unit pulls about 50 KB/us in these kernels, so that what counts is what goes
-// through the busiest of the 256: its blocks' shares of W and, once a block, the rows; a join of K's ranges is another 3.5 us.
-struct MxRowsShape { int ntw, parts; };
-static MxRowsShape pick_rows(bool x4, int M, int N, int kb) {
-  const int tiles = (N + 15) / 16, rows = (M + 3) / 4 * 4;
-  MxRowsShape best = {1, 1};
-  double least = 1e30;
-  for (const int ntw : {1, 2, 4, 6, 8})
-    for (const int parts : {1, 2, 4}) {
-      if (parts > 1 && mx_tiles_of_k(kb) < 8 * parts) continue;
-      const int blocks = (tiles + ntw - 1) / ntw * parts;
-      const double kbytes = (ntw * 16 * 17.0 + rows * (x4 ? 17.0 : 64.0)) * kb / parts / 1000;
-      const double us = (blocks + 255) / 256 * kbytes / 50 + (parts > 1 ? 3.5 : 0);
-      if (us < least) { least = us; best = {ntw, parts}; }
-    }
-  return best;
-}
-// Where waves share their rows: from more features on than 256 blocks of 128 give each compute unit one (512 for up to 16 rows, whose share of the traffic is
+constexpr int kMxRegisterRows = 4;   // rows of bf16 that a wave loads into registers, past LDS
+// Where waves share their rows in LDS: from more features on than 256 blocks of 128 give each compute unit one (512 for up to 16 rows, whose share of the traffic is
 // small).  Blocks of 256 features once there would be more than three blocks of 128 a unit, of which two share K where the registers let two blocks lie on a
 // unit (up to 32 rows) and each unit has its two.  us at K 4096, f32 results, for 16 / 32 / 48 / 64 rows (256 features without / with halves of K):
 //   features   alone            128 shared     256 shared     256 in halves
@@ -839,16 +842,36 @@ static MxRowsShape pick_rows(bool x4, int M, int N, int kb) {
 //    131072    54  79  89 100   50 65 75 81    48 56 66 79    47 53  82  88
 //    262144   113 149 170 196  102 125 135 160  93 117 134 155  99 109 157 171
 enum { MX_ALONE, MX_SHARED_128, MX_SHARED_256, MX_SHARED_256_HALVES };
-static int pick_shared(int M, int N) {
+static int pick_shared(bool x4, int M, int N) {
+  if (x4 || M <= kMxRegisterRows) return MX_ALONE;
   const int tiles = (N + 15) / 16, blocks128 = (tiles + 7) / 8, blocks256 = (tiles + 15) / 16;
   if (blocks128 <= (M <= 16 ? 512 : 256)) return MX_ALONE;
   if (blocks128 <= 768) return MX_SHARED_128;
   return M <= 32 && blocks256 <= 512 ? MX_SHARED_256_HALVES : MX_SHARED_256;
 }
+// Tiles of features to a block and ranges of K.  A compute unit pulls about 50 KB/us in these kernels, so that what counts is what goes
+// through the busiest of the 256: its blocks' shares of W and, once a block, the rows; a join of K's ranges is another 3.5 us.
+struct MxRowsShape { int ntw, parts, shared; };
+static MxRowsShape pick_rows(bool x4, int M, int N, int kb) {
+  const int tiles = (N + 15) / 16, rows = (M + 3) / 4 * 4;
+  MxRowsShape best = {4, 1, pick_shared(x4, M, N)};
+  if (best.shared != MX_ALONE) return best;
+  double least = 1e30;
+  for (const int ntw : {1, 2, 4, 6, 8})
+    for (const int parts : {1, 2, 4}) {
+      if (parts > 1 && mx_tiles_of_k(kb) < 8 * parts) continue;
+      const int blocks = (tiles + ntw - 1) / ntw * parts;
+      const double kbytes = (ntw * 16 * 17.0 + rows * (x4 ? 17.0 : 64.0)) * kb / parts / 1000;
+      const double us = (blocks + 255) / 256 * kbytes / 50 + (parts > 1 ? 3.5 : 0);
+      if (us < least) { least = us; best = {ntw, parts, MX_ALONE}; }
+    }
+  return best;
+}
 template <int XF, typename TY, int MT>
 static void launch_rows_mt(const MxProduct& p, hipStream_t s) {
+  const MxRowsShape w = pick_rows(XF == MX_X4, p.M, p.N, p.kb);
   if constexpr (XF == MX_RING) {
-    switch (pick_shared(p.M, p.N)) {
+    switch (w.shared) {
       case MX_SHARED_128: launch_rows_t<XF, TY, MT, 4, 2, 2>(p, 1, s); return;
       case MX_SHARED_256: launch_rows_t<XF, TY, MT, 4, 1, 4>(p, 1, s); return;
       case MX_SHARED_256_HALVES:
@@ -857,7 +880,6 @@ static void launch_rows_mt(const MxProduct& p, hipStream_t s) {
       default: break;
     }
   }
-  const MxRowsShape w = pick_rows(XF == MX_X4, p.M, p.N, p.kb);
   // (eight waves where a compute unit has one block, and LDS for it)
   const bool eight = MT == 1 && ((p.N + 15) / 16 + w.ntw - 1) / w.ntw * w.parts <= 256;
   constexpr int K1 = mx_rows_lds(XF, MT, 1, 8) <= 160 * 1024 ? 8 : 4, E = MT == 1 ? 8 : 4;
@@ -938,7 +960,7 @@ template <bool X4, typename TY>
 static void launch_linear_t(const MxProduct& p, hipStream_t s) {
   constexpr int XF = X4 ? MX_X4 : MX_RING;
   switch ((p.M + 15) / 16) {
-    case 1: if (p.M <= 4) launch_rows_mt<X4 ? MX_X4 : MX_REGS, TY, 1>(p, s); else launch_rows_mt<XF, TY, 1>(p, s); break;
+    case 1: if (p.M <= kMxRegisterRows) launch_rows_mt<X4 ? MX_X4 : MX_REGS, TY, 1>(p, s); else launch_rows_mt<XF, TY, 1>(p, s); break;
     case 2: launch_rows_mt<XF, TY, 2>(p, s); break;
     case 3: launch_rows_mt<XF, TY, 3>(p, s); break;
     case 4: launch_rows_mt<XF, TY, 4>(p, s); break;
@@ -960,7 +982,7 @@ static void launch_linear_t(const MxProduct& p, hipStream_t s) {
 // known here.)
 static size_t mx_parts_bytes(bool x4, long M, int N, int kb) {
   if (M <= 0) return 0;
-  const int parts = M <= kMxFewRows ? !x4 && pick_shared((int)M, N) != MX_ALONE ? 1 : pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts;
+  const int parts = M <= kMxFewRows ? pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts;
   return parts > 1 ? ((size_t)parts * M * ((N + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256 : 0;
 }
 size_t mx_linear_workspace(bool x4, long M, int N, int kb) {

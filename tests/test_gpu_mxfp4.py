@@ -155,6 +155,23 @@ def test_linear_with_few_rows_and_many_features(m, n, k, out):
 
 
 @pytest.mark.parametrize("act", ["bf16", "mxfp4"])
+@pytest.mark.parametrize("m,n,k", [(1, 99001, 4096), (4, 33000, 8192), (5, 33000, 8192)])
+def test_few_rows_many_features_and_ranges_of_k(m, n, k, act):
+    """K is split over blocks where rows lie in registers, and not where waves share them.  The matrix is codes and scales at random."""
+    rng = torch.Generator(device="cuda").manual_seed(n)
+    codes = torch.randint(0, 256, (n, k // 2), dtype=torch.uint8, device="cuda", generator=rng)
+    scales = torch.randint(120, 131, (n, k // 32), dtype=torch.uint8, device="cuda", generator=rng)
+    w = ec.Mxfp4(codes, scales)
+    x = torch.randn((m, k), device="cuda", generator=rng).bfloat16()
+    arg = ec.mxfp4_quantize(x) if act == "mxfp4" else x
+    xv = (ec.mxfp4_dequantize(arg) if act == "mxfp4" else x).double()
+    y = ec.mxfp4_linear(arg, ec.mxfp4_pack(w), torch.float32)
+    wv = ec.mxfp4_dequantize(w).double()
+    off = (y.double() - (wv @ xv.t()).t()).abs()
+    assert (off <= (k / 32 + 144) * 2.0 ** -23 * (wv.abs() @ xv.abs().t()).t()).all()
+
+
+@pytest.mark.parametrize("act", ["bf16", "mxfp4"])
 @pytest.mark.parametrize("m", [1, 20, 130])
 def test_blocks_that_are_none_and_wide_scales(m, act):
     """A NaN block reaches the products of its row and no others; scales from 2^-60 to 2^60 in one row; a zero matrix."""
@@ -255,3 +272,47 @@ def test_head_in_four_bits_and_tokens_drawn_from_its_logits():
     assert (entropy[:, 0].long() == logits.argmax(dim=1)).all()
     greedy, _ = ec.row_sample(logits, u, temperature=0.0)
     assert (greedy == entropy[:, 0].int()).all()
+
+
+def test_more_than_two_to_the_32_threads():
+    """2^32 groups of eight values and some: a launch of its own for what one does not take."""
+    rows, k = 2 ** 18 + 3, 131072
+    if torch.cuda.mem_get_info()[0] < 180 << 30:
+        pytest.skip("180 GiB are needed")
+    x = torch.zeros((rows, k), dtype=torch.bfloat16, device="cuda")
+    some = [0, 2 ** 17 - 1, 2 ** 17, 2 ** 18 - 1, 2 ** 18, rows - 1]
+    x[some] = torch.randn((len(some), k), device="cuda").bfloat16()
+    q = ec.mxfp4_quantize(x)
+    ref = ec.mxfp4_quantize(x[some])
+    assert torch.equal(q.codes[some], ref.codes) and torch.equal(q.scales[some], ref.scales)
+    assert all(not q.scales[i:i + 4096].any() for i in (1, 2 ** 17 + 1, 2 ** 18 - 4097))
+    x.fill_(1)
+    values = ec.load_library().ec_mx_dequantize(q.codes.data_ptr(), q.scales.data_ptr(), rows, k, x.data_ptr(), ec.EC_T_BF16, k,
+                                                torch.cuda.current_stream().cuda_stream)
+    assert values == ec.EC_OK
+    assert torch.equal(x[some], ec.mxfp4_dequantize(ref, torch.bfloat16))
+    assert all(not x[i:i + 4096].any() for i in (1, 2 ** 17 + 1, 2 ** 18 - 4097))
+    del x
+    packed, few = ec.mxfp4_pack(q), ec.mxfp4_pack(ref)
+    y = torch.randn((2, k), device="cuda").bfloat16()
+    # Another number of features may split K into other ranges, so that float32 sums meet in another order: each of the two results is
+    # within (k / 32 + 144) 2^-23 of the products' magnitudes, as everywhere here, and they of each other within twice that.
+    size = y.double().abs() @ ec.mxfp4_dequantize(ref).double().abs().t()
+    off = (ec.mxfp4_linear(y, packed, torch.float32)[:, some].double() - ec.mxfp4_linear(y, few, torch.float32).double()).abs()
+    assert (off <= 2 * (k / 32 + 144) * 2.0 ** -23 * size).all()
+    del q, packed
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m", [3, 40, 130])
+def test_scales_at_any_byte_and_a_matrix_that_is_not_packed(m):
+    n, k = 200, 256
+    packed = ec.mxfp4_pack(ec.mxfp4_quantize(on_gpu(matrix(n, k))))
+    q = ec.mxfp4_quantize(on_gpu(matrix(m, k, 3), "bf16"))
+    ref = ec.mxfp4_linear(q, packed)
+    for off in (1, 2, 3):
+        scales = torch.zeros(q.scales.numel() + off, dtype=torch.uint8, device="cuda")[off:].view_as(q.scales)
+        scales.copy_(q.scales)
+        assert torch.equal(ec.mxfp4_linear(ec.Mxfp4(q.codes, scales), packed), ref)
+    with pytest.raises(ValueError):
+        ec.mxfp4_linear(q, ec.Mxfp4Matrix(packed.data[:-1], n, k))
