@@ -316,6 +316,9 @@ def row_entropy_noalloc(logits, stats, stream=None):
         raise EcError(rc, lib.ec_last_error(None).decode())
 
 
+_INT_MAX = 2 ** 31 - 1
+
+
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise ValueError(what)
@@ -373,6 +376,7 @@ def _rows_of(x):
     _need(x.stride(1) == 1 or cols <= 1, "the columns of a row must be next to each other")
     ld = x.stride(0) if rows > 1 else cols
     _need(ld >= cols, "rows must not overlap")
+    _need(max(rows, cols) <= _INT_MAX, "at most 2^31 - 1 rows and columns")   # (what the calls' arguments hold)
     return rows, cols, ld
 
 
@@ -387,7 +391,7 @@ def row_sample(logits, uniforms, temperature: float = 1.0, top_k: int = 0, top_p
     _need(uniforms.dtype == torch.float32 and uniforms.shape == (rows,) and (rows <= 1 or uniforms.stride(0) == 1),
           "uniforms must be float32 [rows]")
     lib = _lib or load_library()
-    cfg = ec_sample_cfg(temperature, top_k, top_p, min_p)
+    cfg = ec_sample_cfg(temperature, max(-1, min(top_k, _INT_MAX)), top_p, min_p)
 
     def call(raw):
         tokens = torch.empty((rows,), dtype=torch.int32, device=logits.device)
@@ -421,6 +425,7 @@ def _mx_of(q):
     _need(codes.dim() == 2 and scales.dim() == 2 and codes.shape[0] == scales.shape[0] and
           codes.shape[1] == 16 * scales.shape[1], "codes [rows, k/2] and scales [rows, k/32] are needed")
     _need(codes.is_contiguous() and scales.is_contiguous(), "codes and scales must be contiguous")
+    _need(max(codes.shape[0], 2 * codes.shape[1]) <= _INT_MAX, "at most 2^31 - 1 rows and columns")
     return codes, scales, codes.shape[0], 2 * codes.shape[1]
 
 
@@ -486,6 +491,7 @@ def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
     lib = _lib or load_library()
 
     def call(raw):
+        _need(w.data.dtype == torch.uint8 and w.data.numel() >= lib.ec_mx_packed_bytes(w.n, k), "data is not a matrix [n, k] of mxfp4_pack")
         y = torch.empty((rows, w.n), dtype=dtype, device=w.data.device)
         size = lib.ec_mx_linear_workspace_bytes(x_kind, rows, w.n, k)
         ws, at = _workspace(torch, size, w.data.device)

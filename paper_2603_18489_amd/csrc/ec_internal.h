@@ -287,7 +287,7 @@ struct SampleArgs {
   double scale, per_z;  // log2(e) / temperature; 16 / temperature
   int top_k;            // 0: all
   double top_p;
-  unsigned long long min_weight;   // least weight kept (the maximum's is 2^46)
+  double min_z;         // temperature * ln(min_p): the least logit kept, less the maximum; -inf: all
 };
 // logits [rows, V] with row stride ld, float32 or bfloat16 -> a token id (-1: none) and (probability among the kept, among all,
 // number kept, share of the kept) a row

@@ -74,7 +74,7 @@ int ec_row_sample(const void* logits, int32_t type, int32_t rows, int32_t vocab,
   a.per_z = 16.0 / (greedy ? 1.0 : (double)cfg->temperature);
   a.top_k = greedy ? 1 : cfg->top_k < vocab ? cfg->top_k : 0;
   a.top_p = cfg->top_p;
-  a.min_weight = cfg->min_p > 0.f ? (unsigned long long)std::ceil(std::fmax((double)cfg->min_p, 0x1p-45) * 0x1p46) : 0;
+  a.min_z = cfg->min_p > 0.f ? std::log((double)cfg->min_p) * (greedy ? 1.0 : (double)cfg->temperature) : -INFINITY;
   launch_sample_rows(logits, type == EC_T_BF16, rows, vocab, ld, uniforms, a, tokens, (float4*)stats, workspace,
                      (hipStream_t)hip_stream);
   return op_done("sampling kernels");

@@ -348,14 +348,14 @@ __device__ __forceinline__ u64 draw_at(float u, u64 total) {
 // The place of the token: the first whose running sum of kept weights is `want` or more.  kept, count: of these tokens; `at` is called by
 // every thread with them and says what is wanted.  Returns true to one lane.
 template <typename S, typename W>
-__device__ __forceinline__ bool draw_place(const S& src, const SampleRow& row, const Cut& cut, int shift, u64 min_weight, Scratch& x,
+__device__ __forceinline__ bool draw_place(const S& src, const SampleRow& row, const Cut& cut, int shift, double least, Scratch& x,
                                            u64& kept, uint32_t& count, W wanted, int& place, float& logit) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   u64 part = 0;
   uint32_t n = 0;
   auto weight = [&](int at, float v) {
     const u64 w = row.weight(v);
-    const bool keep = v > -INFINITY && w >= min_weight && cut.keeps(key_of(v), at + shift);
+    const bool keep = v > -INFINITY && v >= least && cut.keeps(key_of(v), at + shift);
     n += keep;
     return keep ? w : 0;
   };
@@ -428,7 +428,7 @@ __device__ void sample_whole(const S& src, const SampleRow& row, const SampleArg
   uint32_t n;
   int place;
   float z;
-  if (draw_place(src, row, cut, 0, a.min_weight, x, kept, n, [&](u64 k) { return draw_at(u, k); }, place, z))
+  if (draw_place(src, row, cut, 0, row.m + a.min_z, x, kept, n, [&](u64 k) { return draw_at(u, k); }, place, z))
     put_token(tokens, stats, r, place, z, row, kept, n, all);
 }
 
@@ -776,18 +776,17 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       __syncthreads();
       // Top-k that ends among tokens of no weight takes nothing from the others: all that it says is how many are kept, if nothing else does.
       const int bin_k = y.bin_k;
-      fixed = by_k && bin_k == kBins - 1 && !by_p && a.min_weight == 0 ? a.top_k : 0;
+      fixed = by_k && bin_k == kBins - 1 && !by_p && a.min_z == -INFINITY ? a.top_k : 0;
       by_k = by_k && bin_k < kBins - 1;
       const u64 want = by_p ? mass_wanted(a.top_p, all) : 0;
       if (by_p && !by_k && mb < want && want <= mb + s) y.bin_p = tid;
       __syncthreads();
-      // kBins: no cut.  (The bin of min_p's border is known up to the rounding of its logarithm.  Where top-p goes by the sum of the top-k,
+      // kBins: no cut.  (The bin of min_p's border is known up to roundings.  Where top-p goes by the sum of the top-k,
       // these have to be there.)
       const int k_at = by_k ? bin_k : kBins, p_at = y.bin_p;
       lo = hi = min(k_at, p_at);
-      if (a.min_weight > 0 && !(by_k && by_p)) {
-        const double border = log2((double)a.min_weight * 0x1p-46) / a.scale;   // (z of the border less the maximum: <= 0)
-        const int bm = (int)fmax(fmin((double)top - floor(((double)m + border) * a.per_z), (double)kBins), 0.0);
+      if (a.min_z > -INFINITY && !(by_k && by_p)) {
+        const int bm = (int)fmax(fmin((double)top - floor((row.m + a.min_z) * a.per_z), (double)kBins), 0.0);
         lo = min(lo, max(bm - 1, 0));
         hi = min(hi, bm + 1);
       }
@@ -863,7 +862,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       u64 kept;
       int place;
       float v;
-      if (draw_place(src, row, cut, 0, a.min_weight, x, kept, count, [&](u64 k) { return draw_at(u, k); }, place, v))
+      if (draw_place(src, row, cut, 0, row.m + a.min_z, x, kept, count, [&](u64 k) { return draw_at(u, k); }, place, v))
         put_token(tokens, stats, r, y.list[place].y, v, row, kept, count, all);
       return;
     }
@@ -871,7 +870,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
     u64 n = 0;
     src.each([&](int at, float v, bool) {
       const u64 w = row.weight(v);
-      if (v > -INFINITY && w >= a.min_weight && cut.keeps(key_of(v), at)) {
+      if (v > -INFINITY && v >= row.m + a.min_z && cut.keeps(key_of(v), at)) {
         ++n;
         atomicAdd(&y.part_kept[y.list[at].y / part_size], w);
       }
@@ -905,7 +904,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
     uint32_t n;
     int place;
     float v;
-    const bool found = draw_place(src, row, cut, first, a.min_weight, x, here, n,
+    const bool found = draw_place(src, row, cut, first, row.m + a.min_z, x, here, n,
                                   [&](u64 k) { return tried ? min((u64)1, k) : min(want - base, k); }, place, v);
     if (found) put_token(tokens, stats, r, first + place, v, row, kept, count, all);
     if (here > 0) break;   // (the same for all threads)
@@ -953,7 +952,7 @@ static void launch_sample_ne(const T* logits, int rows, int parts, int V, size_t
   PartSum* sums = (PartSum*)ws;
   Spread* spreads = (Spread*)(ws + b.sums);
   const dim3 grid(parts, rows);
-  if (a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0) {
+  if (a.top_k > 0 || a.top_p < 1.0 || a.min_z > -INFINITY) {
     sample_parts_kernel<T, NE, true><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
     launch_sample_draw<T, true, kList>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
   } else {
@@ -974,7 +973,7 @@ static void launch_sample_t(const T* logits, int rows, int V, size_t ld, const f
   const SampleBytes b = sample_bytes(rows, V);
   for (int r = 0; r < rows; r += kSampleBatch) {
     const int n = rows - r < kSampleBatch ? rows - r : kSampleBatch;
-    const SampleSizes w = sample_sizes(n, V, a.top_k > 0 || a.top_p < 1.0 || a.min_weight > 0);
+    const SampleSizes w = sample_sizes(n, V, a.top_k > 0 || a.top_p < 1.0 || a.min_z > -INFINITY);
     const T* z = logits + (size_t)r * ld;
     if (w.ne == 8) launch_sample_ne<T, 8>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s);
     else launch_sample_ne<T, 16>(z, n, w.parts, V, ld, uniforms + r, a, tokens + r, stats + r, (char*)workspace, b, s);

@@ -216,3 +216,40 @@ def test_columns_and_rows_beyond_are_left_alone():
                            stats.data_ptr(), ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
     assert rc == ec.EC_OK
     assert (tokens[rows:] == 77).all() and (stats[rows:] == 77).all() and (tokens[:rows] >= 0).all()
+
+
+@pytest.mark.parametrize("filters", [dict(temperature=0.8), dict(top_k=50, top_p=0.9), dict(min_p=0.05)], ids=str)
+def test_more_rows_than_are_drawn_at_a_time(filters):
+    """Rows past 1024 in long rows: each the same as by itself among few."""
+    V, rows = 17001, 2100
+    z = torch.randn((rows, V), device="cuda") * 3
+    u = torch.rand(rows, device="cuda")
+    tokens, stats = ec.row_sample(z, u, **filters)
+    for lo in (0, 1000, 1023, 1024, 2040, 2090):
+        few, of_few = ec.row_sample(z[lo:lo + 10], u[lo:lo + 10].contiguous(), **filters)
+        assert torch.equal(tokens[lo:lo + 10], few)
+        torch.testing.assert_close(stats[lo:lo + 10], of_few, rtol=2.0 ** -22, atol=0)
+    check(z[1020:1030], u[1020:1030].cpu().numpy(), **filters)
+
+
+def test_a_top_k_beyond_32_bits_is_all():
+    z, u = logits(4, 5000)
+    u = torch.from_numpy(u).cuda()
+    for a, b in zip(ec.row_sample(z, u, top_k=2 ** 32 + 5), ec.row_sample(z, u)):
+        assert torch.equal(a, b)
+    with pytest.raises(ec.EcError):
+        ec.row_sample(z, u, top_k=-2 ** 32 + 5)
+
+
+@pytest.mark.parametrize("V", [16384, 16385, 20481])
+@pytest.mark.parametrize("filters", [dict(), dict(top_k=4, top_p=0.99), dict(top_p=0.7), dict(min_p=2.0 ** -50), dict(top_k=16383)], ids=str)
+def test_around_the_longest_row_of_one_block(V, filters):
+    z, u = logits(3, V)
+    check(z, u, **filters)
+
+
+def test_more_kept_of_the_top_k_than_are_listed():
+    """Flat rows in which top-k, and top-p among these, end far down."""
+    z = torch.randn((3, 60000), device="cuda") * 0.01
+    check(z, [0.1, 0.5, 0.999], top_k=40000, top_p=0.9)
+    check(z.bfloat16(), [0.1, 0.5, 0.999], top_k=40000, top_p=0.9, min_p=0.97)

@@ -126,3 +126,13 @@ def test_the_binding_refuses_what_is_not_on_a_gpu_or_has_another_form():
                  lambda: ec.mxfp4_linear(x.float(), w), lambda: ec.mxfp4_linear(x[:, :32], w), lambda: ec.mxfp4_linear(x, w, torch.float16)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_the_binding_refuses_numbers_that_its_arguments_do_not_hold():
+    many, wide = torch.empty((2 ** 32 + 3, 32), device="meta"), torch.empty((3, 2 ** 32 + 32), device="meta")
+    for call in (lambda: ec.mxfp4_quantize(many), lambda: ec.mxfp4_quantize(wide),
+                 lambda: ec.row_sample(many, torch.empty(2 ** 32 + 3, device="meta")),
+                 lambda: ec.mxfp4_dequantize(ec.Mxfp4(torch.empty((2 ** 32 + 3, 16), dtype=torch.uint8, device="meta"),
+                                                      torch.empty((2 ** 32 + 3, 1), dtype=torch.uint8, device="meta")))):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
