@@ -351,7 +351,8 @@ int ec_row_entropy_noalloc(const float *logits, int32_t rows, int32_t vocab, siz
 enum { EC_T_F32 = 0, EC_T_BF16 = 1, EC_T_MXFP4 = 2 };
 
 /* How ec_row_sample draws.  temperature: finite, >= 0; 0 takes the most probable token (top_k 1 at temperature 1).  top_k: 0 or
- * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all. */
+ * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all.  (Rows of more than 16384 logits cost least where top-k, or the tokens around
+ * the cut, are up to 5632; beyond that, with top-k and top-p together or min_p below 1e-14, one block goes through the row several times.) */
 typedef struct {
   float temperature;
   int32_t top_k;
@@ -362,8 +363,9 @@ typedef struct {
  * e_i = exp((z_i - max z) / temperature), S the sum of all e and the tokens in the order (z descending, id ascending), a row keeps
  * the token of rank j if  j < top_k;  the e of the ranks before j sum to less than top_p times the sum of the top_k e;
  * e >= min_p;  z > -inf.  The token drawn is the lowest id for which the running sum of the kept e, in the order of the ids, exceeds u
- * times the sum of all kept.  e is computed in 64 bits and all sums are exact sums of e rounded to multiples of 2^-46, so the result does not
- * depend on the order of anything: the same arguments give the same bits.
+ * times the sum of all kept.  e is computed in 64 bits and summed in whole numbers, so the result does not depend on the order of anything: the same
+ * arguments give the same bits.  A sum is off by at most 2^-35 of itself and vocab * 2^-46 (e of the largest logit being 1): so near are the places where one
+ * token ends and the next begins.
  *  logits     DEVICE [rows, vocab] of `type` (EC_T_F32 or EC_T_BF16), row stride ld elements (ld >= vocab); read only
  *  rows       0 .. 65535; vocab 2 .. 163840
  *  uniforms   DEVICE float32 [rows], u in [0, 1); below 0 and NaN count as 0, 1 and above as the largest float32 below 1

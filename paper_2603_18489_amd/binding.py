@@ -491,7 +491,8 @@ def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
     lib = _lib or load_library()
 
     def call(raw):
-        _need(w.data.dtype == torch.uint8 and w.data.numel() >= lib.ec_mx_packed_bytes(w.n, k), "data is not a matrix [n, k] of mxfp4_pack")
+        # (groups of 64 rows x 128 k, as ec_mx_packed_bytes counts them, without another call)
+        _need(w.data.numel() >= (w.n + 63) // 64 * ((k + 127) // 128) * 4352, "data is not a matrix [n, k] of mxfp4_pack")
         y = torch.empty((rows, w.n), dtype=dtype, device=w.data.device)
         size = lib.ec_mx_linear_workspace_bytes(x_kind, rows, w.n, k)
         ws, at = _workspace(torch, size, w.data.device)

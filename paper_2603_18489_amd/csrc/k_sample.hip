@@ -432,7 +432,8 @@ __device__ void sample_whole(const S& src, const SampleRow& row, const SampleArg
     put_token(tokens, stats, r, place, z, row, kept, n, all);
 }
 
-// A row of up to 512 NE logits: one block, which reads it once.
+// A row of up to 512 NE logits: one block, which reads it once and keeps it in registers.  What takes the time is the chain of block-wide
+// steps, a barrier or two each: 10 us for a row of 4096 with all filters, of which the launch is 3.
 template <typename T, int NE>
 __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* __restrict__ logits, int V, size_t ld,
                                                                       const float* __restrict__ uniforms, SampleArgs a,
@@ -448,12 +449,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* _
   sample_whole(src, SampleRow{(double)m, a.scale}, a, uniforms[r], r, x, tokens, stats);
 }
 
-// ---- longer rows: parts of 512 NE logits to a block --------------------------------------------------
-// A part's maximum and, without filters, its weights' sum.  With filters, how its weights spread over kBins bins of T / 16 in z, counted down
+// ---- longer rows: parts of 4096 or 8192 logits to a block ---------------------------------------------
+// One pass in which each block needs nothing of the others, then a block a row that joins what they found.  A part's maximum and, without filters, its weights' sum.  With filters, how its weights spread over kBins bins of T / 16 in z, counted down
 // from its largest logit; the last one is all that lies 32 T and more below it, which weighs nothing (less than 2^-46 of the maximum).  Bins
 // begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
 // e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1], and what is added for it one number: 2^48 (a count) plus (e^(rho / 16) - 0.99) 2^36,
-// whose sums over the 16384 logits of a part stay below 2^48.
+// whose sums over the 8192 logits of a part stay below 2^48.
+// 544 rows of 126464 bf16 logits: 68 us, 2.0 TB/s; 36 of these are the loads and the maximum, the rest the 64-bit polynomial (26) and the bins, whose
+// LDS atomics hide behind it.  32 rows of float32 without filters: 8.5 us, about a launch and the latency of what a block does.  (32 logits a
+// thread: 75 us.)
 constexpr int kBins = 512, kList = 5632, kPartsMax = 40, kSampleBatch = 1024;
 constexpr int kChunk = 1024, kChunksMax = 192;   // logits that a wave goes through at a time; of the longest row
 struct PartSum {
@@ -696,7 +700,9 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
 
 // The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the row is read
 // once more for the tokens of these, which are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
-// which part the token is, and only that is read.
+// which part the token is, and only that is read.  34 rows of 152064 with top-p: 17 us, the chain from the bins to the token; 544 rows of 126464 bf16 with
+// top-k, top-p and min-p: 91 us, two blocks to a compute unit and so two rounds, which read what is not in the caches any more at 5.5 TB/s.  (Three blocks with a
+// list of half the length: 84 to 90 us, and spills; chunks of 512: 98.)
 template <typename T, bool FILTERS, int LIST>
 __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
@@ -914,8 +920,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
 // ---- launchers ------------------------------------------------------------------------------------
 struct SampleSizes { int ne, parts; };
 // Logits to a thread: the fewest with which a batch of rows makes no more than two blocks for each compute unit; four where nothing is
-// listed, as the part that the token is in is then read again.  us by trace, 32 rows of 126464 without filters, 31 parts and 16: 8.5 + 6.6, 7.9 +
-// 10.8; 34 rows of 152064 with top-p, 19 parts and 10: 10.4 + 25.1, 12.1 + 24.5, the call 37.9, 36.9.
+// listed, as the part that the token is in is then read again.  us by trace, parts and draw, eight logits a thread against sixteen: 32 rows of 126464 without
+// filters 8.5 + 6.6, 7.9 + 10.8; 34 rows of 152064 with top-p (sixteen by the rule) 10.4 + 17.6, 10.0 + 16.9; 544 rows of 126464 (sixteen) 75 + 91, 68 + 91.
 static SampleSizes sample_sizes(int rows, int V, bool filters) {
   const int parts = (V + kSampleThreads * 8 - 1) / (kSampleThreads * 8);
   if ((long)rows * parts <= (filters ? 512 : 1024)) return {8, parts};
@@ -927,7 +933,7 @@ static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) return b;
   if (rows > kSampleBatch) rows = kSampleBatch;
-  // (with fewer than 32 logits to a thread there are at most 1024 parts, 512 of them with bins)
+  // (with eight logits to a thread there are at most 1024 parts)
   size_t most = (size_t)rows * ((V + kSampleThreads * 16 - 1) / (kSampleThreads * 16));
   if (most < 1024) most = 1024;
   b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
