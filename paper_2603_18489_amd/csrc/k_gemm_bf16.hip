@@ -637,7 +637,8 @@ static void launch_skinny_mt_w4(const bf16_t* Ap, int MT_src, const void* Wq, in
   constexpr int K8 = MT > 2 ? 4 : 8;   // (eight waves have half the registers)
   if constexpr (EPI == EPI_LOGITS) {
     switch (lm_tiles(total_nt)) {
-      case 8: launch_skinny_t<EPI, MT, 8, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
+      // (two waves a block: more blocks on a compute unit, sums of two.  126464 x 4096, us for 16 / 32 / 64 rows: 46 60 87; four waves 46 68 98, one 49 56 127)
+      case 8: launch_skinny_t<EPI, MT, 8, 2, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
       case 4: launch_skinny_t<EPI, MT, 4, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
       default: launch_skinny_t<EPI, MT, 2, 4, 1, WF_E2M1>(Ap, MT_src, Wq, total_nt, KB, e, s); break;
     }
