@@ -53,6 +53,19 @@ __device__ __forceinline__ u64 wave_before_u64(u64 v) {
   return s - v;
 }
 
+__device__ __forceinline__ uint32_t wave_upto_u32(uint32_t s) {   // (this lane's too)
+  s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x111, 0xf, 0xf, false);
+  s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x112, 0xf, 0xf, false);
+  s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x114, 0xf, 0xf, false);
+  s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x118, 0xf, 0xf, false);
+  s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x142, 0xa, 0xf, false);
+  s += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)s, 0x143, 0xc, 0xf, false);
+  return s;
+}
+__device__ __forceinline__ int lanes_before(u64 mask) {   // of those in the mask
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
 struct SampleRow {
   double m, scale;   // maximum; log2(e) / T
   __device__ __forceinline__ u64 weight(float z) const { return exp2_fixed46(((double)z - m) * scale); }
@@ -455,9 +468,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* _
 // begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
 // e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1], and what is added for it one number: 2^48 (a count) plus (e^(rho / 16) - 0.99) 2^36,
 // whose sums over the 8192 logits of a part stay below 2^48.
-// 544 rows of 126464 bf16 logits: 68 us, 2.0 TB/s; 36 of these are the loads and the maximum, the rest the 64-bit polynomial (26) and the bins, whose
-// LDS atomics hide behind it.  32 rows of float32 without filters: 8.5 us, about a launch and the latency of what a block does.  (32 logits a
-// thread: 75 us.)
+// 544 rows of 126464 bf16 logits: 91 us, 1.5 TB/s; 36 of these are the loads and the maximum, the rest instructions: the 64-bit polynomial (26), bins, whose
+// LDS atomics hide behind it, and the list below (23, for which the draw takes 50 us instead of 91; found by every wave for itself and with the logits in it: 28).  32 rows of float32 without filters: 8.5 us, about a launch and the latency of what a block does.  (32 logits a
+// thread, without the list: 75 us, 16: 68.)
 constexpr int kBins = 512, kList = 5632, kPartsMax = 40, kSampleBatch = 1024;
 constexpr int kChunk = 1024, kChunksMax = 192;   // logits that a wave goes through at a time; of the longest row
 struct PartSum {
@@ -465,12 +478,31 @@ struct PartSum {
   int count;   // -1: a NaN.  With filters: the logits of the last bin, -2 where logits are too large for the bins (2^16 T).  Without: all above -inf
   u64 sum;     // (without filters)
   float of_wave[kSampleWaves];   // the largest of each 64 NE logits in a row, NaN aside
+  int listed, depth;             // with filters: how many tokens are listed, all of the first `depth` bins
 };
 typedef u64 Spread[kBins];
+// With filters a part lists the tokens of its first bins, as many whole bins as have up to one in 32 of its logits, in the order of the ids: a cut that lies
+// there in all parts needs the row's logits no more.
+constexpr int kOfListed = 32, kListedMost = kSampleThreads * 16 / kOfListed;
 
 // number of the bin of a logit, counted up in z; whole, and monotonous whatever z
 __device__ __forceinline__ float bin_of(float z, float per_z) { return floorf(fminf(fmaxf(z * per_z, -1e30f), 1e30f)); }
 __device__ __forceinline__ int bins_below(float top, float b) { return (int)fminf(top - b, (float)(kBins - 1)); }
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key); }
+// The least key of the logits whose bin is at most b below the bin `top` (bins go with the logits' order): a few keys around where it should be,
+// one a lane, or bisected.  c: 16 / T.
+__device__ __forceinline__ uint32_t first_key(float top, float c, int b) {
+  auto in = [&](uint32_t k) { return bins_below(top, bin_of(logit_of(k), c)) <= b; };
+  const uint32_t guess = min(max(key_of((top - (float)b) / c), 0x00800020u), 0xff7fffdfu) - 32;
+  const u64 yes = __builtin_amdgcn_ballot_w64(in(guess + (threadIdx.x & 63)));
+  if (yes && !(yes & 1)) return guess + (uint32_t)__builtin_ctzll(yes);
+  uint32_t i = 0x00800000u, j = 0xff7fffffu;   // (keys of the lowest and the highest finite value)
+  while (i < j) {
+    const uint32_t mid = i + (j - i) / 2;
+    if (in(mid)) j = mid; else i = mid + 1;
+  }
+  return i;
+}
 __device__ __forceinline__ u64 spread_of(float z, float b, double per_z) {
   const double rho = fma((double)z, per_z, -(double)b);
   // e^(rho / 16) - 0.99, degree 5 through the Chebyshev nodes of [-1/16, 17/16] (rounding z 16 / T may move a border that far): off by 9e-14
@@ -493,8 +525,11 @@ __device__ __forceinline__ u64 bin_mass(u64 cnt, u64 frac, double unit) {
 template <typename T, int NE, bool FILTERS>
 __global__ __launch_bounds__(kSampleThreads) void sample_parts_kernel(const T* __restrict__ logits, int V, size_t ld, double scale,
                                                                       double per_z, PartSum* __restrict__ sums,
-                                                                      Spread* __restrict__ spreads) {
+                                                                      Spread* __restrict__ spreads, int2* __restrict__ candidates) {
   __shared__ u64 spread[kBins], wsum[kSampleWaves];
+  __shared__ uint16_t few[kSampleThreads * NE];   // (as far as it is used)
+  __shared__ float list_from;
+  __shared__ int list_depth;
   __shared__ float wmax[kSampleWaves];
   __shared__ int wnan[kSampleWaves], wcnt[kSampleWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -512,7 +547,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_parts_kernel(const T* _
   m = wave_max_dpp(wmax[lane & (kSampleWaves - 1)]);
   nan = __builtin_amdgcn_ballot_w64(wnan[lane & (kSampleWaves - 1)]) != 0;
   u64 sum = 0;
-  int count = 0;
+  int count = 0, listed = 0, depth = 0;
   if (nan || !(fabsf(m) < INFINITY)) {
     count = nan ? -1 : 0;
   } else if constexpr (FILTERS) {
@@ -531,6 +566,48 @@ __global__ __launch_bounds__(kSampleThreads) void sample_parts_kernel(const T* _
     for (int w = 0; w < kSampleWaves; ++w) count += wcnt[w];
     if (fabsf(top) > 0x1p20f) count = -2;
     if (threadIdx.x < kBins) spreads[out][threadIdx.x] = spread[threadIdx.x];
+    // how many bins are listed, and from which logit on: found by one wave for all
+    constexpr uint32_t MOST = kSampleThreads * NE / kOfListed;
+    if (wave == kSampleWaves - 1) {
+      uint32_t before = 0;
+      for (int b = 0; b < kBins; b += 64) {
+        const uint32_t upto = before + wave_upto_u32((uint32_t)(spread[b + lane] >> 48));
+        const u64 fits = __builtin_amdgcn_ballot_w64(upto <= MOST);
+        depth += __builtin_popcountll(fits);
+        if (~fits) break;
+        before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+      }
+      const float from = depth ? logit_of(first_key(top, c, min(depth, kBins - 1) - 1)) : INFINITY;
+      if (lane == 0) { list_from = from; list_depth = depth; }
+    }
+    __syncthreads();
+    // each wave's tokens to where those of the waves before it end
+    const float from = list_from;
+    depth = list_depth;
+    u64 has[NE];
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < NE; ++e) {
+      has[e] = __builtin_amdgcn_ballot_w64(src.v[e] >= from);
+      mine += __builtin_popcountll(has[e]);
+    }
+    if (lane == 0) wcnt[wave] = mine;
+    __syncthreads();
+    int to = 0;
+#pragma unroll
+    for (int w = 0; w < kSampleWaves; ++w) { to += w < wave ? wcnt[w] : 0; listed += wcnt[w]; }
+    listed = min(listed, (int)MOST);
+#pragma unroll
+    for (int e = 0; e < NE; ++e)
+      if (has[e]) {
+        if (src.v[e] >= from) few[to + lanes_before(has[e])] = (uint16_t)(src.first + e * 64);
+        to += __builtin_popcountll(has[e]);
+      }
+    __syncthreads();
+    if ((int)threadIdx.x < listed) {
+      const int place = few[threadIdx.x];
+      candidates[(size_t)out * MOST + threadIdx.x] = make_int2(__float_as_int(load_f32(logits + (size_t)r * ld + lo + place)), lo + place);
+    }
   } else {
     const SampleRow row = {(double)m, scale};
     src.each([&](int, float v, bool) { sum += row.weight(v); count += v > -INFINITY; });
@@ -544,7 +621,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_parts_kernel(const T* _
     for (int w = 0; w < kSampleWaves; ++w) { sum += wsum[w]; count += wcnt[w]; }
   }
   if (lane == 0) sums[out].of_wave[wave] = wmax[wave];
-  if (threadIdx.x == 0) { sums[out].m = m; sums[out].count = count; sums[out].sum = sum; }
+  if (threadIdx.x == 0) { sums[out].m = m; sums[out].count = count; sums[out].sum = sum; sums[out].listed = listed; sums[out].depth = depth; }
 }
 
 // Maximum of a row from its parts (a lane each); 0 as it should be, -1: none, or a NaN, -2: too large for bins.
@@ -587,24 +664,10 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (V + kChunk - 1) / kChunk;
   constexpr int CW = kChunksMax / 64;   // waves with a chunk a lane
   static_assert(kChunksMax % 64 == 0 && CW <= kSampleWaves, "a lane a chunk");
-  // The lowest logit of bin hi, the highest of bin `from`: bins go with the logits' order, so bisect it.
-  auto logit_of = [](uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); };
+  // the lowest logit of bin hi, the highest of bin `from`
   uint32_t least = 0x00800000u, most = 0xff7fffffu;   // (keys of the lowest and the highest finite value)
-  auto bin_of_key = [&](uint32_t k) { return bins_below(top, bin_of(logit_of(k), c)); };
-  // first key of bin b or above it: a few keys around where it should be, or bisected
-  auto first_key = [&](int b) {
-    const uint32_t guess = min(max(key_of((top - (float)b) / c), 0x00800020u), 0xff7fffdfu) - 32;
-    const u64 yes = __builtin_amdgcn_ballot_w64(bin_of_key(guess + lane) <= b);
-    if (yes && !(yes & 1)) return guess + (uint32_t)__builtin_ctzll(yes);
-    uint32_t i = 0x00800000u, j = 0xff7fffffu;
-    while (i < j) {
-      const uint32_t mid = i + (j - i) / 2;
-      if (bin_of_key(mid) <= b) j = mid; else i = mid + 1;
-    }
-    return i;
-  };
-  if (hi < kBins - 1) least = first_key(hi);
-  if (from > 0) most = first_key(from - 1) - 1;
+  if (hi < kBins - 1) least = first_key(top, c, hi);
+  if (from > 0) most = first_key(top, c, from - 1) - 1;
   const float vmin = logit_of(least), vmax = logit_of(most);
   // the chunks to go through, a lane each
   u64 n = 0;
@@ -659,7 +722,7 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (has[e]) {
-        const int to = at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has[e], 0));
+        const int to = at + lanes_before(has[e]);
         if ((has[e] >> lane & 1) && to < LIST) y.list[to] = make_int2(__float_as_int(v[e]), first + e * 64 + lane);
         at += __builtin_popcountll(has[e]);
       }
@@ -698,16 +761,49 @@ __device__ __forceinline__ void list_bins(const T* z, int V, const PartSum* sums
   }
 }
 
-// The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the row is read
-// once more for the tokens of these, which are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
-// which part the token is, and only that is read.  34 rows of 152064 with top-p: 17 us, the chain from the bins to the token; 544 rows of 126464 bf16 with
-// top-k, top-p and min-p: 91 us, two blocks to a compute unit and so two rounds, which read what is not in the caches any more at 5.5 TB/s.  (Three blocks with a
-// list of half the length: 84 to 90 us, and spills; chunks of 512: 98.)
+// The same from what the parts have listed, `most` places each: 64 at a time, a run of these to a wave.
+template <int LIST>
+__device__ __forceinline__ void list_candidates(const int2* candidates, int parts, int most, float c, float top, int from, int hi, RowScratch<LIST>& y) {
+  constexpr int UNITS = kSampleThreads * 16 / kOfListed * (kPartsMax / 2) / 64, PER = (UNITS + kSampleWaves - 1) / kSampleWaves;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, each = most / 64, units = parts * each;   // (at most UNITS)
+  const int per = (units + kSampleWaves - 1) / kSampleWaves;
+  int2 v[PER];
+  u64 has[PER];
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = candidates[(size_t)min(wave * per + i, units - 1) * 64 + lane];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int unit = min(wave * per + i, units - 1), part = unit / each;
+    const int b = bins_below(top, bin_of(__int_as_float(v[i].x), c));
+    has[i] = __builtin_amdgcn_ballot_w64(i < per && wave * per + i < units && (unit - part * each) * 64 + lane < y.chunk_at[part] && b >= from && b <= hi);
+    n += __builtin_popcountll(has[i]);
+  }
+  if (lane == 0) y.x.wcnt[wave] = (uint32_t)n;
+  __syncthreads();
+  int to = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kSampleWaves; ++w) { to += w < wave ? (int)y.x.wcnt[w] : 0; all += (int)y.x.wcnt[w]; }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (has[i]) {
+      const int at = to + lanes_before(has[i]);
+      if ((has[i] >> lane & 1) && at < LIST) y.list[at] = v[i];
+      to += __builtin_popcountll(has[i]);
+    }
+  if (threadIdx.x == 0) y.listed = min(all, LIST);
+}
+
+// The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the tokens of these come from
+// the parts' lists, or, where these are too short, from the row, and are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
+// which part the token is, and only that is read.  34 rows of 152064 with top-p: 16 us, the chain from the bins to the token; 544 rows of 126464 bf16 with
+// top-k, top-p and min-p: 50 us, two blocks to a compute unit and so two rounds.  Where all have to read their row again these take 91 us, 138 MB at 5.5 TB/s
+// (three blocks with a list of half the length: 84 to 90 us, and spills; chunks of 512: 98).
 template <typename T, bool FILTERS, int LIST>
 __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
                                                                      const PartSum* __restrict__ sums, const Spread* __restrict__ spreads,
-                                                                     int* __restrict__ tokens, float4* __restrict__ stats) {
+                                                                     const int2* __restrict__ candidates, int* __restrict__ tokens, float4* __restrict__ stats) {
   extern __shared__ char lds_[];
   RowScratch<LIST>& y = *(RowScratch<LIST>*)lds_;
   Scratch& x = y.x;
@@ -715,6 +811,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
   const float u = uniforms[r];
   const T* z = logits + (size_t)r * ld;
   spreads += (size_t)r * parts;
+  sums += (size_t)r * parts;
   Cut cut;
   u64 all = 0;
   uint32_t count = 0;
@@ -726,7 +823,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
 #pragma unroll
     for (int i = 0; i < 4; ++i) s4[i] = spreads[min(i, parts - 1)][tid];
   }
-  const int state = join_parts(sums + (size_t)r * parts, parts, m, mine);
+  const int listed_of = FILTERS ? sums[min(lane, parts - 1)].listed : 0, depth_of = FILTERS ? sums[min(lane, parts - 1)].depth : 0;
+  const int state = join_parts(sums, parts, m, mine);
   if (state == -1) { no_token(tokens, stats, r); return; }
   const SampleRow row = {(double)m, a.scale};
   if constexpr (FILTERS) {
@@ -741,6 +839,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       if (tid < 64) {
         y.below[tid] = tid < parts && mine.m > -INFINITY ? bins_below(top, bin_of(mine.m, c)) : -1;   // (-1: it has written none)
         y.far[tid] = tid < parts ? mine.count : 0;
+        y.chunk_at[tid] = listed_of;
         y.part_kept[tid] = 0;
       }
       if (tid == 0) { y.bin_k = y.bin_p = kBins; y.listed = 0; }
@@ -831,7 +930,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       sample_whole(src, row, a, u, r, x, tokens, stats);
       return;
     }
-    if (lo < kBins) list_bins(z, V, sums + (size_t)r * parts, part_size, c, top, mode == PLAN_LISTED ? 0 : lo, hi, y);
+    if (lo < kBins) {
+      // (the last bin is listed nowhere)
+      const bool short_of = lane < parts && y.below[lane] >= 0 && y.below[lane] + depth_of <= hi;
+      const int from = mode == PLAN_LISTED ? 0 : lo, most = part_size / kOfListed;
+      if (hi < kBins - 1 && !__builtin_amdgcn_ballot_w64(short_of)) list_candidates(candidates + (size_t)r * parts * most, parts, most, c, top, from, hi, y);
+      else list_bins(z, V, sums, part_size, c, top, from, hi, y);
+    }
     __syncthreads();
     InList src;
     src.fetch(y.list, lo < kBins ? y.listed : 0);
@@ -921,14 +1026,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
 struct SampleSizes { int ne, parts; };
 // Logits to a thread: the fewest with which a batch of rows makes no more than two blocks for each compute unit; four where nothing is
 // listed, as the part that the token is in is then read again.  us by trace, parts and draw, eight logits a thread against sixteen: 32 rows of 126464 without
-// filters 8.5 + 6.6, 7.9 + 10.8; 34 rows of 152064 with top-p (sixteen by the rule) 10.4 + 17.6, 10.0 + 16.9; 544 rows of 126464 (sixteen) 75 + 91, 68 + 91.
+// filters 8.5 + 6.6, 7.9 + 10.8; before parts listed tokens, 34 rows of 152064 with top-p (sixteen by the rule) 10.4 + 17.6, 10.0 + 16.9.
 static SampleSizes sample_sizes(int rows, int V, bool filters) {
   const int parts = (V + kSampleThreads * 8 - 1) / (kSampleThreads * 8);
   if ((long)rows * parts <= (filters ? 512 : 1024)) return {8, parts};
   return {16, (V + kSampleThreads * 16 - 1) / (kSampleThreads * 16)};
 }
 constexpr int kSampleSmall = 16384;   // logits of a row that one block holds in registers
-struct SampleBytes { size_t sums, all; };
+struct SampleBytes { size_t sums, spreads, all; };   // where each ends
 static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) return b;
@@ -937,33 +1042,36 @@ static SampleBytes sample_bytes(int rows, int V) {
   size_t most = (size_t)rows * ((V + kSampleThreads * 16 - 1) / (kSampleThreads * 16));
   if (most < 1024) most = 1024;
   b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
-  b.all = b.sums + most * sizeof(Spread);
+  b.spreads = b.sums + most * sizeof(Spread);
+  b.all = b.spreads + most * kListedMost * sizeof(int2);
   return b;
 }
 size_t sample_workspace(int rows, int V) { return sample_bytes(rows, V).all; }
 
 template <typename T, bool FILTERS, int LIST>
 static void launch_sample_draw(const T* logits, int rows, int parts, int V, size_t ld, int part_size, const float* uniforms,
-                               const SampleArgs& a, const PartSum* sums, const Spread* spreads, int* tokens, float4* stats, hipStream_t s) {
+                               const SampleArgs& a, const PartSum* sums, const Spread* spreads, const int2* candidates, int* tokens, float4* stats,
+                               hipStream_t s) {
   constexpr int smem = sizeof(RowScratch<LIST>);
   static_assert(smem <= 80 * 1024, "two blocks to a compute unit");
   static std::atomic<uint64_t> done{0};
   allow_lds((const void*)sample_draw_kernel<T, FILTERS, LIST>, smem, done);
-  sample_draw_kernel<T, FILTERS, LIST><<<rows, kSampleThreads, smem, s>>>(logits, V, ld, parts, part_size, uniforms, a, sums, spreads, tokens,
-                                                                          stats);
+  sample_draw_kernel<T, FILTERS, LIST><<<rows, kSampleThreads, smem, s>>>(logits, V, ld, parts, part_size, uniforms, a, sums, spreads, candidates,
+                                                                          tokens, stats);
 }
 template <typename T, int NE>
 static void launch_sample_ne(const T* logits, int rows, int parts, int V, size_t ld, const float* uniforms, const SampleArgs& a, int* tokens,
                              float4* stats, char* ws, const SampleBytes& b, hipStream_t s) {
   PartSum* sums = (PartSum*)ws;
   Spread* spreads = (Spread*)(ws + b.sums);
+  int2* candidates = (int2*)(ws + b.spreads);
   const dim3 grid(parts, rows);
   if (a.top_k > 0 || a.top_p < 1.0 || a.min_z > -INFINITY) {
-    sample_parts_kernel<T, NE, true><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    launch_sample_draw<T, true, kList>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
+    sample_parts_kernel<T, NE, true><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads, candidates);
+    launch_sample_draw<T, true, kList>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, candidates, tokens, stats, s);
   } else {
-    sample_parts_kernel<T, NE, false><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads);
-    launch_sample_draw<T, false, 1>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, tokens, stats, s);
+    sample_parts_kernel<T, NE, false><<<grid, kSampleThreads, 0, s>>>(logits, V, ld, a.scale, a.per_z, sums, spreads, candidates);
+    launch_sample_draw<T, false, 1>(logits, rows, parts, V, ld, kSampleThreads * NE, uniforms, a, sums, spreads, candidates, tokens, stats, s);
   }
 }
 

@@ -253,3 +253,19 @@ def test_more_kept_of_the_top_k_than_are_listed():
     z = torch.randn((3, 60000), device="cuda") * 0.01
     check(z, [0.1, 0.5, 0.999], top_k=40000, top_p=0.9)
     check(z.bfloat16(), [0.1, 0.5, 0.999], top_k=40000, top_p=0.9, min_p=0.97)
+
+
+@pytest.mark.parametrize("filters", [dict(top_k=1000), dict(top_k=200, top_p=0.9), dict(top_p=0.8), dict(min_p=0.2), dict(min_p=0.2, top_k=300)], ids=str)
+@pytest.mark.parametrize("order", ["falling", "rising", "one place", "every part alike"])
+def test_where_the_largest_logits_lie(order, filters):
+    """All in one part of a row, which lists only some, or as many in each."""
+    z, u = logits(3, 90000, seed=3)
+    if order == "one place":
+        z = z.clone()
+        z[:, 20000:20400] += 8
+    elif order == "every part alike":
+        z = z[:, :4096].repeat(1, 22)[:, :90000]
+    else:
+        z = z.sort(dim=1, descending=order == "falling").values
+    check(z, u, **filters)
+    check(z.repeat(30, 1)[:90].bfloat16(), np.resize(u, 90), **filters)
