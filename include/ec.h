@@ -351,7 +351,7 @@ int ec_row_entropy_noalloc(const float *logits, int32_t rows, int32_t vocab, siz
 enum { EC_T_F32 = 0, EC_T_BF16 = 1, EC_T_MXFP4 = 2 };
 
 /* How ec_row_sample draws.  temperature: finite, >= 0; 0 takes the most probable token (top_k 1 at temperature 1).  top_k: 0 or
- * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all.  (Rows of more than 16384 logits cost least where top-k, or the tokens around
+ * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all.  (Rows of more than 4096 logits cost least where top-k, or the tokens around
  * the cut, are up to 5632; beyond that, with top-k and top-p together or min_p below 1e-14, one block goes through the row several times.) */
 typedef struct {
   float temperature;
@@ -374,7 +374,7 @@ typedef struct {
  *  stats      DEVICE float32 [rows, 4], 16-byte aligned; written: the drawn token's probability among the kept tokens, its probability
  *             e / S among all, how many are kept, the share of S that they hold.  NaN where the token is -1
  *  workspace  DEVICE, 256-byte aligned, >= ec_row_sample_workspace_bytes(rows, vocab); BORROWED for the call: calls that overlap in time, and
- *             captured graphs that may run side by side, need one each.  0 bytes: none is needed, and it may be NULL (rows of up to 16384
+ *             captured graphs that may run side by side, need one each.  0 bytes: none is needed, and it may be NULL (rows of up to 4096
  *             logits; also for arguments outside the limits, which the call refuses)
  * Enqueues on hip_stream (NULL = default stream) and returns without synchronising; may be captured into a graph.
  * Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP; ec_last_error(NULL) names the cause. */

@@ -1032,15 +1032,18 @@ static SampleSizes sample_sizes(int rows, int V, bool filters) {
   if ((long)rows * parts <= (filters ? 512 : 1024)) return {8, parts};
   return {16, (V + kSampleThreads * 16 - 1) / (kSampleThreads * 16)};
 }
-constexpr int kSampleSmall = 16384;   // logits of a row that one block holds in registers
+// Logits of a row that one block holds in registers.  us of a call with top-k and top-p, by one block and in parts, for 24 and 591 rows: 4096 logits 12 and 32,
+// 15 and 30; 4097 62 and 173, 16 and 30 (32 logits a thread); 16384 68 and 195, 16 and 38.
+constexpr int kSampleSmall = 4096;
 struct SampleBytes { size_t sums, spreads, all; };   // where each ends
 static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) return b;
   if (rows > kSampleBatch) rows = kSampleBatch;
-  // (with eight logits to a thread there are at most 1024 parts)
+  // (parts of eight logits to a thread where they are at most 1024; the last of several batches may have such where the others do not)
   size_t most = (size_t)rows * ((V + kSampleThreads * 16 - 1) / (kSampleThreads * 16));
-  if (most < 1024) most = 1024;
+  const size_t small = (size_t)rows * ((V + kSampleThreads * 8 - 1) / (kSampleThreads * 8));
+  if (small <= 1024 && most < small) most = small;
   b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
   b.spreads = b.sums + most * sizeof(Spread);
   b.all = b.spreads + most * kListedMost * sizeof(int2);
@@ -1080,8 +1083,7 @@ static void launch_sample_t(const T* logits, int rows, int V, size_t ld, const f
                             float4* stats, void* workspace, hipStream_t s) {
   if (V <= kSampleSmall) {
     if (V <= 1024) sample_small_kernel<T, 2><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
-    else if (V <= 4096) sample_small_kernel<T, 8><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
-    else sample_small_kernel<T, 32><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
+    else sample_small_kernel<T, 8><<<rows, kSampleThreads, 0, s>>>(logits, V, ld, uniforms, a, tokens, stats);
     return;
   }
   const SampleBytes b = sample_bytes(rows, V);

@@ -241,8 +241,8 @@ def test_a_top_k_beyond_32_bits_is_all():
         ec.row_sample(z, u, top_k=-2 ** 32 + 5)
 
 
-@pytest.mark.parametrize("V", [16384, 16385, 20481])
-@pytest.mark.parametrize("filters", [dict(), dict(top_k=4, top_p=0.99), dict(top_p=0.7), dict(min_p=2.0 ** -50), dict(top_k=16383)], ids=str)
+@pytest.mark.parametrize("V", [4095, 4096, 4097, 4200, 8191, 8192, 8193, 16384, 16385, 20481])
+@pytest.mark.parametrize("filters", [dict(), dict(top_k=4, top_p=0.99), dict(top_p=0.7), dict(min_p=2.0 ** -50), dict(top_k=4095), dict(top_k=16383)], ids=str)
 def test_around_the_longest_row_of_one_block(V, filters):
     z, u = logits(3, V)
     check(z, u, **filters)

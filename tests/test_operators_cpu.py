@@ -39,7 +39,7 @@ def test_sample_workspace(lib):
     assert sample(lib, ws=None, **big) == sample(lib, ws=P + 128, **big) == ec.EC_ERR_WORKSPACE
     need = lib.ec_row_sample_workspace_bytes(4, 40000)
     assert need > 0 and sample(lib, size=need - 1, **big) == ec.EC_ERR_WORKSPACE
-    for rows, vocab in ((-1, 40000), (65536, 40000), (4, 1), (4, 163841), (4, 16384), (0, 40000)):
+    for rows, vocab in ((-1, 40000), (65536, 40000), (4, 1), (4, 163841), (4, 4096), (0, 40000)):
         assert lib.ec_row_sample_workspace_bytes(rows, vocab) == 0
     assert sample(lib, rows=0, logits=None, uniforms=None, tokens=None, stats=None, ws=None) == ec.EC_OK
 
