@@ -879,19 +879,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
       by_k = a.top_k > 0 && (u64)a.top_k < finite;
       if (by_k && cb < (u64)a.top_k && (u64)a.top_k <= cb + n) y.bin_k = tid;
       __syncthreads();
-      // Top-k that ends among tokens of no weight takes nothing from the others: all that it says is how many are kept, if nothing else does.
+      // the bin of min_p's border, up to one off by roundings
+      const int bm = a.min_z > -INFINITY ? (int)fmax(fmin((double)top - floor((row.m + a.min_z) * a.per_z), (double)kBins), 0.0) : kBins;
+      // Top-k that ends in the last bin, among tokens of no weight, takes nothing from the others: all that it says is how many are kept,
+      // if nothing else does.  Where min_p's border may lie in that bin too, it cuts there like in any other.
       const int bin_k = y.bin_k;
+      const bool both_last = !by_p && a.min_z > -INFINITY && bm + 1 >= kBins - 1;
       fixed = by_k && bin_k == kBins - 1 && !by_p && a.min_z == -INFINITY ? a.top_k : 0;
-      by_k = by_k && bin_k < kBins - 1;
+      by_k = by_k && (bin_k < kBins - 1 || both_last);
       const u64 want = by_p ? mass_wanted(a.top_p, all) : 0;
       if (by_p && !by_k && mb < want && want <= mb + s) y.bin_p = tid;
       __syncthreads();
-      // kBins: no cut.  (The bin of min_p's border is known up to roundings.  Where top-p goes by the sum of the top-k,
-      // these have to be there.)
+      // kBins: no cut.  (Where top-p goes by the sum of the top-k, these have to be there.)
       const int k_at = by_k ? bin_k : kBins, p_at = y.bin_p;
       lo = hi = min(k_at, p_at);
       if (a.min_z > -INFINITY && !(by_k && by_p)) {
-        const int bm = (int)fmax(fmin((double)top - floor((row.m + a.min_z) * a.per_z), (double)kBins), 0.0);
         lo = min(lo, max(bm - 1, 0));
         hi = min(hi, bm + 1);
       }
