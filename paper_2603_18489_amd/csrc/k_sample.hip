@@ -358,11 +358,11 @@ __device__ __forceinline__ u64 draw_at(float u, u64 total) {
   return min((u64)at + 1, total);
 }
 
-// The place of the token: the first whose running sum of kept weights is `want` or more.  kept, count: of these tokens; `at` is called by
-// every thread with them and says what is wanted.  Returns true to one lane.
+// The place of the token: the first whose running sum of kept weights is `want` or more.  kept, count: of these tokens; `wanted` is called by
+// every thread with them and says what is wanted.  Returns true to one lane, whose `close` says that the token begins or ends within `near` of it.
 template <typename S, typename W>
 __device__ __forceinline__ bool draw_place(const S& src, const SampleRow& row, const Cut& cut, int shift, double least, Scratch& x,
-                                           u64& kept, uint32_t& count, W wanted, int& place, float& logit) {
+                                           u64& kept, uint32_t& count, W wanted, int& place, float& logit, u64 near, bool& close) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   u64 part = 0;
   uint32_t n = 0;
@@ -396,7 +396,7 @@ __device__ __forceinline__ bool draw_place(const S& src, const SampleRow& row, c
       const u64 past = __builtin_amdgcn_ballot_w64(upto >= want);
       if (past) {
         over = true;
-        if (lane == __builtin_ctzll(past)) { found = true; place = at; logit = v; }
+        if (lane == __builtin_ctzll(past)) { found = true; place = at; logit = v; close = want + w - upto < near || upto - want < near; }
       }
       mine += wave_sum_u64(w);
     });
@@ -441,7 +441,8 @@ __device__ void sample_whole(const S& src, const SampleRow& row, const SampleArg
   uint32_t n;
   int place;
   float z;
-  if (draw_place(src, row, cut, 0, row.m + a.min_z, x, kept, n, [&](u64 k) { return draw_at(u, k); }, place, z))
+  bool close;
+  if (draw_place(src, row, cut, 0, row.m + a.min_z, x, kept, n, [&](u64 k) { return draw_at(u, k); }, place, z, 0, close))
     put_token(tokens, stats, r, place, z, row, kept, n, all);
 }
 
@@ -643,13 +644,19 @@ template <int LIST> struct RowScratch {
   };
   uint32_t cnt[kBins];
   int below[64], far[64];   // a part's bins lie so far below the row's (-1: it has none); logits in its last
-  int bin_k, bin_p;
+  int bin_k, bin_p, redo;
   u64 cum_mass[kBins + 1], part_kept[64];   // cum: of the bins above
   uint32_t cum_cnt[kBins + 1];
   int chunk_cnt[kChunksMax], chunk_at[kChunksMax], chunk_id[kChunksMax], listed;
   int2 list[LIST];          // logit and id
 };
 static_assert(offsetof(Scratch, mass) == 0 && sizeof(Scratch::mass) >= kBins * 16, "frac and unit lie over mass");
+
+// A sum of bins is off by up to 2^-36.5 of itself: in each of its logits, where 1 is the weight at the bin's lower end, by 2^-37 from rounding
+// and 7.1e-13 from the polynomial, of 0.992 or more.  So a sum that is wanted and one that is compared with it are off by less than 2^-35 of
+// the largest.  Where a border is as near (in rows of equal logits it may be met exactly: half of them kept, or u the share of the first
+// ones), the block goes through the row, whose sums are exact.  34 rows of 152064 with top-p: 32.1 us as without the test.
+constexpr int kNear = 35;
 
 // Bins lo .. hi hold the cut: all above is kept and all below is not.  LISTED: the tokens of bins 0 .. hi are listed, up to LIST of them;
 // CUT: those of lo .. hi; WHOLE: neither will do.
@@ -800,7 +807,7 @@ __device__ __forceinline__ void list_candidates(const int2* candidates, int part
 // top-k, top-p and min-p: 50 us, two blocks to a compute unit and so two rounds.  Where all have to read their row again these take 91 us, 138 MB at 5.5 TB/s
 // (three blocks with a list of half the length: 84 to 90 us, and spills; chunks of 512: 98).
 template <typename T, bool FILTERS, int LIST>
-__global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
+__global__ __launch_bounds__(kSampleThreads, FILTERS ? 4 : 1) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
                                                                      const PartSum* __restrict__ sums, const Spread* __restrict__ spreads,
                                                                      const int2* __restrict__ candidates, int* __restrict__ tokens, float4* __restrict__ stats) {
@@ -815,6 +822,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
   Cut cut;
   u64 all = 0;
   uint32_t count = 0;
+  bool whole = false;   // the row is gone through by this block
   float m;
   PartHead mine;
   // (a thread a bin of each part; the first four asked for ahead of everything else)
@@ -842,7 +850,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
         y.chunk_at[tid] = listed_of;
         y.part_kept[tid] = 0;
       }
-      if (tid == 0) { y.bin_k = y.bin_p = kBins; y.listed = 0; }
+      if (tid == 0) { y.bin_k = y.bin_p = kBins; y.listed = 0; y.redo = 0; }
       __syncthreads();
       auto row_bin = [&](int p, int b) { return min(b + y.below[p], kBins - 1); };
       constexpr u64 kFrac = (1ull << 48) - 1;
@@ -926,13 +934,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
         }
       }
     }
-    if (mode == PLAN_WHOLE) {
-      InMemory<T> src;
-      src.fetch(z, V);
-      sample_whole(src, row, a, u, r, x, tokens, stats);
-      return;
-    }
-    if (lo < kBins) {
+    whole = mode == PLAN_WHOLE;
+    if (!whole && lo < kBins) {
       // (the last bin is listed nowhere)
       const bool short_of = lane < parts && y.below[lane] >= 0 && y.below[lane] + depth_of <= hi;
       const int from = mode == PLAN_LISTED ? 0 : lo, most = part_size / kOfListed;
@@ -941,10 +944,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
     }
     __syncthreads();
     InList src;
-    src.fetch(y.list, lo < kBins ? y.listed : 0);
+    src.fetch(y.list, !whole && lo < kBins ? y.listed : 0);
     u64 of_k = all;
     for (int by_mass = 0; by_mass < 2; ++by_mass) {
-      if (!(by_mass ? by_p : by_k)) continue;
+      if (whole || !(by_mass ? by_p : by_k)) continue;
       const u64 want = by_mass ? mass_wanted(a.top_p, of_k) : (u64)a.top_k;
       int at = by_mass ? y.bin_p : y.bin_k;
       if (by_mass && by_k) {   // (the sum of the top-k is known only now)
@@ -970,27 +973,34 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
         of_k = select_digits(src, row, by_mass, want, y.cum_cnt[at], y.cum_mass[at],
                              [&](float v) { return bins_below(top, bin_of(v, c)) == at; }, cut, x);
       }
+      if (by_mass) {   // (what is kept, with the cut's token and without)
+        const u64 without = of_k - row.weight(logit_of(cut.key)), near = all >> kNear;
+        whole = want < without + near || of_k < want + near;
+      }
     }
-    if (mode == PLAN_LISTED) {
+    if (!whole && mode == PLAN_LISTED) {
       u64 kept;
       int place;
       float v;
-      if (draw_place(src, row, cut, 0, row.m + a.min_z, x, kept, count, [&](u64 k) { return draw_at(u, k); }, place, v))
+      bool close;
+      if (draw_place(src, row, cut, 0, row.m + a.min_z, x, kept, count, [&](u64 k) { return draw_at(u, k); }, place, v, 0, close))
         put_token(tokens, stats, r, y.list[place].y, v, row, kept, count, all);
       return;
     }
     // what is kept of each part: all above the bins, and some of the list
-    u64 n = 0;
-    src.each([&](int at, float v, bool) {
-      const u64 w = row.weight(v);
-      if (v > -INFINITY && v >= row.m + a.min_z && cut.keeps(key_of(v), at)) {
-        ++n;
-        atomicAdd(&y.part_kept[y.list[at].y / part_size], w);
-      }
-    });
-    count = y.cum_cnt[lo] + (uint32_t)block_sum_u64(n, x);
-    if (fixed) count = fixed;
-    if (cut.last != INT_MAX) cut.last = y.list[cut.last].y;
+    if (!whole) {
+      u64 n = 0;
+      src.each([&](int at, float v, bool) {
+        const u64 w = row.weight(v);
+        if (v > -INFINITY && v >= row.m + a.min_z && cut.keeps(key_of(v), at)) {
+          ++n;
+          atomicAdd(&y.part_kept[y.list[at].y / part_size], w);
+        }
+      });
+      count = y.cum_cnt[lo] + (uint32_t)block_sum_u64(n, x);
+      if (fixed) count = fixed;
+      if (cut.last != INT_MAX) cut.last = y.list[cut.last].y;
+    }
   } else {
     const bool some = lane < parts && mine.m > -INFINITY;
     if (tid < 64)   // (the part's sum, seen from the row's maximum)
@@ -998,29 +1008,47 @@ __global__ __launch_bounds__(kSampleThreads) void sample_draw_kernel(const T* __
     count = (uint32_t)wave_sum_u64(some ? (u64)mine.count : 0);
   }
   __syncthreads();
-  const u64 kept = wave_sum_u64(y.part_kept[lane]);
-  if constexpr (!FILTERS) all = kept;
-  // The part of the token, then the token.  The part's own weights, seen from the row's maximum, may come to a little less than its sum did, to
-  // nothing where each rounds to 0: then the next part's first.
-  const u64 want = draw_at(u, kept);
-  u64 base = wave_before_u64(y.part_kept[lane]);
-  int p = __builtin_ctzll(__builtin_amdgcn_ballot_w64(base + y.part_kept[lane] >= want));
-  {
-    const uint32_t bhi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(base >> 32), p), blo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)base, p);
-    base = (u64)bhi << 32 | blo;
+  if (!whole) {
+    const u64 kept = wave_sum_u64(y.part_kept[lane]);
+    if constexpr (!FILTERS) all = kept;
+    // The part of the token, then the token.  The part's own weights, seen from the row's maximum, may come to a little less than its sum did, to
+    // nothing where each rounds to 0: then the next part's first.  (With filters the row decides, as near a border.)
+    const u64 want = draw_at(u, kept);
+    u64 base = wave_before_u64(y.part_kept[lane]);
+    int p = __builtin_ctzll(__builtin_amdgcn_ballot_w64(base + y.part_kept[lane] >= want));
+    {
+      const uint32_t bhi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(base >> 32), p), blo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)base, p);
+      base = (u64)bhi << 32 | blo;
+    }
+    for (int tried = 0; tried <= parts; ++tried, p = p + 1 < parts ? p + 1 : 0) {
+      const int first = p * part_size;
+      InMemory<T> src;
+      src.fetch(z + first, min(V - first, part_size));
+      u64 here;
+      uint32_t n;
+      int place;
+      float v;
+      bool close;
+      const bool found = draw_place(src, row, cut, first, row.m + a.min_z, x, here, n,
+                                    [&](u64 k) { return tried ? min((u64)1, k) : min(want - base, k); }, place, v, FILTERS ? kept >> kNear : 0, close);
+      if (found) {
+        if (FILTERS && close) y.redo = 1;
+        else put_token(tokens, stats, r, first + place, v, row, kept, count, all);
+      }
+      whole = FILTERS && here == 0;
+      if (here > 0 || whole) break;   // (the same for all threads)
+    }
+    if constexpr (FILTERS) {
+      __syncthreads();
+      whole |= y.redo != 0;
+    }
   }
-  for (int tried = 0; tried <= parts; ++tried, p = p + 1 < parts ? p + 1 : 0) {
-    const int first = p * part_size;
-    InMemory<T> src;
-    src.fetch(z + first, min(V - first, part_size));
-    u64 here;
-    uint32_t n;
-    int place;
-    float v;
-    const bool found = draw_place(src, row, cut, first, row.m + a.min_z, x, here, n,
-                                  [&](u64 k) { return tried ? min((u64)1, k) : min(want - base, k); }, place, v);
-    if (found) put_token(tokens, stats, r, first + place, v, row, kept, count, all);
-    if (here > 0) break;   // (the same for all threads)
+  if constexpr (FILTERS) {
+    if (whole) {
+      InMemory<T> src;
+      src.fetch(z, V);
+      sample_whole(src, row, a, u, r, x, tokens, stats);
+    }
   }
 }
 
