@@ -374,8 +374,8 @@ typedef struct {
  *  stats      DEVICE float32 [rows, 4], 16-byte aligned; written: the drawn token's probability among the kept tokens, its probability
  *             e / S among all, how many are kept, the share of S that they hold.  NaN where the token is -1
  *  workspace  DEVICE, 256-byte aligned, >= ec_row_sample_workspace_bytes(rows, vocab); BORROWED for the call: calls that overlap in time, and
- *             captured graphs that may run side by side, need one each.  0 bytes: none is needed, and it may be NULL (rows of up to 4096
- *             logits; also for arguments outside the limits, which the call refuses)
+ *             captured graphs that may run side by side, need one each.  One for so many rows serves fewer rows too.  0 bytes: none is
+ *             needed, and it may be NULL (rows of up to 4096 logits; also for arguments outside the limits, which the call refuses)
  * Enqueues on hip_stream (NULL = default stream) and returns without synchronising; may be captured into a graph.
  * Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP; ec_last_error(NULL) names the cause. */
 size_t ec_row_sample_workspace_bytes(int32_t rows, int32_t vocab);

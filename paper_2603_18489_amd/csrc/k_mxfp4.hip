@@ -985,13 +985,43 @@ static void launch_linear_t(const MxProduct& p, hipStream_t s) {
 
 // parts' sums [ranges][M][N], then the scales of 4-bit rows in whole dwords.  (These may be wanted for scales that begin at any byte, which is not
 // known here.)
-static size_t mx_parts_bytes(bool x4, long M, int N, int kb) {
-  if (M <= 0) return 0;
-  const int parts = M <= kMxFewRows ? pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts;
+static size_t mx_sums_bytes(int parts, long M, int N) {
   return parts > 1 ? ((size_t)parts * M * ((N + 3) / 4 * 4) * sizeof(float) + 255) / 256 * 256 : 0;
 }
+static size_t mx_parts_bytes(bool x4, long M, int N, int kb) {
+  return mx_sums_bytes(M <= kMxFewRows ? pick_rows(x4, (int)M, N, kb).parts : pick_tiled(x4, (int)M, N, kb).parts, M, N);
+}
+// Ranges of K by the rows there are: pick_rows goes by fours of rows; of 64 that begin at a multiple of 64, what pick_tiled compares differs by the
+// join alone, which costs more the more ranges and rows there are, so that the first row has the most ranges.  Found once for the shapes that
+// a thread has in hand (2 us, where a call takes 9).
+struct MxRanges {
+  static constexpr int FEW = kMxFewRows / 4, ALL = FEW + (kMxSplitRows - kMxFewRows) / 64;
+  int n = 0, kb = 0;
+  bool x4 = false;
+  uint8_t parts[ALL] = {};
+  static long last(int i) { return i < FEW ? 4 * i + 4 : kMxFewRows + 64l * (i - FEW + 1); }
+  static const MxRanges& of(bool x4, int N, int kb) {
+    static thread_local MxRanges known[64];
+    MxRanges& r = known[((uint32_t)N * 2654435761u ^ (uint32_t)(kb * 2 + x4) * 2246822519u) >> 26];
+    if (r.n != N || r.kb != kb || r.x4 != x4) {
+      for (int i = 0; i < ALL; ++i) {
+        const int m = i ? (int)last(i - 1) + 1 : 1;
+        r.parts[i] = (uint8_t)(i < FEW ? pick_rows(x4, m, N, kb).parts : pick_tiled(x4, m, N, kb).parts);
+      }
+      r.n = N; r.kb = kb; r.x4 = x4;
+    }
+    return r;
+  }
+};
+// room for M rows or fewer
 size_t mx_linear_workspace(bool x4, long M, int N, int kb) {
-  return mx_parts_bytes(x4, M, N, kb) + (x4 && M > kMxFewRows ? (size_t)M * mx_tiles_of_k(kb) * 4 : 0);
+  const MxRanges& ranges = MxRanges::of(x4, N, kb);
+  size_t most = 0;
+  for (int i = 0; i < MxRanges::ALL && (i == 0 || MxRanges::last(i - 1) < M); ++i) {
+    const long m = MxRanges::last(i) < M ? MxRanges::last(i) : M;
+    if (ranges.parts[i] > 1) most = most > mx_sums_bytes(ranges.parts[i], m, N) ? most : mx_sums_bytes(ranges.parts[i], m, N);
+  }
+  return most + (x4 && M > kMxFewRows ? (size_t)M * mx_tiles_of_k(kb) * 4 : 0);
 }
 
 void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,

@@ -1070,10 +1070,11 @@ static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) return b;
   if (rows > kSampleBatch) rows = kSampleBatch;
-  // (parts of eight logits to a thread where they are at most 1024; the last of several batches may have such where the others do not)
-  size_t most = (size_t)rows * ((V + kSampleThreads * 16 - 1) / (kSampleThreads * 16));
-  const size_t small = (size_t)rows * ((V + kSampleThreads * 8 - 1) / (kSampleThreads * 8));
-  if (small <= 1024 && most < small) most = small;
+  // Fewer rows may have more parts, of eight logits to a thread, up to 1024 in all: there is room for as many rows of these as it takes.  (The last of
+  // several batches has few rows too.)
+  const size_t p16 = (V + kSampleThreads * 16 - 1) / (kSampleThreads * 16), p8 = (V + kSampleThreads * 8 - 1) / (kSampleThreads * 8);
+  const size_t small = ((size_t)rows < 1024 / p8 ? (size_t)rows : 1024 / p8) * p8;
+  const size_t most = rows * p16 > small ? rows * p16 : small;
   b.sums = (most * sizeof(PartSum) + 255) / 256 * 256;
   b.spreads = b.sums + most * sizeof(Spread);
   b.all = b.spreads + most * kListedMost * sizeof(int2);
