@@ -488,6 +488,7 @@ def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
         ld = ld if rows > 1 else (k + 7) // 8 * 8
         tensors, x_kind, x_scales = (x, w.data), EC_T_BF16, None
     _need(k == w.k, "x has another k than the matrix")
+    _need(w.data.dtype == torch.uint8 and w.data.is_contiguous(), "data must be contiguous uint8, as mxfp4_pack makes it")
     lib = _lib or load_library()
 
     def call(raw):
