@@ -415,6 +415,10 @@ size_t ec_mx_linear_workspace_bytes(int32_t x_type, int64_t rows, int32_t n, int
 int ec_mx_linear(const void *x, const uint8_t *x_scales, int32_t x_type, int64_t rows, size_t ld, const void *packed, int32_t n,
                  int32_t k, void *y, int32_t y_type, size_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Which blocks ec_mx_linear cuts a product into (test and diagnosis aid; pure host computation): shape = {rows of a block, features of
+ * a block, ranges that K is split into}.  Errors: EC_ERR_ARG. */
+int ec_debug_mx_blocks(int32_t x_type, int64_t rows, int32_t n, int32_t k, int32_t shape[3] /*HOST*/);
+
 /* Frees host-side state only; never frees weights or workspace.  NULL is allowed. */
 void ec_destroy(ec_ctx *ctx);
 

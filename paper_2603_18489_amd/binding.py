@@ -33,7 +33,7 @@ KERNEL_CLASS_NAMES = ["embed", "norm", "qkv", "rope_kv", "attn", "oproj", "gateu
 EXPORTS = ["ec_workspace_bytes", "ec_init", "ec_reset", "ec_step", "ec_step_forced", "ec_debug_keep_logits",
            "ec_step_forced_batch", "ec_generate", "ec_profile_enable", "ec_profile_read",
            "ec_debug_read", "ec_debug_read_seq", "ec_debug_block_shape", "ec_debug_attn_tiles", "ec_debug_meeting",
-           "ec_destroy", "ec_strerror", "ec_last_error",
+           "ec_debug_mx_blocks", "ec_destroy", "ec_strerror", "ec_last_error",
            "ec_row_entropy_workspace_bytes", "ec_row_entropy", "ec_row_entropy_noalloc",
            "ec_row_sample_workspace_bytes", "ec_row_sample", "ec_mx_quantize", "ec_mx_dequantize",
            "ec_mx_packed_bytes", "ec_mx_pack", "ec_mx_linear_workspace_bytes", "ec_mx_linear"]
@@ -163,6 +163,8 @@ def load_library() -> C.CDLL:
     lib.ec_mx_pack.argtypes = [vp, vp, C.c_int32, C.c_int32, vp, C.c_size_t, vp]
     lib.ec_mx_linear_workspace_bytes.restype = C.c_size_t
     lib.ec_mx_linear_workspace_bytes.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32]
+    lib.ec_debug_mx_blocks.restype = C.c_int
+    lib.ec_debug_mx_blocks.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, i32p]
     lib.ec_mx_linear.restype = C.c_int
     lib.ec_mx_linear.argtypes = [vp, vp, C.c_int32, C.c_int64, C.c_size_t, vp, C.c_int32, C.c_int32, vp, C.c_int32,
                                  C.c_size_t, vp, C.c_size_t, vp]
@@ -248,6 +250,15 @@ def attn_tiles(cfg, rows: Sequence[int], positions: Sequence[int]) -> int:
     if rc != EC_OK:
         raise EcError(rc, load_library().ec_last_error(None).decode())
     return tiles.value
+
+
+def mx_blocks(x_type: int, rows: int, n: int, k: int):
+    """ec_debug_mx_blocks: (rows, features, ranges of K) of the blocks of a 4-bit product."""
+    shape = (C.c_int32 * 3)()
+    rc = load_library().ec_debug_mx_blocks(x_type, rows, n, k, shape)
+    if rc != EC_OK:
+        raise EcError(rc, load_library().ec_last_error(None).decode())
+    return tuple(shape)
 
 
 def _raw_stream(torch, stream, device: int) -> int:

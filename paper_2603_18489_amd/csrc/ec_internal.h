@@ -305,6 +305,7 @@ void launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, long rows
 void launch_mx_pack(const uint8_t* codes, const uint8_t* scales, int n, int kb, uint8_t* packed, hipStream_t s);
 // x: bfloat16 rows, or codes where x_scales is given; workspace: mx_linear_workspace bytes
 size_t mx_linear_workspace(bool x4, long M, int N, int kb);
+void mx_linear_blocks(bool x4, long M, int N, int kb, int32_t shape[3]);   // rows and features of a block, ranges of K
 void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,
                       bool y_bf16, size_t ldy, void* workspace, hipStream_t s);
 

@@ -137,6 +137,14 @@ size_t ec_mx_linear_workspace_bytes(int32_t x_type, int64_t rows, int32_t n, int
   return mx_linear_workspace(x_type == EC_T_MXFP4, rows, n, k / 32);
 }
 
+int ec_debug_mx_blocks(int32_t x_type, int64_t rows, int32_t n, int32_t k, int32_t shape[3]) {
+  if (x_type != EC_T_BF16 && x_type != EC_T_MXFP4) return op_fail(EC_ERR_ARG, "x must be EC_T_BF16 or EC_T_MXFP4");
+  if (rows < 1 || rows > kMxLinearRowsMax || !ec_mx_packed_bytes(n, k)) return op_fail(EC_ERR_ARG, "rows, n or k outside ec_mx_linear's limits");
+  if (!shape) return op_fail(EC_ERR_ARG, "shape must not be NULL");
+  mx_linear_blocks(x_type == EC_T_MXFP4, rows, n, k / 32, shape);
+  return EC_OK;
+}
+
 int ec_mx_linear(const void* x, const uint8_t* x_scales, int32_t x_type, int64_t rows, size_t ld, const void* packed, int32_t n,
                  int32_t k, void* y, int32_t y_type, size_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (x_type != EC_T_BF16 && x_type != EC_T_MXFP4) return op_fail(EC_ERR_ARG, "x must be EC_T_BF16 or EC_T_MXFP4");

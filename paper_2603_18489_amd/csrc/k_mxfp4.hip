@@ -931,9 +931,10 @@ static void launch_tiled4_t(const MxProduct& p, int parts, hipStream_t s) {
 //   4 bits 64 x 256 1.00 + 3    128 x 128 1.00 + 3  (16x16x128: quicker to start)
 //          256 x 256 2.50 + 4.5 192 x 384 2.90 + 4.5  128 x 256 1.40 + 4.5  192 x 256 2.00 + 4.5  (32x32x64)
 enum { MX_128x256, MX_64x256, MX_128x128, MX_256x256_4, MX_192x384_4, MX_128x256_4, MX_192x256_4, MX_SHAPES };
+static const int kMxBlockRows[MX_SHAPES] = {128, 64, 128, 256, 192, 128, 192}, kMxBlockCols[MX_SHAPES] = {256, 256, 128, 256, 384, 256, 256};
 struct MxTiledShape { int shape, parts; };
 static MxTiledShape pick_tiled(bool x4, int M, int N, int kb) {
-  static const int bm[MX_SHAPES] = {128, 64, 128, 256, 192, 128, 192}, bn[MX_SHAPES] = {256, 256, 128, 256, 384, 256, 256};
+  const int *bm = kMxBlockRows, *bn = kMxBlockCols;
   static const double us16[MX_SHAPES] = {1.65, 1.05, 1.05}, us4[MX_SHAPES] = {0, 1.0, 1.0, 2.5, 2.9, 1.4, 2.0};
   const int stages = x4 ? (mx_tiles_of_k(kb) + 1) / 2 : mx_tiles_of_k(kb);
   MxTiledShape best = {MX_128x128, 1};
@@ -961,6 +962,19 @@ static void launch_tiled(const MxProduct& p, hipStream_t s) {
 }
 
 constexpr int kMxFewRows = 64;   // up to here W is streamed past all rows at once
+void mx_linear_blocks(bool x4, long M, int N, int kb, int32_t shape[3]) {
+  if (M <= kMxFewRows) {
+    const MxRowsShape w = pick_rows(x4, (int)M, N, kb);
+    shape[0] = (int)((M + 15) / 16 * 16);
+    shape[1] = w.shared == MX_ALONE ? w.ntw * 16 : w.shared == MX_SHARED_128 ? 128 : 256;
+    shape[2] = w.parts;
+  } else {
+    const MxTiledShape w = pick_tiled(x4, (int)M, N, kb);
+    shape[0] = kMxBlockRows[w.shape];
+    shape[1] = kMxBlockCols[w.shape];
+    shape[2] = w.parts;
+  }
+}
 template <bool X4, typename TY>
 static void launch_linear_t(const MxProduct& p, hipStream_t s) {
   constexpr int XF = X4 ? MX_X4 : MX_RING;
