@@ -51,7 +51,7 @@ def test_equal_logits_at_whole_shares(V, kept, level, temperature):
     z = torch.full((len(SHARES), V), -INF, device="cuda")
     at = np.sort(np.random.default_rng(V).permutation(V)[:kept])
     z[:, at] = level
-    for n, filters in ((kept // 2, dict(top_p=0.5)), (kept // 4, dict(top_p=0.25, min_p=0.5)), (kept, dict(min_p=0.3)), (kept - 1000, dict(top_k=kept - 1000)),
+    for n, filters in ((kept, dict()), (kept // 2, dict(top_p=0.5)), (kept // 4, dict(top_p=0.25, min_p=0.5)), (kept, dict(min_p=0.3)), (kept - 1000, dict(top_k=kept - 1000)),
                        (kept // 4, dict(top_k=kept // 2, top_p=0.5))):
         tokens, stats = check(z, SHARES, temperature=temperature, **filters)
         assert (stats[:, 2] == n).all() and (tokens == at[np.floor(np.array(SHARES) * n).astype(int)]).all()
