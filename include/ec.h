@@ -351,8 +351,12 @@ int ec_row_entropy_noalloc(const float *logits, int32_t rows, int32_t vocab, siz
 enum { EC_T_F32 = 0, EC_T_BF16 = 1, EC_T_MXFP4 = 2 };
 
 /* How ec_row_sample draws.  temperature: finite, >= 0; 0 takes the most probable token (top_k 1 at temperature 1).  top_k: 0 or
- * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all.  (Rows of more than 4096 logits cost least where top-k, or the tokens around
- * the cut, are up to 5632; beyond that, with top-k and top-p together or min_p below 1e-14, one block goes through the row several times.) */
+ * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all.
+ * Rows of more than 4096 logits cost least (32 of 126464: 25 to 66 us) where few tokens are near the cut.  One block goes through the whole row
+ * several times (220 to 510 us) where more than 5632 have to be looked at: those of the cut's sixteenth of a temperature in z (three sixteenths
+ * for min_p, and all that weighs less than e^-32 for one below 1e-14), with top-k and top-p together all of the top-k; where a border lies within 2^-35 of the
+ * row's sum; and where one of its runs of 4096 or 8192 logits has a largest one beyond 65536 temperatures from 0, as a range masked with the
+ * type's lowest value does (375 us; masked with -inf: 63). */
 typedef struct {
   float temperature;
   int32_t top_k;
@@ -363,9 +367,9 @@ typedef struct {
  * e_i = exp((z_i - max z) / temperature), S the sum of all e and the tokens in the order (z descending, id ascending), a row keeps
  * the token of rank j if  j < top_k;  the e of the ranks before j sum to less than top_p times the sum of the top_k e;
  * e >= min_p;  z > -inf.  The token drawn is the lowest id for which the running sum of the kept e, in the order of the ids, exceeds u
- * times the sum of all kept.  e is computed in 64 bits and summed in whole numbers, so the result does not depend on the order of anything: the same
- * arguments give the same bits.  A sum is off by at most 2^-35 of itself and vocab * 2^-46 (e of the largest logit being 1): so near are the places where one
- * token ends and the next begins.
+ * times the sum of all kept.  e is computed in 64 bits and summed in whole numbers, so the result does not depend on the order of anything:
+ * the same arguments give the same bits.  The places where one token ends and the next begins are off by at most 2^-43 of a sum and vocab *
+ * 2^-45 (e of the largest logit being 1); among equal logits they are exact.
  *  logits     DEVICE [rows, vocab] of `type` (EC_T_F32 or EC_T_BF16), row stride ld elements (ld >= vocab); read only
  *  rows       0 .. 65535; vocab 2 .. 163840
  *  uniforms   DEVICE float32 [rows], u in [0, 1); below 0 and NaN count as 0, 1 and above as the largest float32 below 1

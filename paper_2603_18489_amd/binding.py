@@ -395,7 +395,8 @@ def row_sample(logits, uniforms, temperature: float = 1.0, top_k: int = 0, top_p
                stream=None):
     """ec_row_sample: a token drawn from each row of a float32 or bfloat16 CUDA matrix [rows, vocab], from the numbers
     `uniforms` (float32 [rows], in [0, 1)).  Returns an int32 tensor [rows] of tokens and a float32 tensor [rows, 4]
-    (probability among the kept tokens, among all, number kept, share of the probability kept).  `stream` as for row_entropy."""
+    (probability among the kept tokens, among all, number kept, share of the probability kept).  Mask logits with -inf rather than with
+    low finite numbers: long rows with filters cost less so.  `stream` as for row_entropy; no gradients."""
     import torch
     kind = _plain_type(logits.dtype)
     rows, vocab, ld = _rows_of(logits)
@@ -486,7 +487,7 @@ def mxfp4_pack(q: Mxfp4, stream=None) -> Mxfp4Matrix:
 
 def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
     """ec_mx_linear: x W^T, float32 or bfloat16 (the default), for x a bfloat16 CUDA matrix [rows, k] (row stride a multiple
-    of 8 elements) or one in 4 bits (Mxfp4)."""
+    of 8 elements) or one in 4 bits (Mxfp4).  For inference: the result carries no gradient, whatever x requires."""
     import torch
     dtype = torch.bfloat16 if dtype is None else dtype
     kind = _plain_type(dtype)

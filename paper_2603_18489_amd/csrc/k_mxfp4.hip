@@ -23,7 +23,7 @@ __device__ __forceinline__ uint32_t mx_scale(float amax) {
   const uint32_t e = __float_as_uint(amax) >> 23;   // (biased exponent, 0 for subnormals)
   return e == 255 ? 255u : e > 2 ? e - 2 : 0u;
 }
-// 2^(127 - s): what brings a block of scale s to the codes' range.  s = 254 and 253 give subnormals, which are kept.
+// 2^(127 - s): what brings a block of scale s to the codes' range.  A finite block has s <= 252; the other value is for 255, whose codes are not used.
 __device__ __forceinline__ float mx_to_codes(uint32_t s) {
   return s < 254 ? __uint_as_float((254 - s) << 23) : 0x1p-127f;
 }
@@ -175,10 +175,11 @@ enum { MX_RING = 0, MX_REGS = 1, MX_X4 = 2 };   // where a wave's rows go: bf16 
 // waves share that out, and their sums meet in LDS in the order of the waves.  What a wave multiplies next is on its way while
 // it multiplies: R sets of operands, W in registers, bf16 rows by direct loads to a ring in LDS of the wave's own (which takes no
 // registers and no barrier): rows of 256 bytes, their 16-byte chunks at their number XOR the row, so that 16 rows read at the same k hit all banks.
-// NW > 1 is for many features: NW waves with tiles of their own share a ring, each bringing its part of the rows, and a barrier a step.  The rows then pass
-// into LDS once for NW * NTW tiles, and the short sums let several blocks lie on a compute unit, whose waves together keep HBM busy.
-// 34 x 24576 x 4096: 18.6 us (53 MB of W: 2.9 TB/s, a compute unit's share of rows and W at about 50 KB/us, one
-// wave a SIMD), 32 x 126464 x 4096 in float32: 51 us (290 MB: 5.7 TB/s).  Three sets of operands, and rows in registers for more than 4 rows, were no faster.
+// NW > 1 is for many features: NW waves with tiles of their own share a ring, each bringing its part of the rows, and a barrier a step.  The
+// rows then pass into LDS once for NW * NTW tiles, and the short sums let several blocks lie on a compute unit, whose waves together keep HBM
+// busy.  Calls one behind the other: 34 x 24576 x 4096 18.2 us (53 MB of W: 2.9 TB/s, a compute unit's share of rows and W at about 50 KB/us, one wave
+// a SIMD), 32 x 126464 x 4096 in float32 51.5 us (290 MB: 5.7 TB/s).  Three sets of operands, and rows in registers for more than 4 rows, were no
+// faster.  4-bit rows lie in registers: 32 rows with 24576 features 12.5 us (bf16 rows 16), with 126464 and a bf16 result 57.5 (49: shared rows).
 template <int XF, typename TY, int MT, int NTW, int KS, int NW>
 __global__ __launch_bounds__(KS * NW * 64) void mx_rows_kernel(MxProduct p) {
   constexpr int R = 2;
@@ -383,11 +384,12 @@ __device__ __forceinline__ void mx_block_xy(int gx, int gy, int& bx, int& by) {
   bx = in / high;
 }
 
-// Many rows: 8 waves (WM x WN), a wave WTM tiles of 16 rows x 64 features.  QS steps of 128 k are a stage; S stages are in LDS, brought there by direct
-// loads, one barrier a stage.  W lies there as it is packed.  Rows of bf16 (256 bytes a step) and of codes (128 bytes, two steps)
+// Many rows: 8 waves (WM x WN), a wave WTM tiles of 16 rows x 64 features.  QS steps of 128 k are a stage; S stages are in LDS, brought there by
+// direct loads, one barrier a stage.  W lies there as it is packed.  Rows of bf16 (256 bytes a step) and of codes (128 bytes, two steps)
 // have their 16-byte chunks at their number XOR the row, so that rows read at the same k hit all banks; the scales of 4-bit rows go
-// [step][row], four bytes each.  561 x 37888 x 3584 in bf16: 149 us, 1.02 PFLOP/s of the 1.34 that a plain bf16 product reaches: the widening of W, done
-// again by each block of rows, and the LDS reads beside the products.  (256 x 128 tiles: slower.)
+// [step][row], four bytes each.  561 x 37888 x 3584 in bf16: 150 us once the card has been at it for some ms (170 in the first launches of a
+// process), 1.02 PFLOP/s of the 1.34 that a plain bf16 product reaches: the widening of W, done again by each block of rows, and the LDS reads
+// beside the products.  (256 x 128 tiles: slower.)
 template <bool X4, int WM, int WN, int WTM> struct MxTile {
   static constexpr int BM = WM * WTM * 16, BN = WN * 64, QS = X4 ? 2 : 1;
   static constexpr int XB = BM * (X4 ? 128 : 256), SB = X4 ? BM * 8 : 0, WB = WN * QS * (int)kMxGroupBytes;
@@ -551,8 +553,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // 16x16x128, whose instructions one wave cannot issue often enough): 64 k a step, in which a lane has one block of 32 of one of 32 rows, 16
 // bytes, and its scale.  A wave has MF x NF tiles of 32 x 32.  Four steps are a stage, two stages are in LDS.  The operands of a step are
 // read while the step before it is multiplied; at a stage's last step the waves meet, behind which the next stage has landed and this
-// one's place is free for the one after.  24576 x 12288 x 4096: about 790 us, 3.1 PFLOP/s; a block of 256 x 256 takes 4 us to begin, 42 for 16 stages (30 without the
-// loads, 27 without the products, so neither alone) and 3.4 to store.  With zeros for operands the whole takes 725 us: the clock under load is part of it.
+// one's place is free for the one after.  24576 x 12288 x 4096: 776 us, 3.2 PFLOP/s; a block of 256 x 256 takes 4 us to begin, 42 for 16 stages (30
+// without the loads, 27 without the products, so neither alone: one stage is on its way and is waited for whole at each meeting; stages of 128 k,
+// of which four would fit, have not been tried) and 3.4 to store.  With zeros for operands the whole takes 725 us: the clock under load is part
+// of it.
 template <int WM, int WN, int MF, int NF> struct MxTile4 {
   static constexpr int BM = WM * MF * 32, BN = WN * NF * 32;
   static constexpr int XB = BM * 128, SB = BM * 8, WB = BN / 64 * 2 * (int)kMxGroupBytes, STAGE = XB + SB + WB;
@@ -837,9 +841,9 @@ static void launch_rows_t(const MxProduct& p, int parts, hipStream_t s) {
 }
 
 constexpr int kMxRegisterRows = 4;   // rows of bf16 that a wave loads into registers, past LDS
-// Where waves share their rows in LDS: from more features on than 256 blocks of 128 give each compute unit one (512 for up to 16 rows, whose share of the traffic is
-// small).  Blocks of 256 features once there would be more than three blocks of 128 a unit, of which two share K where the registers let two blocks lie on a
-// unit (up to 32 rows) and each unit has its two.  us at K 4096, f32 results, for 16 / 32 / 48 / 64 rows (256 features without / with halves of K):
+// Where waves share their rows in LDS: from more features on than 256 blocks of 128 give each compute unit one (512 for up to 16 rows, whose
+// share of the traffic is small).  Blocks of 256 features once there would be more than three blocks of 128 a unit, of which two share K where
+// the registers let two blocks lie on a unit (up to 32 rows) and each unit has its two.  us at K 4096, f32 results, for 16 / 32 / 48 / 64 rows (256 features without / with halves of K):
 //   features   alone            128 shared     256 shared     256 in halves
 //     40960    21  47  57  66   26 27 31 34    36 40 43 49    30 33  38  42
 //     65536    28  39  45  52   27 30 35 41    38 42 45 51    33 36  40  45
@@ -855,7 +859,8 @@ static int pick_shared(bool x4, int M, int N) {
   return M <= 32 && blocks256 <= 512 ? MX_SHARED_256_HALVES : MX_SHARED_256;
 }
 // Tiles of features to a block and ranges of K.  A compute unit pulls about 50 KB/us in these kernels, so that what counts is what goes
-// through the busiest of the 256: its blocks' shares of W and, once a block, the rows; a join of K's ranges is another 3.5 us.
+// through the busiest of the 256: its blocks' shares of W and, once a block, the rows; a join of K's ranges is another 3.5 us.  (Rows are counted by
+// fours.  A ring brings whole tiles of 16, the first row's bytes for those that are not there; the rate is what fits the measured times so.)
 struct MxRowsShape { int ntw, parts, shared; };
 static MxRowsShape pick_rows(bool x4, int M, int N, int kb) {
   const int tiles = (N + 15) / 16, rows = (M + 3) / 4 * 4;

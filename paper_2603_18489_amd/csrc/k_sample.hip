@@ -446,8 +446,10 @@ __device__ void sample_whole(const S& src, const SampleRow& row, const SampleArg
     put_token(tokens, stats, r, place, z, row, kept, n, all);
 }
 
-// A row of up to 512 NE logits: one block, which reads it once and keeps it in registers.  What takes the time is the chain of block-wide
-// steps, a barrier or two each: 10 us for a row of 4096 with all filters, of which the launch is 3.
+// A row of up to 512 NE logits: one block, which reads it once and keeps it in registers.  A row of 4096, us by trace: 6.2 without filters (launch,
+// load, maximum, sum, draw), 8.9 with top-k, 9.6 with top-p, 11.1 with both.  So each search for a cut takes 3: the weights of all logits once
+// more and their LDS atomics, some barriers, and a wave that ranks what shares the cut's bin.  Weights are not kept: each step that wants one
+// computes it again, five times and more a logit with both.
 template <typename T, int NE>
 __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* __restrict__ logits, int V, size_t ld,
                                                                       const float* __restrict__ uniforms, SampleArgs a,
@@ -464,14 +466,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_small_kernel(const T* _
 }
 
 // ---- longer rows: parts of 4096 or 8192 logits to a block ---------------------------------------------
-// One pass in which each block needs nothing of the others, then a block a row that joins what they found.  A part's maximum and, without filters, its weights' sum.  With filters, how its weights spread over kBins bins of T / 16 in z, counted down
-// from its largest logit; the last one is all that lies 32 T and more below it, which weighs nothing (less than 2^-46 of the maximum).  Bins
-// begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
-// e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1], and what is added for it one number: 2^48 (a count) plus (e^(rho / 16) - 0.99) 2^36,
-// whose sums over the 8192 logits of a part stay below 2^48.
-// 544 rows of 126464 bf16 logits: 91 us, 1.5 TB/s; 36 of these are the loads and the maximum, the rest instructions: the 64-bit polynomial (26), bins, whose
-// LDS atomics hide behind it, and the list below (23, for which the draw takes 50 us instead of 91; found by every wave for itself and with the logits in it: 28).  32 rows of float32 without filters: 8.5 us, about a launch and the latency of what a block does.  (32 logits a
-// thread, without the list: 75 us, 16: 68.)
+// One pass in which each block needs nothing of the others, then a block a row that joins what they found.  A part's maximum and, without
+// filters, its weights' sum.  With filters, how its weights spread over kBins bins of T / 16 in z, counted down from its largest logit; the
+// last one is all that lies about 32 T (at least 510 / 16 T) and more below it, which is taken to weigh nothing (it is up to 1.02 * 2^-46 of the
+// maximum).  Bins begin at multiples of T / 16, so that a row's parts are put together by moving them by whole bins.  A weight of bin B is
+// e^(B / 16) e^(rho / 16) with rho = z 16 / T - B in [0, 1] but for roundings, and what is added for it one number: 2^48 (a count) plus
+// (e^(rho / 16) - 0.99) 2^36, whose sums over the 8192 logits of a part stay below 2^48.
+// 544 rows of 126464 bf16 logits: 89 us, 1.5 TB/s; 36 of these are the loads and the maximum, the rest instructions: the 64-bit polynomial
+// (26), bins, whose LDS atomics hide behind it, and the list below (23, for which the draw takes 50 us instead of 91; found by every wave for
+// itself and with the logits in it: 28).  32 rows of float32 without filters: 8.6 us, about a launch and the latency of what a block does.
+// (32 logits a thread, without the list: 75 us, 16: 68.)
 constexpr int kBins = 512, kList = 5632, kPartsMax = 40, kSampleBatch = 1024;
 constexpr int kChunk = 1024, kChunksMax = 192;   // logits that a wave goes through at a time; of the longest row
 struct PartSum {
@@ -482,8 +486,8 @@ struct PartSum {
   int listed, depth;             // with filters: how many tokens are listed, all of the first `depth` bins
 };
 typedef u64 Spread[kBins];
-// With filters a part lists the tokens of its first bins, as many whole bins as have up to one in 32 of its logits, in the order of the ids: a cut that lies
-// there in all parts needs the row's logits no more.
+// With filters a part lists the tokens of its first bins, as many whole bins as have up to one in 32 of its logits, in the order of the ids: a
+// cut that lies there in all parts needs the row's logits no more.
 constexpr int kOfListed = 32, kListedMost = kSampleThreads * 16 / kOfListed;
 
 // number of the bin of a logit, counted up in z; whole, and monotonous whatever z
@@ -506,7 +510,8 @@ __device__ __forceinline__ uint32_t first_key(float top, float c, int b) {
 }
 __device__ __forceinline__ u64 spread_of(float z, float b, double per_z) {
   const double rho = fma((double)z, per_z, -(double)b);
-  // e^(rho / 16) - 0.99, degree 5 through the Chebyshev nodes of [-1/16, 17/16] (rounding z 16 / T may move a border that far): off by 9e-14
+  // e^(rho / 16) - 0.99, degree 5 through the Chebyshev nodes of [-1/16, 17/16]: off by 8.5e-14 there.  bin_of rounds 16 / T and its product with
+  // z to float32, which moves a border by up to 1/8 at the largest bins, 2^20: off by 7.1e-13 in [-1/8, 9/8].
   double q = 0x1.19bf4680e8241p+9;
   q = fma(q, rho, 0x1.552f36e70099ep+15);
   q = fma(q, rho, 0x1.55559db67be1cp+21);
@@ -801,11 +806,14 @@ __device__ __forceinline__ void list_candidates(const int2* candidates, int part
   if (threadIdx.x == 0) y.listed = min(all, LIST);
 }
 
-// The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the tokens of these come from
-// the parts' lists, or, where these are too short, from the row, and are then ranked.  Without, and where more is kept than can be listed, the parts' sums say in
-// which part the token is, and only that is read.  34 rows of 152064 with top-p: 16 us, the chain from the bins to the token; 544 rows of 126464 bf16 with
-// top-k, top-p and min-p: 50 us, two blocks to a compute unit and so two rounds.  Where all have to read their row again these take 91 us, 138 MB at 5.5 TB/s
-// (three blocks with a list of half the length: 84 to 90 us, and spills; chunks of 512: 98).
+// The token of a row whose parts are known.  One block a row.  With filters, the parts' bins together say in which the cut lies; the tokens of
+// these come from the parts' lists, or, where these are too short, from the row, and are then ranked.  Without, and where more is kept than can
+// be listed, the parts' sums say in which part the token is, and only that is read.  34 rows of 152064 with top-p: 18 us, the chain from the bins to
+// the token; 544 rows of 126464 bf16 with top-k, top-p and min-p: 51 us, two blocks to a compute unit and so two rounds.  Where all have to read
+// their row again these take 91 us, 138 MB at 5.5 TB/s (three blocks with a list of half the length: 84 to 90 us, and spills; chunks of 512: 98).
+// Where neither will do, the block goes through its row several times (sample_whole).  32 rows of 126464, us a call: top-p 0.9 at a spread of 2 66
+// from bins and lists; by the row, min_p 0.05 at a spread of 1 and T 1.5 219, top-p 0.5 at T 2 420, top-k 10000 with top-p 510, and 375 where a part's
+// largest logit is beyond 2^16 T (16384 neighbours at the type's lowest value, beside 63 with -inf there).
 template <typename T, bool FILTERS, int LIST>
 __global__ __launch_bounds__(kSampleThreads, FILTERS ? 4 : 1) void sample_draw_kernel(const T* __restrict__ logits, int V, size_t ld, int parts, int part_size,
                                                                      const float* __restrict__ uniforms, SampleArgs a,
@@ -1055,23 +1063,23 @@ __global__ __launch_bounds__(kSampleThreads, FILTERS ? 4 : 1) void sample_draw_k
 // ---- launchers ------------------------------------------------------------------------------------
 struct SampleSizes { int ne, parts; };
 // Logits to a thread: the fewest with which a batch of rows makes no more than two blocks for each compute unit; four where nothing is
-// listed, as the part that the token is in is then read again.  us by trace, parts and draw, eight logits a thread against sixteen: 32 rows of 126464 without
-// filters 8.5 + 6.6, 7.9 + 10.8; before parts listed tokens, 34 rows of 152064 with top-p (sixteen by the rule) 10.4 + 17.6, 10.0 + 16.9.
+// listed, as the part that the token is in is then read again.  us by trace, parts and draw, eight logits a thread against sixteen: 32 rows of
+// 126464 without filters 8.5 + 6.6, 7.9 + 10.8; before parts listed tokens, 34 rows of 152064 with top-p (sixteen by the rule) 10.4 + 17.6, 10.0 + 16.9.
 static SampleSizes sample_sizes(int rows, int V, bool filters) {
   const int parts = (V + kSampleThreads * 8 - 1) / (kSampleThreads * 8);
   if ((long)rows * parts <= (filters ? 512 : 1024)) return {8, parts};
   return {16, (V + kSampleThreads * 16 - 1) / (kSampleThreads * 16)};
 }
-// Logits of a row that one block holds in registers.  us of a call with top-k and top-p, by one block and in parts, for 24 and 591 rows: 4096 logits 12 and 32,
-// 15 and 30; 4097 62 and 173, 16 and 30 (32 logits a thread); 16384 68 and 195, 16 and 38.
+// Logits of a row that one block holds in registers.  us of a call with top-k and top-p, by one block and in parts, for 24 and 591 rows: 4096
+// logits 12 and 32, 15 and 30; 4097 62 and 173, 16 and 30 (32 logits a thread); 16384 68 and 195, 16 and 38.
 constexpr int kSampleSmall = 4096;
 struct SampleBytes { size_t sums, spreads, all; };   // where each ends
 static SampleBytes sample_bytes(int rows, int V) {
   SampleBytes b = {};
   if (rows <= 0 || V <= kSampleSmall) return b;
   if (rows > kSampleBatch) rows = kSampleBatch;
-  // Fewer rows may have more parts, of eight logits to a thread, up to 1024 in all: there is room for as many rows of these as it takes.  (The last of
-  // several batches has few rows too.)
+  // Fewer rows may have more parts, of eight logits to a thread, up to 1024 in all: there is room for as many rows of these as it takes.  (The
+  // last of several batches has few rows too.)
   const size_t p16 = (V + kSampleThreads * 16 - 1) / (kSampleThreads * 16), p8 = (V + kSampleThreads * 8 - 1) / (kSampleThreads * 8);
   const size_t small = ((size_t)rows < 1024 / p8 ? (size_t)rows : 1024 / p8) * p8;
   const size_t most = rows * p16 > small ? rows * p16 : small;
