@@ -347,8 +347,9 @@ int ec_row_entropy_noalloc(const float *logits, int32_t rows, int32_t vocab, siz
 /* Types of the tensors that the calls below take.  EC_T_MXFP4 is microscaled 4-bit floating point: 32 consecutive values of a
  * row share a scale 2^(s - 127), s one byte (255: the block is NaN), and a value is a 4-bit e2m1 code (1 sign, 2 exponent bits with
  * bias 1, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) times the scale.  Codes uint8 [rows, k/2], an even k in the low four bits;
- * scales uint8 [rows, k/32]; both without gaps between rows. */
-enum { EC_T_F32 = 0, EC_T_BF16 = 1, EC_T_MXFP4 = 2 };
+ * scales uint8 [rows, k/32]; both without gaps between rows.  EC_T_E4M3 is 8-bit floating point (1 sign, 4 exponent bits with bias 7, 3
+ * mantissa bits, no infinities), as an ec_kv_cache keeps it. */
+enum { EC_T_F32 = 0, EC_T_BF16 = 1, EC_T_MXFP4 = 2, EC_T_E4M3 = 3 };
 
 /* How ec_row_sample draws.  temperature: finite, >= 0; 0 takes the most probable token (top_k 1 at temperature 1).  top_k: 0 or
  * vocab and more: all.  top_p in (0, 1], 1: all.  min_p in [0, 1], 0: all.
@@ -422,6 +423,91 @@ int ec_mx_linear(const void *x, const uint8_t *x_scales, int32_t x_type, int64_t
 /* Which blocks ec_mx_linear cuts a product into (test and diagnosis aid; pure host computation): shape = {rows of a block, features of
  * a block, ranges that K is split into}.  Errors: EC_ERR_ARG. */
 int ec_debug_mx_blocks(int32_t x_type, int64_t rows, int32_t n, int32_t k, int32_t shape[3] /*HOST*/);
+
+/* Rotary positions.  Pair i of dim/2 of a head turns by the angle 2 pi position turns[i]:
+ *   (x, y) -> amplitude (x cos - y sin, x sin + y cos);  inverse != 0: by the angle's negative, which is the transposed rotation and so
+ * what takes a gradient back.  A pair is the components i and i + dim/2 (what a step does itself), or 2 i and 2 i + 1 where interleaved != 0;
+ * components from dim on are left as they are.  The angle is computed in 64 bits and the whole turns dropped there; cos and sin are float32
+ * (1e-7), the result is rounded to its type once.
+ *
+ * ec_rotary_frequencies writes turns[i] = theta_i / 2 pi with theta_i = base^(-2 i / dim), and for a longer context than a model learned:
+ * original 0: theta_i / factor; otherwise, with r_i the turns of pair i over `original` positions, a share clamp((r_i - low) / (high - low), 0, 1)
+ * of theta_i is kept and the rest divided by factor.  Pure host computation.  Errors: EC_ERR_ARG (dim odd or outside [2, 512], base not
+ * positive, factor below 1, low not below high, anything not finite). */
+typedef struct {
+  int32_t dim;
+  double base, factor, original, low, high;
+} ec_rotary_cfg;
+int ec_rotary_frequencies(const ec_rotary_cfg *cfg, double *turns /*HOST [dim/2]*/);
+
+/*  x, out     DEVICE [rows, heads, head_dim] of `type` (EC_T_F32 or EC_T_BF16), aligned to its elements; element (r, h, c) is at r ld +
+ *             h ld_head + c.  out's elements must not meet; it may be x itself (with its strides), or must not overlap it
+ *  rows       0 .. 2^24; heads 1 .. 1024; head_dim 2 .. 512; dim even, at most head_dim
+ *  positions  DEVICE int32 [rows]; any value
+ *  turns      DEVICE float64 [dim/2]
+ * Strides that are multiples of 16 bytes cost least.  Enqueues on hip_stream and returns without synchronising; may be captured.
+ * Errors: EC_ERR_ARG, EC_ERR_HIP. */
+int ec_rotary(const void *x, int32_t type, int64_t rows, int32_t heads, int32_t head_dim, size_t ld, size_t ld_head,
+              const int32_t *positions, const double *turns, int32_t dim, int32_t interleaved, float amplitude, int32_t inverse, void *out,
+              size_t out_ld, size_t out_ld_head, void *hip_stream);
+
+/* A paged cache of keys and values of one layer, for sequences that come and go and may share pages.  It has `pages` pages of `page` tokens
+ * (32, 64, 128 or 256) of all kv heads; token t of page p is slot p * page + t.  Under EC_T_E4M3 each token's head is kept as 8-bit codes and a
+ * power of two, the least 2^e with e >= -126 that leaves its largest magnitude at 448 or less; a value goes to the nearest code, ties to the
+ * even one.  Under EC_T_BF16 values are rounded to bfloat16.  A token's head that holds an infinity, a NaN or a value that is rounded to
+ * 2^128 is kept as NaN throughout.  The layout inside is the library's.
+ *  data       DEVICE, 256-byte aligned, ec_kv_bytes() (0 for arguments outside the limits); BORROWED.  Slots that have not been written
+ *             hold whatever the memory held (zeros read as zeros)
+ *  pages      1 or more, pages * page < 2^31; kv_heads 1 .. 1024; head_dim 64 or 128 */
+typedef struct {
+  void *data;
+  int32_t type, pages, page, kv_heads, head_dim;
+} ec_kv_cache;
+size_t ec_kv_bytes(const ec_kv_cache *cache);
+
+/* Keys and values of some tokens into the cache, and out of it.  Out, every value is exact in float32 (bfloat16: but for magnitudes below 2^-126).
+ *  k, v       DEVICE [rows, kv_heads, head_dim] of `type` (EC_T_F32 or EC_T_BF16), aligned to their elements, strides as ec_rotary's; what
+ *             is written must not overlap anything.  Strides that are multiples of 16 bytes cost least
+ *  rows       0 .. 2^20
+ *  slots      DEVICE int32 [rows], in any order.  Written: a row whose slot is not in the cache (-1 for padding) is left out, and of rows that
+ *             name the same slot the last one is stored.  Read: a slot that is not in the cache reads zeros
+ * Enqueue on hip_stream and return without synchronising; may be captured.  Errors: EC_ERR_ARG, EC_ERR_HIP. */
+int ec_kv_write(const ec_kv_cache *cache, const void *k, const void *v, int32_t type, int32_t rows, size_t k_ld, size_t k_ld_head,
+                size_t v_ld, size_t v_ld_head, const int32_t *slots, void *hip_stream);
+int ec_kv_read(const ec_kv_cache *cache, const int32_t *slots, int32_t rows, void *k, void *v, int32_t type, size_t k_ld,
+               size_t k_ld_head, size_t v_ld, size_t v_ld_head, void *hip_stream);
+
+/* Attention of a batch of sequences over the cache.  Sequence b has the rows starts[b] .. starts[b + 1] - 1 of q (starts NULL: max_rows rows
+ * each, one sequence after the other; then rows = seqs * max_rows) and lengths[b] keys: key j is token j % page of page table[b][j / page].
+ * All sequences see the first prefix_len tokens of the pages prefix[] before their own, which are read once for all of them.
+ *   out[r, h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q[r, h] . k_j),  over the prefix and the sequence's keys; of these, under causal
+ * != 0, row i of n sees the keys before lengths[b] - n + i + 1.  Heads h of a group of heads / kv_heads share kv head h / group.  A row that
+ * sees no key gets zeros, and keys that it does not see are without effect, NaN among them.  Probabilities are rounded to bfloat16 once,
+ * everything else is held in float32 and the result rounded to bfloat16.
+ * Kept inside the buffers whatever the tables hold: starts are clamped to [0, rows], a sequence's rows beyond max_rows and rows of no sequence are
+ * left as they were, lengths are clamped to [0, max_keys], and the tokens of a page outside [0, pages) are not seen. */
+typedef struct {
+  int32_t rows, heads;           /* 0 .. 2^20; a multiple of kv_heads, at most 1024 */
+  int32_t seqs;                  /* 1 .. 65535 */
+  int32_t max_rows, max_keys;    /* most of a sequence; what the launches are sized by: the closer, the cheaper */
+  int32_t table_pages;           /* pages of a sequence in the table: max_keys <= table_pages * page */
+  int32_t prefix_pages, prefix_len;
+  int32_t causal;
+  float scale;                   /* positive */
+  size_t table_ld;               /* row stride of the table */
+} ec_kv_attention_cfg;
+/*  cfg        HOST, read before the call returns
+ *  q, out     DEVICE bfloat16 [rows, heads, head_dim], 16-byte aligned, strides (as ec_rotary's) multiples of 8 elements; out must not overlap q
+ *  table      DEVICE int32 [seqs, table_pages]; lengths DEVICE int32 [seqs]; starts DEVICE int32 [seqs + 1] or NULL; prefix DEVICE int32
+ *             [prefix_pages] (may be NULL for prefix_len 0)
+ *  workspace  DEVICE, 256-byte aligned, >= ec_kv_attention_workspace_bytes(cache, cfg) (0 for many sizes, and for arguments outside the limits;
+ *             cache->data is not looked at); BORROWED for the call: calls that overlap in time, and captured graphs that may run side by
+ *             side, need one each
+ * Enqueues on hip_stream and returns without synchronising; may be captured.  Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP. */
+size_t ec_kv_attention_workspace_bytes(const ec_kv_cache *cache, const ec_kv_attention_cfg *cfg);
+int ec_kv_attention(const ec_kv_cache *cache, const ec_kv_attention_cfg *cfg, const void *q, size_t q_ld, size_t q_ld_head,
+                    const int32_t *table, const int32_t *lengths, const int32_t *starts, const int32_t *prefix, void *out, size_t out_ld,
+                    size_t out_ld_head, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Frees host-side state only; never frees weights or workspace.  NULL is allowed. */
 void ec_destroy(ec_ctx *ctx);

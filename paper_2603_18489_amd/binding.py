@@ -24,7 +24,7 @@ EC_ERR_HOST_MEMORY = -6
 EC_ERR_NONFINITE = -7
 (EC_K_EMBED, EC_K_NORM, EC_K_QKV, EC_K_ROPE_KV, EC_K_ATTN, EC_K_OPROJ, EC_K_GATEUP, EC_K_SWIGLU,
  EC_K_DOWN, EC_K_LMHEAD, EC_K_VOCAB_REDUCE, EC_K_DECIDE, EC_K_COUNT) = range(13)
-EC_T_F32, EC_T_BF16, EC_T_MXFP4 = 0, 1, 2
+EC_T_F32, EC_T_BF16, EC_T_MXFP4, EC_T_E4M3 = 0, 1, 2, 3
 KERNEL_CLASS_NAMES = ["embed", "norm", "qkv", "rope_kv", "attn", "oproj", "gateup", "swiglu",
                       "down", "lmhead", "vocab_reduce", "decide"]
 (EC_DBG_LOGITS, EC_DBG_KCACHE, EC_DBG_VCACHE, EC_DBG_X, EC_DBG_MASKED, EC_DBG_HIST, EC_DBG_ROWS,
@@ -36,7 +36,9 @@ EXPORTS = ["ec_workspace_bytes", "ec_init", "ec_reset", "ec_step", "ec_step_forc
            "ec_debug_mx_blocks", "ec_destroy", "ec_strerror", "ec_last_error",
            "ec_row_entropy_workspace_bytes", "ec_row_entropy", "ec_row_entropy_noalloc",
            "ec_row_sample_workspace_bytes", "ec_row_sample", "ec_mx_quantize", "ec_mx_dequantize",
-           "ec_mx_packed_bytes", "ec_mx_pack", "ec_mx_linear_workspace_bytes", "ec_mx_linear"]
+           "ec_mx_packed_bytes", "ec_mx_pack", "ec_mx_linear_workspace_bytes", "ec_mx_linear",
+           "ec_rotary_frequencies", "ec_rotary", "ec_kv_bytes", "ec_kv_write", "ec_kv_read",
+           "ec_kv_attention_workspace_bytes", "ec_kv_attention"]
 
 
 class ec_model_cfg(C.Structure):
@@ -85,6 +87,19 @@ class ec_step_result(C.Structure):
 
 class ec_sample_cfg(C.Structure):
     _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
+
+
+class ec_rotary_cfg(C.Structure):
+    _fields_ = [("dim", C.c_int32)] + [(n, C.c_double) for n in ("base", "factor", "original", "low", "high")]
+
+
+class ec_kv_cache(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int32) for n in ("type", "pages", "page", "kv_heads", "head_dim")]
+
+
+class ec_kv_attention_cfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "heads", "seqs", "max_rows", "max_keys", "table_pages", "prefix_pages",
+                                         "prefix_len", "causal")] + [("scale", C.c_float), ("table_ld", C.c_size_t)]
 
 
 class ec_gen_stats(C.Structure):
@@ -168,6 +183,22 @@ def load_library() -> C.CDLL:
     lib.ec_mx_linear.restype = C.c_int
     lib.ec_mx_linear.argtypes = [vp, vp, C.c_int32, C.c_int64, C.c_size_t, vp, C.c_int32, C.c_int32, vp, C.c_int32,
                                  C.c_size_t, vp, C.c_size_t, vp]
+    lib.ec_rotary_frequencies.restype = C.c_int
+    lib.ec_rotary_frequencies.argtypes = [C.POINTER(ec_rotary_cfg), vp]
+    lib.ec_rotary.restype = C.c_int
+    lib.ec_rotary.argtypes = [vp, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_size_t, C.c_size_t, vp, vp, C.c_int32, C.c_int32,
+                              C.c_float, C.c_int32, vp, C.c_size_t, C.c_size_t, vp]
+    lib.ec_kv_bytes.restype = C.c_size_t
+    lib.ec_kv_bytes.argtypes = [C.POINTER(ec_kv_cache)]
+    lib.ec_kv_write.restype = C.c_int
+    lib.ec_kv_write.argtypes = [C.POINTER(ec_kv_cache), vp, vp, C.c_int32, C.c_int32] + [C.c_size_t] * 4 + [vp, vp]
+    lib.ec_kv_read.restype = C.c_int
+    lib.ec_kv_read.argtypes = [C.POINTER(ec_kv_cache), vp, C.c_int32, vp, vp, C.c_int32] + [C.c_size_t] * 4 + [vp]
+    lib.ec_kv_attention_workspace_bytes.restype = C.c_size_t
+    lib.ec_kv_attention_workspace_bytes.argtypes = [C.POINTER(ec_kv_cache), C.POINTER(ec_kv_attention_cfg)]
+    lib.ec_kv_attention.restype = C.c_int
+    lib.ec_kv_attention.argtypes = [C.POINTER(ec_kv_cache), C.POINTER(ec_kv_attention_cfg), vp, C.c_size_t, C.c_size_t, vp, vp, vp, vp,
+                                    vp, C.c_size_t, C.c_size_t, vp, C.c_size_t, vp]
     lib.ec_destroy.restype = None
     lib.ec_destroy.argtypes = [vp]
     lib.ec_strerror.restype = C.c_char_p
@@ -511,6 +542,188 @@ def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
         ws, at = _workspace(torch, size, w.data.device)
         _done(lib, lib.ec_mx_linear(tensors[0].data_ptr(), x_scales, x_kind, rows, ld, w.data.data_ptr(), w.n, k,
                                     y.data_ptr(), kind, w.n, at, size, raw))
+        return y
+    return _place(stream, call, *tensors)
+
+
+def _heads_of(x, what: str):
+    """rows, heads, components and the two strides of a tensor [rows, heads, head_dim] whose components are next to each other"""
+    _need(x.dim() == 3, f"{what} must be [rows, heads, head_dim]")
+    rows, heads, dim = x.shape
+    _need(max(rows, heads, dim) <= _INT_MAX, "at most 2^31 - 1 rows, heads and components")
+    ld, ld_head, one = x.stride()
+    _need(one == 1 or dim <= 1, "the components of a head must be next to each other")
+    return rows, heads, dim, ld if rows > 1 else 0, ld_head if heads > 1 else 0
+
+
+def _ints(t, size, what: str):
+    import torch
+    _need(t.dtype == torch.int32 and tuple(t.shape) == size and t.is_contiguous(), f"{what} must be contiguous int32 {list(size)}")
+
+
+class RotaryPlan(NamedTuple):
+    """How rotary() turns rows: turns (float64 [dim/2], on the GPU) of each pair a position."""
+    turns: object
+    dim: int
+    interleaved: bool
+    amplitude: float
+
+
+def rotary_plan(dim: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0, original: float = 0.0,
+                low: float = 1.0, high: float = 32.0, amplitude: float = 1.0, device="cuda") -> RotaryPlan:
+    """ec_rotary_frequencies: theta_i = base^(-2 i / dim) for the first `dim` components of a head, divided by `factor` for a longer
+    context - all of them (original 0), or those that turn fewer than `high` times over `original` positions (wholly below `low` turns)."""
+    import torch
+    _need(0 < dim <= _INT_MAX, "dim must be positive")
+    lib = _lib or load_library()
+    turns = np.zeros(dim // 2 + 1)
+    _done(lib, lib.ec_rotary_frequencies(C.byref(ec_rotary_cfg(dim, base, factor, original, low, high)), turns.ctypes.data))
+    return RotaryPlan(torch.from_numpy(turns[:-1].copy()).to(device), dim, bool(interleaved), float(amplitude))
+
+
+def rotary(x, positions, plan: RotaryPlan, inverse: bool = False, out=None, stream=None):
+    """ec_rotary: a float32 or bfloat16 CUDA tensor [rows, heads, head_dim] (queries and keys beside each other, say) turned by the rows'
+    positions (int32 [rows]).  `out` may be x itself.  The result carries no gradient, whatever x requires: rotary(gradient, positions, plan,
+    inverse=True) is x's."""
+    import torch
+    kind = _plain_type(x.dtype)
+    rows, heads, dim, ld, ld_head = _heads_of(x, "x")
+    _ints(positions, (rows,), "positions")
+    _need(plan.turns.dtype == torch.float64 and plan.turns.is_contiguous() and tuple(plan.turns.shape) == (plan.dim // 2,),
+          "turns must be contiguous float64 [dim/2], as rotary_plan makes them")
+    if out is not None:
+        _need(out.dtype == x.dtype and out.shape == x.shape, "out must have x's shape and type")
+    lib = _lib or load_library()
+
+    def call(raw):
+        y = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device) if out is None else out
+        _, _, _, to, to_head = _heads_of(y, "out")
+        _done(lib, lib.ec_rotary(x.data_ptr(), kind, rows, heads, dim, ld, ld_head, positions.data_ptr(), plan.turns.data_ptr(), plan.dim,
+                                 plan.interleaved, plan.amplitude, inverse, y.data_ptr(), to, to_head, raw))
+        return y
+    return _place(stream, call, x, positions, plan.turns, *(() if out is None else (out,)))
+
+
+class KvCache(NamedTuple):
+    """A paged cache of keys and values of one layer (ec_kv_cache): `data` uint8 on the GPU, laid out by the library; token t of page p is
+    slot p * page + t."""
+    data: object
+    kind: int
+    pages: int
+    page: int
+    kv_heads: int
+    head_dim: int
+
+
+def kv_cache(pages: int, kv_heads: int, head_dim: int, page: int = 64, dtype=None, device="cuda") -> KvCache:
+    """A cache of zeros for pages * page tokens, in e4m3 with a power of two to a token and head (torch.float8_e4m3fn, the default) or in
+    torch.bfloat16."""
+    import torch
+    _need(dtype in (None, torch.float8_e4m3fn, torch.bfloat16), "a cache is float8_e4m3fn or bfloat16")
+    _need(max(pages, kv_heads, head_dim, page) <= _INT_MAX, "at most 2^31 - 1 tokens")
+    lib = _lib or load_library()
+    kind = EC_T_BF16 if dtype == torch.bfloat16 else EC_T_E4M3
+    size = lib.ec_kv_bytes(C.byref(ec_kv_cache(None, kind, pages, page, kv_heads, head_dim)))
+    _need(size > 0, "page must be 32, 64, 128 or 256, head_dim 64 or 128, kv_heads at most 1024, and the tokens fewer than 2^31")
+    return KvCache(torch.zeros((size,), dtype=torch.uint8, device=device), kind, pages, page, kv_heads, head_dim)
+
+
+def _cache_struct(lib, cache: KvCache):
+    import torch
+    c = ec_kv_cache(cache.data.data_ptr() or None, cache.kind, cache.pages, cache.page, cache.kv_heads, cache.head_dim)
+    _need(cache.data.dtype == torch.uint8 and cache.data.is_contiguous() and cache.data.numel() >= max(lib.ec_kv_bytes(C.byref(c)), 1),
+          "data is not a cache of kv_cache")
+    return c
+
+
+def kv_write(cache: KvCache, k, v, slots, stream=None) -> None:
+    """ec_kv_write: float32 or bfloat16 CUDA tensors [rows, kv_heads, head_dim] into the slots (int32 [rows]) of a cache.  A row whose slot is
+    not in the cache (-1) is left out; of rows that name the same slot the last one is stored."""
+    kind = _plain_type(k.dtype)
+    rows, heads, dim, k_ld, k_head = _heads_of(k, "k")
+    _need(v.dtype == k.dtype and v.shape == k.shape, "v must have k's shape and type")
+    _, _, _, v_ld, v_head = _heads_of(v, "v")
+    _need((heads, dim) == (cache.kv_heads, cache.head_dim), "k and v have other heads than the cache")
+    _ints(slots, (rows,), "slots")
+    lib = _lib or load_library()
+
+    def call(raw):
+        c = _cache_struct(lib, cache)
+        _done(lib, lib.ec_kv_write(C.byref(c), k.data_ptr(), v.data_ptr(), kind, rows, k_ld, k_head, v_ld, v_head, slots.data_ptr(), raw))
+    return _place(stream, call, cache.data, k, v, slots)
+
+
+def kv_read(cache: KvCache, slots, dtype=None, stream=None):
+    """ec_kv_read: keys and values [rows, kv_heads, head_dim] of the slots (int32 [rows]), bfloat16 (the default) or float32.  A slot that is
+    not in the cache reads zeros."""
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    kind = _plain_type(dtype)
+    _need(slots.dim() == 1, "slots must be contiguous int32 [rows]")
+    rows = slots.shape[0]
+    _ints(slots, (rows,), "slots")
+    _need(rows <= _INT_MAX, "at most 2^31 - 1 rows")
+    lib = _lib or load_library()
+
+    def call(raw):
+        c = _cache_struct(lib, cache)
+        k, v = (torch.empty((rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.data.device) for _ in range(2))
+        head, ld = cache.head_dim, cache.kv_heads * cache.head_dim
+        _done(lib, lib.ec_kv_read(C.byref(c), slots.data_ptr(), rows, k.data_ptr(), v.data_ptr(), kind, ld, head, ld, head, raw))
+        return k, v
+    return _place(stream, call, cache.data, slots)
+
+
+def kv_attention(q, cache: KvCache, table, lengths, starts=None, max_rows: Optional[int] = None, max_keys: Optional[int] = None,
+                 prefix=None, prefix_len: int = 0, causal: bool = False, scale: Optional[float] = None, out=None, stream=None):
+    """ec_kv_attention: bfloat16 queries [rows, heads, head_dim] (strides multiples of 8) of a batch of sequences over a cache.  Sequence b has
+    the pages table[b] (int32 [seqs, pages]), lengths[b] keys (int32 [seqs]) and the rows starts[b] .. starts[b + 1] - 1 (int32 [seqs + 1];
+    without it as many rows each).  prefix: pages (int32) whose first prefix_len tokens all sequences see before their own.  causal: row i of n
+    sees its sequence's keys before lengths[b] - n + i + 1.  max_rows, max_keys: the most of any sequence, where that is known on
+    the host to be less than all rows and the whole table; what is beyond is not computed.  scale: 1 / sqrt(head_dim) by default.  Without `out`
+    the rows of no sequence are zeros; with it they are left as they were.  No gradients."""
+    import torch
+    _need(q.dtype == torch.bfloat16, "q must be bfloat16")
+    rows, heads, dim, ld, ld_head = _heads_of(q, "q")
+    _need(dim == cache.head_dim, "q has another head_dim than the cache")
+    _need(table.dim() == 2 and table.dtype == torch.int32 and (table.shape[1] <= 1 or table.stride(1) == 1), "table must be int32 [seqs, pages]")
+    seqs, width = table.shape
+    _need(max(seqs, width) <= _INT_MAX, "at most 2^31 - 1 sequences and pages")
+    _ints(lengths, (seqs,), "lengths")
+    tensors = [cache.data, q, table, lengths]
+    if starts is not None:
+        _ints(starts, (seqs + 1,), "starts")
+        tensors.append(starts)
+    else:
+        _need(seqs > 0 and rows % seqs == 0 and max_rows in (None, rows // seqs), "without starts every sequence has rows / seqs rows")
+        max_rows = rows // seqs
+    prefix_pages = 0
+    if prefix is not None:
+        _need(prefix.dim() == 1, "prefix must be contiguous int32 [pages]")
+        prefix_pages = prefix.shape[0]
+        _ints(prefix, (prefix_pages,), "prefix")
+        tensors.append(prefix)
+    if out is not None:
+        _need(out.dtype == q.dtype and out.shape == q.shape, "out must have q's shape and type")
+        tensors.append(out)
+    max_rows = rows if max_rows is None else min(max_rows, rows)
+    max_keys = min(width * cache.page, _INT_MAX) if max_keys is None else max_keys
+    _need(max(prefix_len, prefix_pages, max_keys) <= _INT_MAX and min(prefix_len, max_rows, max_keys) >= 0, "lengths must be in [0, 2^31)")
+    lib = _lib or load_library()
+    cfg = ec_kv_attention_cfg(rows, heads, seqs, max_rows, max_keys, width, prefix_pages, prefix_len, causal,
+                              dim ** -0.5 if scale is None else scale, table.stride(0) if seqs > 1 else width)
+
+    def call(raw):
+        c = _cache_struct(lib, cache)
+        y = out
+        if y is None:
+            y = (torch.empty if starts is None else torch.zeros)((rows, heads, dim), dtype=q.dtype, device=q.device)
+        _, _, _, to, to_head = _heads_of(y, "out")
+        size = lib.ec_kv_attention_workspace_bytes(C.byref(c), C.byref(cfg))
+        ws, at = _workspace(torch, size, q.device)
+        _done(lib, lib.ec_kv_attention(C.byref(c), C.byref(cfg), q.data_ptr(), ld, ld_head, table.data_ptr(), lengths.data_ptr(),
+                                       None if starts is None else starts.data_ptr(), prefix.data_ptr() if prefix_pages else None,
+                                       y.data_ptr(), to, to_head, at, size, raw))
         return y
     return _place(stream, call, *tensors)
 

@@ -309,6 +309,40 @@ void mx_linear_blocks(bool x4, long M, int N, int kb, int32_t shape[3]);   // ro
 void launch_mx_linear(const void* x, const uint8_t* x_scales, long M, size_t ld, const uint8_t* packed, int N, int kb, void* y,
                       bool y_bf16, size_t ldy, void* workspace, hipStream_t s);
 
+// rotary positions (k_rotary.hip); strides in elements
+void launch_rotary(const void* x, bool bf16, long rows, int heads, int head_dim, size_t ld, size_t ld_head, const int* positions,
+                   const double* turns, int dim, bool interleaved, float amplitude, bool inverse, void* out, size_t out_ld,
+                   size_t out_ld_head, hipStream_t s);
+
+// paged cache of keys and values (k_kv.h, k_kv.hip, k_kv_attn.hip)
+struct KvCache {
+  uint8_t* data;
+  int pages, page, kv_heads, head_dim;
+  bool e4m3;
+};
+// bytes of the codes, behind which the scales are: 64 bytes to 32 tokens of a head
+inline size_t kv_code_bytes(const KvCache& c) {
+  return (size_t)c.pages * c.page * c.kv_heads * c.head_dim * (c.e4m3 ? 2 : 4);
+}
+inline size_t kv_bytes(const KvCache& c) { return kv_code_bytes(c) + (size_t)c.pages * c.page * c.kv_heads * 2; }
+// ld: row and head strides of k, of v
+void launch_kv_write(const KvCache& c, const void* k, const void* v, bool bf16, int rows, const size_t (&ld)[4], const int* slots,
+                     hipStream_t s);
+void launch_kv_read(const KvCache& c, void* k, void* v, bool bf16, int rows, const size_t (&ld)[4], const int* slots, hipStream_t s);
+// What ec_kv_attention is asked for, as ec.h describes it; sizes are checked by the caller.
+struct KvAttention {
+  const bf16_t* q; size_t q_ld, q_head;
+  bf16_t* out; size_t out_ld, out_head;
+  int rows, heads, seqs, max_rows, max_keys;
+  const int *table, *lengths, *starts;
+  int width; size_t table_ld;
+  const int* prefix; int prefix_len;
+  bool causal;
+  float scale;
+};
+size_t kv_attention_workspace(const KvCache& c, const KvAttention& a);
+void launch_kv_attention(const KvCache& c, const KvAttention& a, void* workspace, hipStream_t s);
+
 void launch_decide(const DecideArgs& a, int B, hipStream_t s);
 void launch_init_state(int* x, uint8_t* masked, int* hist, DevState* st, const int* prompt_dev,
                        int P, int N, int mask_id, hipStream_t s);

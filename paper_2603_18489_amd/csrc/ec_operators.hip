@@ -1,8 +1,7 @@
 // Entry points of the operators around a step: tokens drawn from rows of logits, matrices in microscaled 4-bit floating point.
 #include <cmath>
-#include <string>
 
-#include "ec_internal.h"
+#include "ec_operators.h"
 
 using namespace ec;
 
@@ -14,25 +13,6 @@ constexpr int kMxKMax = 131072;
 constexpr int64_t kMxRowsMax = 1 << 24;   // to and from 4 bits
 constexpr int64_t kMxLinearRowsMax = 1 << 19;
 constexpr int kMxLinearColsMax = 1 << 20;
-
-int op_fail(int code, const char* msg) {
-  set_global_error(msg);
-  return code;
-}
-// what the launches left behind
-int op_done(const char* what) {
-  const hipError_t e = hipGetLastError();
-  if (e == hipSuccess) return EC_OK;
-  try {
-    set_global_error((std::string(what) + ": " + hipGetErrorString(e)).c_str());
-  } catch (...) {
-    set_global_error(what);
-  }
-  return EC_ERR_HIP;
-}
-bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
-bool plain_type(int32_t t) { return t == EC_T_F32 || t == EC_T_BF16; }
-size_t type_bytes(int32_t t) { return t == EC_T_F32 ? 4 : 2; }
 
 int check_mx(const uint8_t* codes, const uint8_t* scales, int32_t k) {
   if (!codes || !scales) return op_fail(EC_ERR_ARG, "codes and scales must not be NULL");

@@ -1,0 +1,114 @@
+// Rotary positions: pairs of a head's components turned by an angle that grows with the row's position.
+//
+// Pair i of dim/2 at position p turns by a = 2 pi p turns[i]:  (x, y) -> A (x cos a - y sin a, x sin a + y cos a), with -a for the
+// inverse, which is the transposed rotation and so the gradient's.  The whole turns are dropped in 64 bits, where p turns[i] is exact
+// to 2^-53 of itself: at position 2^20 and a turn in 6 positions the angle is off by 2^-33.
+#include "ec_internal.h"
+
+namespace ec {
+
+namespace {
+
+// cos and sin of 2 pi t.  t less its nearest quarter, exactly, leaves at most an eighth of a turn, y in [-pi/4, pi/4]; Taylor's series to
+// y^9 and y^10 are off by less than 2e-9 there, below the rounding of float32 (6e-8).
+__device__ __forceinline__ float2 cos_sin_of_turns(double t) {
+  const double quarters = __builtin_rint(t * 4.0);
+  const float y = (float)((t - 0.25 * quarters) * 6.283185307179586);
+  const int q = (int)(quarters - 4.0 * __builtin_floor(quarters * 0.25));
+  const float z = y * y;
+  const float s = y * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), 1.f);
+  const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800, 1.f / 40320), -1.f / 720), 1.f / 24), -0.5f), 1.f);
+  const float a = q & 1 ? s : c, b = q & 1 ? c : s;
+  return make_float2(q == 1 || q == 2 ? -a : a, q == 2 || q == 3 ? -b : b);
+}
+
+template <typename T, int N> struct alignas(sizeof(T) * N) Words { T v[N]; };
+
+}  // namespace
+
+struct RotaryArgs {
+  const void* x; void* out;
+  size_t ld, ld_head, out_ld, out_ld_head;
+  long rows;
+  int heads, head_dim, dim;
+  const int* positions; const double* turns;
+  float amplitude, sign;   // sign: -1 for the inverse
+};
+
+// A block takes RB rows with all their heads: first the rows' cosines and sines into LDS, once for all heads, then the pairs, V of them to
+// a thread at a time (V elements of each half, or 2 V neighbours).
+template <typename T, int V, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int RB) {
+  extern __shared__ float2 cs[];   // [RB][dim/2]
+  const int half = a.dim >> 1, per_head = half / V, per_row = a.heads * per_head;
+  const long row0 = (long)blockIdx.x * RB;
+  const int n = (int)min((long)RB, a.rows - row0);
+  for (int i = threadIdx.x; i < n * half; i += 256) {
+    const int r = i / half;
+    const float2 v = cos_sin_of_turns((double)a.positions[row0 + r] * a.turns[i - r * half]);
+    cs[i] = make_float2(v.x * a.amplitude, v.y * a.amplitude * a.sign);
+  }
+  __syncthreads();
+  typedef Words<T, V> W;
+  for (int i = threadIdx.x; i < n * per_row; i += 256) {
+    const int r = i / per_row, j = i - r * per_row, head = j / per_head, p = (j - head * per_head) * V;
+    const size_t at = (size_t)(row0 + r) * a.ld + (size_t)head * a.ld_head;
+    const size_t to = (size_t)(row0 + r) * a.out_ld + (size_t)head * a.out_ld_head;
+    const int c0 = INTERLEAVED ? 2 * p : p, c1 = INTERLEAVED ? 2 * p + V : p + half;
+    alignas(16) T v[2 * V];
+    *(W*)v = *(const W*)((const T*)a.x + at + c0);
+    *(W*)(v + V) = *(const W*)((const T*)a.x + at + c1);
+    const float2* f = cs + r * half + p;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      T &s = v[INTERLEAVED ? 2 * k : k], &t = v[INTERLEAVED ? 2 * k + 1 : k + V];
+      const float x = load_f32(&s), y = load_f32(&t);
+      store_f32(&s, fmaf(x, f[k].x, -(y * f[k].y)));
+      store_f32(&t, fmaf(x, f[k].y, y * f[k].x));
+    }
+    *(W*)((T*)a.out + to + c0) = *(const W*)v;
+    *(W*)((T*)a.out + to + c1) = *(const W*)(v + V);
+  }
+  // the components that do not turn
+  const int rest = (a.head_dim - a.dim) / V;
+  if (a.x == a.out || rest == 0) return;
+  for (int i = threadIdx.x; i < n * a.heads * rest; i += 256) {
+    const int r = i / (a.heads * rest), j = i - r * (a.heads * rest), head = j / rest, c = a.dim + (j - head * rest) * V;
+    *(W*)((T*)a.out + (size_t)(row0 + r) * a.out_ld + (size_t)head * a.out_ld_head + c) =
+        *(const W*)((const T*)a.x + (size_t)(row0 + r) * a.ld + (size_t)head * a.ld_head + c);
+  }
+}
+
+template <typename T, int V>
+static void launch_rotary_v(const RotaryArgs& a, bool interleaved, hipStream_t s) {
+  // about 1024 pieces of V pairs to a block
+  const long per_row = (long)a.heads * (a.dim / 2 / V);
+  const int RB = (int)max(1L, min(16L, 1024 / per_row));
+  const size_t lds = (size_t)RB * (a.dim / 2) * sizeof(float2);
+  const long blocks = (a.rows + RB - 1) / RB;
+  if (interleaved) rotary_kernel<T, V, true><<<(unsigned)blocks, 256, lds, s>>>(a, RB);
+  else rotary_kernel<T, V, false><<<(unsigned)blocks, 256, lds, s>>>(a, RB);
+}
+
+void launch_rotary(const void* x, bool bf16, long rows, int heads, int head_dim, size_t ld, size_t ld_head, const int* positions,
+                   const double* turns, int dim, bool interleaved, float amplitude, bool inverse, void* out, size_t out_ld,
+                   size_t out_ld_head, hipStream_t s) {
+  const RotaryArgs a = {x, out, ld, ld_head, out_ld, out_ld_head, rows, heads, head_dim, dim, positions, turns, amplitude,
+                        inverse ? -1.f : 1.f};
+  // the largest power of two that everything is a multiple of
+  const size_t es = bf16 ? 2 : 4;
+  const size_t all = ld | ld_head | out_ld | out_ld_head | (size_t)(dim / 2) | (size_t)(head_dim - dim) | (size_t)x / es | (size_t)out / es;
+  const int v = all % 8 == 0 && bf16 ? 8 : all % 4 == 0 ? 4 : all % 2 == 0 ? 2 : 1;
+  if (bf16) {
+    if (v == 8) launch_rotary_v<bf16_t, 8>(a, interleaved, s);
+    else if (v == 4) launch_rotary_v<bf16_t, 4>(a, interleaved, s);
+    else if (v == 2) launch_rotary_v<bf16_t, 2>(a, interleaved, s);
+    else launch_rotary_v<bf16_t, 1>(a, interleaved, s);
+  } else {
+    if (v == 4) launch_rotary_v<float, 4>(a, interleaved, s);
+    else if (v == 2) launch_rotary_v<float, 2>(a, interleaved, s);
+    else launch_rotary_v<float, 1>(a, interleaved, s);
+  }
+}
+
+}  // namespace ec

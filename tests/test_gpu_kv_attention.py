@@ -1,0 +1,282 @@
+"""Attention over a paged cache (ec_kv_attention) against the definition in 64 bits on what the cache holds, through the binding.  The bounds come
+with the reference: they count the rounding of probabilities to bfloat16, float32 scores and sums, and the result's rounding."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18489_amd as ec
+from tests.kv_reference import attended
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+
+
+def ints(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+
+
+class Batch:
+    """Sequences with their pages here and there in a cache that is otherwise full of NaN and of large values"""
+
+    def __init__(self, counts, lengths, heads, kv_heads, hd, page, cache, prefix=0, seed=0, sharp=1.0, fill=255):
+        rng = self.rng = np.random.default_rng(seed)
+        self.counts, self.lengths, self.prefix_len, self.hd, self.page = list(counts), list(lengths), prefix, hd, page
+        seqs = len(counts)
+        self.width, shared = max(1, -(-max(lengths, default=0) // page)), -(-prefix // page)
+        pages = seqs * self.width + shared + 3
+        order = rng.permutation(pages)
+        self.table = order[:seqs * self.width].reshape(seqs, self.width)
+        self.prefix = order[seqs * self.width:seqs * self.width + shared]
+        self.cache = ec.kv_cache(pages, kv_heads, hd, page, DTYPES[cache])
+        self.cache.data.fill_(fill)
+        slots = [self.table[b][np.arange(n) // page] * page + np.arange(n) % page for b, n in enumerate(lengths)]
+        slots.append(self.prefix[np.arange(prefix) // page] * page + np.arange(prefix) % page if prefix else np.zeros(0))
+        every = ints(np.concatenate(slots).astype(np.int64))
+        k, v = (torch.from_numpy((rng.standard_normal((len(every), kv_heads, hd)) * np.exp(rng.standard_normal((1, kv_heads, hd)) / 2) *
+                                  np.exp(rng.standard_normal((len(every), kv_heads, 1)) / 2)).astype(np.float32)).cuda() for _ in range(2))
+        ec.kv_write(self.cache, k, v, every)
+        k, v = ec.kv_read(self.cache, every, torch.float32)
+        cuts = np.cumsum([0] + list(lengths) + [prefix])
+        self.k, self.v = ([t[a:b].double().cpu().numpy() for a, b in zip(cuts[:-1], cuts[1:])] for t in (k, v))
+        self.every = every
+        self.starts = np.cumsum([0] + self.counts)
+        self.q = (torch.randn((self.starts[-1], heads, hd), device="cuda", generator=torch.Generator("cuda").manual_seed(seed)) * sharp).bfloat16()
+
+    def call(self, ragged=True, q=None, **more):
+        if ragged:
+            more = dict(starts=ints(self.starts), max_rows=max(self.counts)) | more
+        if self.prefix_len:
+            more = dict(prefix=ints(self.prefix), prefix_len=self.prefix_len) | more
+        return ec.kv_attention(self.q if q is None else q, self.cache, ints(self.table), ints(self.lengths), **more)
+
+    def check(self, out, causal=False, scale=None, seen_of=None):
+        scale = self.hd ** -0.5 if scale is None else scale
+        out, q = out.double().cpu().numpy(), self.q.double().cpu().numpy()
+        for b, (n, t) in enumerate(zip(self.counts, self.lengths)):
+            keys, values = (np.concatenate((x[-1], x[b])) for x in (self.k, self.v))
+            seen = np.ones((n, self.prefix_len + t), dtype=bool)
+            if causal:
+                seen[:, self.prefix_len:] = np.arange(t) < (t - n + 1 + np.arange(n))[:, None]
+            if seen_of:
+                seen &= seen_of(b, n, t)
+            at = slice(self.starts[b], self.starts[b + 1])
+            want, bound = attended(q[at], keys, values, seen, scale)
+            assert np.array_equal(np.isnan(out[at]), np.isnan(want))
+            with np.errstate(invalid="ignore"):
+                far = np.abs(out[at] - want) > bound
+            assert not far.any(), (b, np.argwhere(far)[:5], (np.abs(out[at] - want) / bound).max())
+            assert (out[at][~seen.any(axis=1)] == 0).all()
+
+
+SHAPES = [  # rows and keys of the sequences, heads, kv heads, head dim, page, prefix
+    ([1], [1], 1, 1, 64, 32, 0), ([1], [1000], 28, 4, 128, 64, 0), ([3, 1, 2], [33, 0, 64], 4, 4, 64, 32, 0), ([17], [100], 8, 1, 128, 128, 0),
+    ([5, 0, 16, 34], [31, 32, 97, 300], 4, 2, 128, 64, 0), ([1, 1, 1, 1], [5, 700, 1, 0], 28, 4, 128, 256, 0), ([2, 3], [40, 10], 6, 2, 64, 32, 50),
+    ([1] * 9, [3, 0, 40, 12, 65, 1, 31, 33, 8], 28, 4, 128, 64, 333), ([40, 7], [0, 0], 4, 4, 128, 32, 65), ([130], [257], 2, 1, 64, 64, 0),
+    ([70, 130], [200, 1], 3, 3, 128, 64, 100), ([1], [5000], 4, 4, 128, 64, 0), ([2], [70], 12, 4, 128, 32, 4111), ([300], [513], 4, 2, 128, 128, 0),
+    ([48, 49, 33], [64, 96, 47], 16, 2, 64, 32, 0), ([500, 1], [600, 700], 2, 2, 128, 64, 31)]
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_against_the_definition(shape, causal, cache):
+    counts, lengths, heads, kv_heads, hd, page, prefix = shape
+    b = Batch(counts, lengths, heads, kv_heads, hd, page, cache, prefix, seed=len(counts) + page)
+    b.check(b.call(causal=causal), causal)
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("sharp,scale", [(0.0, None), (8.0, None), (1.0, 3.0), (40.0, 0.01)])
+def test_flat_and_sharp_rows(sharp, scale, cache):
+    b = Batch([5, 60], [700, 90], 8, 2, 128, 64, cache, 130, sharp=sharp)
+    b.check(b.call(scale=scale), scale=scale)
+
+
+def test_rows_of_equal_count_and_defaults():
+    b = Batch([4, 4, 4], [100, 64, 3], 8, 4, 64, 32, "e4m3")
+    assert torch.equal(b.call(ragged=False), b.call())
+    assert torch.equal(b.call(ragged=False, max_keys=100), b.call())
+    b.check(b.call(max_rows=None))
+
+
+def test_what_is_behind_the_keys_does_not_count():
+    """bytes of every kind where no key is: NaN codes, largest scales, zeros"""
+    outs = []
+    for fill in (0, 127, 255, 128, 254):
+        b = Batch([3, 20, 1], [33, 7, 95], 8, 4, 128, 64, "e4m3", 40, fill=fill)
+        outs.append(b.call(causal=True))
+        b.check(outs[-1], True)
+    assert all(torch.equal(outs[0], o) for o in outs[1:])
+    for fill in (255, 127):
+        b = Batch([3, 20, 1], [33, 7, 95], 8, 4, 128, 64, "bf16", 40, fill=fill)
+        b.check(b.call(causal=True), True)
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+def test_keys_that_a_row_does_not_see_may_be_nan(cache):
+    n, t = 50, 64
+    b = Batch([n], [t], 4, 2, 128, 32, cache)
+    clean = b.call(causal=True)
+    at = 40      # rows see the keys before t - n + i + 1: those up to row 25 do not see key 40
+    bad = torch.zeros((1, 2, 128), device="cuda")
+    bad[..., 3] = float("nan")
+    for which in range(2):
+        other = Batch([n], [t], 4, 2, 128, 32, cache)
+        k, v = ec.kv_read(other.cache, ints([other.table[0][at // 32] * 32 + at % 32]), torch.float32)
+        ec.kv_write(other.cache, *((bad, v) if which == 0 else (k, bad)), ints([other.table[0][at // 32] * 32 + at % 32]))
+        out = other.call(causal=True)
+        first = at - (t - n)
+        assert torch.equal(out[:first], clean[:first]) and torch.isnan(out[first:]).all()
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+def test_pages_that_are_not_there_are_not_seen(cache):
+    b = Batch([3, 40], [200, 150], 4, 2, 64, 32, cache, 70)
+    b.table[0][1], b.table[1][4], b.prefix[1] = -1, b.cache.pages, 2 ** 31 - 1
+
+    def seen(which, n, t):
+        s = np.ones((n, 70 + t), dtype=bool)
+        s[:, 32:64] = False
+        s[:, 70 + 32:70 + 64] &= which != 0
+        s[:, 70 + 128:] &= which != 1
+        return s
+    b.check(b.call(), seen_of=seen)
+
+
+def test_rows_of_no_sequence_and_beyond_the_most_are_left_as_they_were():
+    b = Batch([6, 2, 5], [40, 50, 60], 4, 4, 128, 32, "e4m3", 33)
+    full = b.call()
+    out = torch.full_like(b.q, 7.0)
+    starts = ints([2, 6, 8, 11])      # two rows before the first, two behind the last
+    assert b.call(starts=starts, max_rows=6, out=out) is out
+    assert (out[:2] == 7).all() and (out[11:] == 7).all() and torch.equal(out[6:8], full[6:8]) and torch.equal(out[2:6], full[2:6])
+    out.fill_(7.0)
+    b.call(max_rows=3, out=out)
+    assert torch.equal(out[:3], full[:3]) and (out[3:6] == 7).all() and torch.equal(out[8:11], full[8:11]) and (out[11:] == 7).all()
+    assert (b.call(starts=starts, max_rows=6)[:2] == 0).all()
+    # starts that are no starts: nothing outside out, and nothing hangs
+    for bad in ([0, -5, 20, 13], [13, 8, 6, 0], [-1, -1, -1, -1], [2 ** 31 - 1, -2 ** 31, 0, 13]):
+        b.call(starts=ints(bad), max_rows=6)
+    bad = b.lengths
+    b.lengths = [-1, 2 ** 31 - 1, -2 ** 31]
+    assert torch.isfinite(b.call(prefix=None, prefix_len=0, max_keys=50)[:6]).all()
+    b.lengths = bad
+    torch.cuda.synchronize()
+
+
+def test_strides():
+    b = Batch([3, 20], [100, 40], 6, 3, 64, 32, "bf16", 20)
+    want = b.call()
+    wide = torch.randn((23, 10, 72), device="cuda").bfloat16()
+    wide[:, 2:8, :64] = b.q
+    assert torch.equal(b.call(q=wide[:, 2:8, :64]), want)
+    out = torch.full((6, 23, 64), 7.0, device="cuda").bfloat16().transpose(0, 1)
+    assert torch.equal(b.call(q=b.q.transpose(0, 1).contiguous().transpose(0, 1), out=out), want)
+    out = torch.full((23, 8, 80), 7.0, device="cuda").bfloat16()
+    b.call(out=out[:, 1:7, 8:72])
+    assert torch.equal(out[:, 1:7, 8:72], want)
+    out[:, 1:7, 8:72] = 7
+    assert (out == 7).all()
+    table = torch.full((2, b.width + 5), -9, dtype=torch.int32, device="cuda")
+    table[:, :b.width] = ints(b.table)
+    assert torch.equal(ec.kv_attention(b.q, b.cache, table[:, :b.width], ints(b.lengths), ints(b.starts), 20, prefix=ints(b.prefix), prefix_len=20), want)
+    one = b.q[:1, :1].expand(23, 6, 64)
+    assert torch.equal(b.call(q=one), b.call(q=one.contiguous()))
+
+
+def test_a_prefix_is_as_good_as_keys_of_ones_own():
+    """the same keys as a shared prefix and as pages in every sequence's own table"""
+    page, prefix = 32, 96
+    b = Batch([2, 30, 1], [10, 70, 33], 8, 4, 128, page, "e4m3", prefix)
+    b.check(b.call())
+    table = np.concatenate((np.tile(b.prefix, (3, 1)), b.table), axis=1)
+    own = ec.kv_attention(b.q, b.cache, ints(table), ints(np.array(b.lengths) + prefix), ints(b.starts), 30)
+    b.check(own)
+
+
+def test_no_rows_no_keys_a_graph_and_another_stream():
+    b = Batch([3, 9], [700, 300], 8, 4, 128, 64, "e4m3", 1100)
+    none = ec.kv_attention(b.q[:0], b.cache, ints(b.table), ints([0, 0]))
+    assert none.shape == (0, 8, 128)
+    assert (ec.kv_attention(b.q, b.cache, ints(np.zeros((1, 0))), ints([5]), max_keys=0) == 0).all()
+    want = b.call()
+    lengths, starts, table, prefix = ints(b.lengths), ints(b.starts), ints(b.table), ints(b.prefix)
+    q, out = b.q.clone(), torch.zeros_like(b.q)
+
+    def call(**more):
+        return ec.kv_attention(q, b.cache, table, lengths, starts, 9, prefix=prefix, prefix_len=1100, **more)
+    graphs = []
+    for _ in range(2):      # two graphs of the same call, each with its workspace
+        call(out=out)
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call(out=out)
+    for i in range(4):
+        q.normal_()
+        lengths.copy_(ints([700 - 100 * i, 300 - i]))
+        eager = call()
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    assert torch.equal(b.call(stream=s), want)
+
+
+def test_the_same_bits_every_time():
+    b = Batch([34, 20, 1], [900, 1100, 40], 8, 4, 128, 64, "e4m3", 2000)
+    first = b.call()
+    for _ in range(5):
+        assert torch.equal(b.call(), first)
+
+
+def test_keys_beyond_4_gib():
+    cache = ec.kv_cache(40000, 4, 128, 128)
+    assert cache.data.numel() > 2 ** 32
+    table = np.array([[39999, 3, 20000, 39000]])
+    slots = ints(np.concatenate([p * 128 + np.arange(128) for p in table[0]]))
+    k, v = torch.randn((512, 4, 128), device="cuda"), torch.randn((512, 4, 128), device="cuda")
+    ec.kv_write(cache, k, v, slots)
+    k, v = (t.double().cpu().numpy() for t in ec.kv_read(cache, slots, torch.float32))
+    q = torch.randn((2, 8, 128), device="cuda").bfloat16()
+    out = ec.kv_attention(q, cache, ints(table), ints([500]))
+    want, bound = attended(q.double().cpu().numpy(), k[:500], v[:500], np.ones((2, 500), dtype=bool), 128 ** -0.5)
+    assert (np.abs(out.double().cpu().numpy() - want) <= bound).all()
+
+
+def test_a_step_of_two_sequences_with_one_prompt():
+    """rotary positions, the cache and the attention as a program strings them together: a prompt is written once, each of two sequences adds some
+    tokens in its own pages, some of them are written again, and a few rows of each attend to everything"""
+    rng = np.random.default_rng(7)
+    heads, kv_heads, hd, page, prompt = 8, 4, 128, 32, 75
+    plan = ec.rotary_plan(hd, 500000.0)
+    cache = ec.kv_cache(10, kv_heads, hd, page)
+    prefix, table = np.array([4, 9, 1]), np.array([[0, 5], [7, 2]])
+    own = [40, 51]
+
+    def slots_of(pages, at):
+        return np.asarray(pages)[np.asarray(at) // page] * page + np.asarray(at) % page
+
+    def rows(n):
+        return torch.randn((n, heads + 2 * kv_heads, hd), device="cuda").bfloat16()
+
+    held = {}      # slot -> the key and value that were written last
+
+    def write(qkv, positions, slots):
+        turned = ec.rotary(qkv[:, :heads + kv_heads], ints(positions), plan)
+        ec.kv_write(cache, turned[:, heads:], qkv[:, heads + kv_heads:], ints(slots))
+        for r, s in enumerate(slots):
+            held[int(s)] = (turned[r, heads:], qkv[r, heads + kv_heads:])
+        return turned[:, :heads]
+    write(rows(prompt), np.arange(prompt), slots_of(prefix, np.arange(prompt)))
+    for b in range(2):
+        write(rows(own[b]), prompt + np.arange(own[b]), slots_of(table[b], np.arange(own[b])))
+    again = [np.sort(rng.permutation(own[b])[:n]) for b, n in ((0, 5), (1, 9))]
+    q = write(rows(14), prompt + np.concatenate(again), np.concatenate([slots_of(table[b], again[b]) for b in range(2)]))
+    out = ec.kv_attention(q, cache, ints(table), ints(own), ints([0, 5, 14]), 9, max_keys=51, prefix=ints(prefix), prefix_len=prompt)
+    from tests.kv_reference import kept
+    for b, at in ((0, slice(0, 5)), (1, slice(5, 14))):
+        slots = np.concatenate((slots_of(prefix, np.arange(prompt)), slots_of(table[b], np.arange(own[b]))))
+        k, v = (kept(torch.stack([held[int(s)][i] for s in slots]).double().cpu().numpy(), "e4m3") for i in range(2))
+        want, bound = attended(q[at].double().cpu().numpy(), k, v, np.ones((at.stop - at.start, len(slots)), dtype=bool), hd ** -0.5)
+        assert (np.abs(out[at].double().cpu().numpy() - want) <= bound).all()

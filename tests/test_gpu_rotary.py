@@ -1,0 +1,133 @@
+"""Rotary positions (ec_rotary) against the formula in 64 bits, through the binding.
+
+The bound: y = 2 pi (t - quarters / 4), |y| <= pi/4, is rounded to float32 (2^-24 y), the series and their last operations to 2^-24, and the
+amplitude's and the pair's products and sum once each: 4 x 2^-24 of amplitude (|x| + |y|) in all; one rounding more for bfloat16.  The
+angle in 64 bits is off by 2^-52 of itself, 2e-9 radians at position 2^24."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18489_amd as ec
+from tests.kv_reference import HALF, turned
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def theta_of(dim, base):
+    return base ** (-2.0 * np.arange(dim // 2) / dim)
+
+
+def check(y, x, positions, theta, dtype, interleaved=False, amplitude=1.0, inverse=False):
+    x = x.double().cpu().numpy()
+    positions = positions.cpu().numpy()
+    want = turned(x, positions, theta, interleaved, amplitude, inverse)
+    size = turned(np.abs(x), np.zeros_like(positions), theta)      # |x| and |y| of each pair, at both places
+    half = len(theta)
+    pair = size[..., :2 * half].reshape(*size.shape[:2], half, 2) if interleaved else np.stack((size[..., :half], size[..., half:2 * half]), -1)
+    both = pair.sum(-1)
+    both = np.repeat(both, 2, -1) if interleaved else np.concatenate((both, both), -1)
+    angle = np.abs(positions).max(initial=0) * 2.0 ** -52
+    off = (4 * HALF["f32"] + angle) * abs(amplitude) * both
+    if dtype == "bf16":
+        off = off + HALF["bf16"] * (np.abs(want[..., :2 * half]) + off)
+    got = y.double().cpu().numpy()
+    assert (np.abs(got - want)[..., :2 * half] <= off + 1e-37).all()
+    assert np.array_equal(got[..., 2 * half:], x[..., 2 * half:])
+
+
+def data(rows, heads, head_dim, dtype, pad=0, last=4096, seed=0):
+    rng = np.random.default_rng(seed + rows)
+    x = torch.from_numpy(rng.standard_normal((rows, heads * head_dim + pad)).astype(np.float32)).cuda().to(DTYPES[dtype])
+    return x[:, :heads * head_dim].unflatten(1, (heads, head_dim)), torch.from_numpy(rng.integers(0, last, rows).astype(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,heads,head_dim,dim,pad", [(1, 1, 2, 2, 0), (1, 64, 128, 128, 0), (3, 5, 64, 64, 8), (5, 3, 128, 64, 4), (7, 2, 96, 38, 0),
+                                                         (2, 7, 80, 22, 3), (33, 9, 512, 512, 0), (17, 4, 6, 4, 1), (1000, 36, 128, 128, 0),
+                                                         (65, 1, 3, 2, 0), (257, 1024, 2, 2, 2)])
+def test_against_the_formula(rows, heads, head_dim, dim, pad, dtype, interleaved):
+    x, at = data(rows, heads, head_dim, dtype, pad)
+    plan = ec.rotary_plan(dim, 10000.0, interleaved, amplitude=1.25)
+    check(ec.rotary(x, at, plan), x, at, theta_of(dim, 10000.0), dtype, interleaved, 1.25)
+    check(ec.rotary(x, at, plan, inverse=True), x, at, theta_of(dim, 10000.0), dtype, interleaved, 1.25, True)
+
+
+def test_far_and_negative_positions():
+    x, _ = data(9, 4, 128, "f32")
+    at = torch.tensor([0, 1, -1, 2 ** 20 + 1, 2 ** 24 - 1, -(2 ** 23), 7, 131071, 2 ** 22], dtype=torch.int32, device="cuda")
+    check(ec.rotary(x, at, ec.rotary_plan(128, 500000.0)), x, at, theta_of(128, 500000.0), "f32")
+
+
+@pytest.mark.parametrize("factor,original,low,high", [(8.0, 0, 1, 32), (16.0, 8192, 1, 32), (13.37, 4096, 1, 4), (1.0, 2048, 1, 4)])
+def test_scaled_frequencies(factor, original, low, high):
+    dim, base = 96, 10000.0
+    theta = theta_of(dim, base)
+    share = np.clip((original * theta / (2 * np.pi) - low) / (high - low), 0, 1) if original else np.zeros_like(theta)
+    theta = share * theta + (1 - share) * theta / factor
+    plan = ec.rotary_plan(dim, base, True, factor, original, low, high)
+    np.testing.assert_allclose(plan.turns.cpu().numpy() * 2 * np.pi, theta, rtol=1e-14)
+    x, at = data(50, 6, 128, "f32", last=100000)
+    check(ec.rotary(x, at, plan), x, at, theta, "f32", True)
+
+
+def test_strides_in_place_and_what_lies_between():
+    rows, heads, hd = 37, 6, 128
+    wide = torch.randn((rows, 10, hd + 16), device="cuda").bfloat16()
+    before, at = wide.clone(), torch.arange(rows, dtype=torch.int32, device="cuda")
+    plan = ec.rotary_plan(64)
+    x = wide[:, 2:2 + heads, 8:8 + hd]
+    want = ec.rotary(x.contiguous(), at, plan)
+    assert ec.rotary(x, at, plan, out=x) is x and torch.equal(x, want)
+    wide[:, 2:2 + heads, 8:8 + hd] = before[:, 2:2 + heads, 8:8 + hd]
+    assert torch.equal(wide, before)
+    # heads before rows, every second row, one row for all
+    t = torch.randn((heads, 2 * rows, hd), device="cuda")
+    out = torch.empty((heads, rows, hd), device="cuda").transpose(0, 1)
+    x = t.transpose(0, 1)[::2]
+    ec.rotary(x, at, plan, out=out)
+    assert torch.equal(out, ec.rotary(x.contiguous(), at, plan))
+    one = t[:1, :1].transpose(0, 1).expand(rows, heads, hd)
+    assert torch.equal(ec.rotary(one, at, plan), ec.rotary(one.contiguous(), at, plan))
+    # one element off every alignment
+    off = torch.randn(rows * heads * hd + 1, device="cuda").bfloat16()[1:].view(rows, heads, hd)
+    assert torch.equal(ec.rotary(off, at, plan), ec.rotary(off.clone(), at, plan))
+
+
+def test_the_inverse_is_the_gradient():
+    """against differences: the operator is linear, so that <g, R(x + d) - R(x - d)> / 2 = <R' g, d>, whatever d is"""
+    x, at = data(20, 4, 64, "f32", seed=1)
+    plan = ec.rotary_plan(48, interleaved=True, amplitude=0.8)
+    g, d = torch.randn_like(x), torch.randn_like(x)
+    moved = (ec.rotary(x + d, at, plan).double() - ec.rotary(x - d, at, plan).double()) / 2
+    left, right = (g.double() * moved).sum(), (ec.rotary(g, at, plan, inverse=True).double() * d.double()).sum()
+    # each element is off by at most 4 x 2^-24 of its pair on both sides (and its sums x + d, x - d by 2^-24)
+    size = (g.abs().double().sum() * 3 * 8 * HALF["f32"] * float((x.abs() + d.abs()).max()))
+    assert abs(left - right) <= size
+
+
+def test_no_rows_infinities_and_a_graph():
+    plan = ec.rotary_plan(64)
+    none = torch.empty((0, 4, 64), device="cuda")
+    assert ec.rotary(none, torch.empty(0, dtype=torch.int32, device="cuda"), plan).shape == (0, 4, 64)
+    x, at = data(4, 3, 64, "f32")
+    x = x.clone()
+    x[1, 1, 5], x[2, 0, 40] = float("inf"), float("nan")
+    y = ec.rotary(x, at, plan)
+    bad = torch.zeros_like(x, dtype=torch.bool)
+    bad[1, 1, [5, 37]] = True
+    bad[2, 0, [8, 40]] = True
+    assert torch.equal(~torch.isfinite(y), bad)      # (only what is in a pair with them)
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(x)
+    with torch.cuda.graph(graph):
+        ec.rotary(x, at, plan, out=out)
+    for seed in range(3):
+        new, _ = data(4, 3, 64, "f32", seed=seed)
+        x.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ec.rotary(x, at, plan))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    assert torch.equal(ec.rotary(x, at, plan, stream=s), out)
