@@ -73,13 +73,132 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int b) {
   return s;
 }
 
+// What a block works on: rows of a sequence (or of the whole call, over the prefix) and a slice of its keys.
+struct Part {
+  Seq s;
+  const int* table;
+  int first, queries;         // its queries begin here; queries of the sequence and kv head
+  int kvh, slice, c_lo, c_hi; // chunks
+  int seen_first;             // keys that its first row sees
+  bool causal;
+  // row, head and keys seen of query `m`; behind the last query: the last one's
+  __device__ __forceinline__ void query(const Args& a, int m, int* row, int* head, int* seen) const {
+    m = min(m, queries - 1);
+    const int r = m / a.group;
+    *row = s.row0 + r;
+    *head = kvh * a.group + (m - r * a.group);
+    *seen = causal ? s.keys - s.n + 1 + r : s.keys;
+  }
+};
+// false: nothing to do.  EACH: queries of a block.  The heads' and sequences' blocks lie next to each other, so that blocks that read the same keys are
+// a multiple of kv_heads apart and mostly share an XCD's L2; late rows, which see most under `causal`, go first.
+template <int EACH, bool PREFIX>
+__device__ __forceinline__ bool part_of(const Args& a, int tiles, Part& p) {
+  unsigned id = blockIdx.x;
+  p.kvh = id % a.place.kv_heads;
+  id /= a.place.kv_heads;
+  const int seqs = PREFIX ? 1 : a.seqs, b = id % seqs;
+  id /= seqs;
+  const int slices = PREFIX ? a.prefix_slices : a.slices;
+  p.slice = id % slices;
+  const int tile = tiles - 1 - (int)(id / slices);
+  p.s = PREFIX ? Seq{0, a.rows, a.prefix_len} : seq_of(a, b);
+  p.first = tile * EACH;
+  p.queries = p.s.n * a.group;
+  if (p.first >= p.queries) return false;
+  p.table = PREFIX ? a.prefix : a.table + (size_t)b * a.table_ld;
+  const int split = PREFIX ? a.prefix_split : a.split;
+  p.causal = !PREFIX && a.causal;
+  p.c_lo = p.slice * split;
+  if (p.slice > 0 && p.c_lo * 32 >= p.s.keys) return false;   // (the slices that are joined go by the keys too)
+  const int last_row = (min(p.first + EACH, p.queries) - 1) / a.group;
+  p.seen_first = p.causal ? p.s.keys - p.s.n + 1 + p.first / a.group : p.s.keys;
+  const int seen_last = p.causal ? p.s.keys - p.s.n + 1 + last_row : p.s.keys;
+  p.c_hi = min(p.c_lo + split, (max(seen_last, 0) + 31) >> 5);
+  return true;
+}
+
+// The pages of every `step`-th chunk from `first` on, 64 of them in a wave's lanes
+struct Pages {
+  const int* table;
+  int first, step, last, shift, ids;
+  __device__ __forceinline__ int of(int i, int lane) {
+    if ((i & 63) == 0) ids = table[min(first + step * (i + lane), last) >> shift];
+    return __builtin_amdgcn_readlane(ids, i & 63);
+  }
+};
+
+// Scores of 16 queries and 32 keys (S^T: a lane has 8 neighbouring keys of query lane & 15) to the probabilities that multiply the values: the
+// running maximum m and sum l move on, acc with them.  hidden(e): whether the lane's key e is not to be seen; asked only where `masked`.
+template <int HT, typename Hidden>
+__device__ __forceinline__ bf16x8 soften(f32x4 (&sc)[2], f32x4 (&acc)[HT], float& m, float& l, const float (&vs)[8], float scale, bool masked,
+                                         Hidden hidden) {
+  if (masked) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (hidden(e)) sc[e >> 2][e & 3] = -INFINITY;
+  }
+  const float mx = max_of_swap32(max_of_swap16(max_of_8(sc[0], sc[1]))) * scale;
+  if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
+    const float m_new = max_of(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int h = 0; h < HT; ++h) acc[h] *= alpha;
+  }
+  float p[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], scale, -m));
+    l += p[e];
+    p[e] *= vs[e];
+  }
+  if (masked) {   // (a hidden key's power of two may be none)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (hidden(e)) p[e] = 0.f;
+  }
+  return u4_as_bf16x8(make_uint4(pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]), pack2_bf16(p[4], p[5]), pack2_bf16(p[6], p[7])));
+}
+
+// a piece of values, with the keys from `live` on (of its 8) as zeros: what lies behind the last key may be anything
+template <int ES> __device__ __forceinline__ void cut_values(u32x4& v, int live) {
+  if constexpr (ES == 1) {
+    const uint64_t keep = live >= 8 ? ~0ull : (1ull << (8 * max(live, 0))) - 1;
+    v &= (u32x4){(uint32_t)keep, (uint32_t)(keep >> 32), (uint32_t)keep, (uint32_t)(keep >> 32)};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] &= (2 * e < live ? 0xffffu : 0u) | (2 * e + 1 < live ? 0xffff0000u : 0u);
+  }
+}
+
+// 8 neighbouring components of a query, o / l or, where slices are joined, o and (m, l)
+template <int HD, bool DIRECT>
+__device__ __forceinline__ void leave(const Args& a, int row, int head, int slice, int c, const float (&o)[8], float m, float l) {
+  if constexpr (DIRECT) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    *(uint4*)(a.out + (size_t)row * a.out_ld + (size_t)head * a.out_head + c) =
+        make_uint4(pack2_bf16(o[0] * inv, o[1] * inv), pack2_bf16(o[2] * inv, o[3] * inv), pack2_bf16(o[4] * inv, o[5] * inv),
+                   pack2_bf16(o[6] * inv, o[7] * inv));
+  } else {
+    const size_t at = ((size_t)row * a.heads + head) * (a.prefix_slices + a.slices) + slice;
+    float4* to = (float4*)(a.part + at * HD + c);
+    to[0] = make_float4(o[0], o[1], o[2], o[3]);
+    to[1] = make_float4(o[4], o[5], o[6], o[7]);
+    if (c == 0) a.sums[at] = make_float2(m, l);
+  }
+}
+
 // One chunk as a lane holds it
 template <int ES, int HD> struct Chunk {
   static constexpr int U = KvChunk<ES, HD>::kUnits, V = HD / 32 * ES;
   u32x4 k[2 * U], v[V];
   uint32_t ks[2];
   u32x2 vs;
-  __device__ __forceinline__ void load(const Args& a, size_t chunk, int lane) {
+  int there;
+  __device__ __forceinline__ void load(const Args& a, int page, int no, int kvh, int lane) {
+    there = page >= 0 && page < a.pages;
+    const size_t chunk = ((((size_t)(there ? page : 0) * a.place.kv_heads + kvh) << a.place.shift) + (no & ((1 << a.place.shift) - 1)));
     const u32x4* p = (const u32x4*)(a.data + chunk * KvChunk<ES, HD>::kBytes) + lane;
 #pragma unroll
     for (int i = 0; i < 2 * U; ++i) k[i] = p[i * 64];
@@ -99,44 +218,26 @@ template <int ES, int HD> struct Chunk {
 
 constexpr int kWaves = 4;
 
-// A block's waves go through the chunks of its slice in turn, each with QT tiles of 16 queries, and meet in LDS.  PREFIX: the rows of the
-// whole call over the prefix.  DIRECT: there is one slice, and the block writes the result.
+// Few queries: up to 48 of a sequence and kv head.  A block's waves go through the chunks of its slice in turn, each with all QT tiles of 16
+// queries and a chunk's pieces in registers, the next chunk's on their way, and meet in LDS.
+// DIRECT: there is one slice, and the block writes the result.
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
-__global__ __launch_bounds__(256) void kv_attention_kernel(Args a, int tiles) {
+__global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles) {
   constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
   typedef Chunk<ES, HD> C;
   extern __shared__ float4 lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane >> 4, col = lane & 15;
-  unsigned id = blockIdx.x;
-  const int kvh = id % a.place.kv_heads;
-  id /= a.place.kv_heads;
-  const int slices = PREFIX ? a.prefix_slices : a.slices, slice = id % slices;
-  id /= slices;
-  const int tile = id % tiles, b = id / tiles;
-  const Seq s = PREFIX ? Seq{0, a.rows, a.prefix_len} : seq_of(a, b);
-  const int first = tile * 16 * QT, queries = s.n * a.group;    // of this sequence and kv head
-  if (first >= queries) return;
-  const int* table = PREFIX ? a.prefix : a.table + (size_t)b * a.table_ld;
-  const int split = PREFIX ? a.prefix_split : a.split;
-  const bool causal = !PREFIX && a.causal;
-  const int c_lo = slice * split;
-  if (slice > 0 && c_lo * 32 >= s.keys) return;
-  // keys that the tile's first and last rows see
-  const int last_row = (min(first + 16 * QT, queries) - 1) / a.group;
-  const int seen_first = causal ? s.keys - s.n + 1 + first / a.group : s.keys;
-  const int seen_last = causal ? s.keys - s.n + 1 + last_row : s.keys;
-  const int c_hi = min(c_lo + split, (max(seen_last, 0) + 31) >> 5);
+  Part part;
+  if (!part_of<16 * QT, PREFIX>(a, tiles, part)) return;
 
   bf16x8 qf[QT][HB];
-  int seen[QT], row[QT], head[QT];
+  int seen[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const int m = min(first + t * 16 + col, queries - 1), r = m / a.group;
-    row[t] = s.row0 + r;
-    head[t] = kvh * a.group + (m - r * a.group);
-    seen[t] = causal ? s.keys - s.n + 1 + r : s.keys;
-    const bf16_t* p = a.q + (size_t)row[t] * a.q_ld + (size_t)head[t] * a.q_head + grp * (HD / 4);
+    int row, head;
+    part.query(a, part.first + t * 16 + col, &row, &head, &seen[t]);
+    const bf16_t* p = a.q + (size_t)row * a.q_ld + (size_t)head * a.q_head + grp * (HD / 4);
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) qf[t][hb] = as_bf16x8(*(const u32x4*)(p + hb * 8));
   }
@@ -150,35 +251,24 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(Args a, int tiles) {
     for (int h = 0; h < HT; ++h) acc[t][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
 
-  const int mine = c_lo + wave < c_hi ? (c_hi - c_lo - wave + kWaves - 1) / kWaves : 0;   // chunks of this wave
-  auto chunk_no = [&](int i) { return c_lo + wave + kWaves * i; };
-  int pids = 0;      // lane i: the page of the wave's i-th chunk (of the present 64)
-  auto page_of = [&](int i) {
-    if ((i & 63) == 0) pids = table[min(chunk_no(i + lane), chunk_no(mine - 1)) >> a.place.shift];
-    return __builtin_amdgcn_readlane(pids, i & 63);
-  };
-  C cur, next;
-  int page = 0, page_next = 0;
+  const int from = part.c_lo + wave;                                                        // this wave's first chunk
+  const int mine = from < part.c_hi ? (part.c_hi - from + kWaves - 1) / kWaves : 0;         // and how many it has
+  Pages pages = {part.table, from, kWaves, from + kWaves * (mine - 1), a.place.shift, 0};
   auto fetch = [&](C& c, int i) {
-    const int pg = page_of(i), no = chunk_no(i);
-    const bool there = pg >= 0 && pg < a.pages;
-    c.load(a, ((((size_t)(there ? pg : 0) * a.place.kv_heads + kvh) << a.place.shift) + (no & ((1 << a.place.shift) - 1))), lane);
-    return there ? 1 : 0;
+    const int n = min(i, mine - 1);     // (behind the last chunk it comes once more, from the cache)
+    c.load(a, pages.of(n, lane), from + kWaves * n, part.kvh, lane);
   };
-  if (mine > 0) page = fetch(cur, 0);
-  for (int i = 0; i < mine; ++i) {
-    if (i + 1 < mine) page_next = fetch(next, i + 1);
-    const int key0 = chunk_no(i) * 32, over = key0 + 32;
-    // ---- scores
+  auto step = [&](C& c, int i) {
+    const int key0 = (from + kWaves * i) * 32, k0 = key0 + grp * 8;
     f32x4 sc[QT][2];
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
       bf16x8 kf[HB];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const u32x4 k = cur.k[t2 * U + u];
+        const u32x4 k = c.k[t2 * U + u];
         if constexpr (ES == 1) {
-          const float f = power_of(cur.ks[t2]);
+          const float f = power_of(c.ks[t2]);
           kf[2 * u] = widen8(k[0], k[1], f);
           kf[2 * u + 1] = widen8(k[2], k[3], f);
         } else {
@@ -192,66 +282,39 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(Args a, int tiles) {
         for (int hb = 0; hb < HB; ++hb) sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], qf[t][hb], sc[t][t2], 0, 0, 0);
       }
     }
-    const int k0 = key0 + grp * 8;
-    const bool masked = over > min(seen_first, s.keys) || !page;
+    const bool masked = key0 + 32 > part.seen_first || !c.there;
     if (masked) {
+      const int live = c.there ? part.s.keys - k0 : 0;
 #pragma unroll
-      for (int t = 0; t < QT; ++t)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (k0 + e >= seen[t] || !page) sc[t][e >> 2][e & 3] = -INFINITY;
-      // what lies behind the last key may be anything
-      const int live = page ? min(max(s.keys - k0, 0), 8) : 0;
-#pragma unroll
-      for (int h = 0; h < C::V; ++h) {
-        if constexpr (ES == 1) {
-          const uint64_t keep = live == 8 ? ~0ull : (1ull << (8 * live)) - 1;
-          cur.v[h] &= (u32x4){(uint32_t)keep, (uint32_t)(keep >> 32), (uint32_t)keep, (uint32_t)(keep >> 32)};
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) cur.v[h][e] &= (2 * e < live ? 0xffffu : 0u) | (2 * e + 1 < live ? 0xffff0000u : 0u);
-        }
-      }
+      for (int h = 0; h < C::V; ++h) cut_values<ES>(c.v[h], live);
     }
-    // ---- softmax
     float vs[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vs[e] = power_of((cur.vs[e >> 2] >> (8 * (e & 3))) & 255u);
+    for (int e = 0; e < 8; ++e) vs[e] = power_of((c.vs[e >> 2] >> (8 * (e & 3))) & 255u);
     bf16x8 pf[QT];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const float mx = max_of_swap32(max_of_swap16(max_of_8(sc[t][0], sc[t][1]))) * a.scale;
-      if (__builtin_amdgcn_ballot_w64(mx > m_run[t]) != 0) {
-        const float m_new = max_of(m_run[t], mx), alpha = __builtin_amdgcn_exp2f(m_run[t] - m_new);
-        m_run[t] = m_new;
-        l_run[t] *= alpha;
-#pragma unroll
-        for (int h = 0; h < HT; ++h) acc[t][h] *= alpha;
-      }
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e >> 2][e & 3], a.scale, -m_run[t]));
-        l_run[t] += p[e];
-        p[e] *= vs[e];
-      }
-      if (masked)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (k0 + e >= seen[t] || !page) p[e] = 0.f;
-      pf[t] = u4_as_bf16x8(make_uint4(pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]), pack2_bf16(p[4], p[5]), pack2_bf16(p[6], p[7])));
-    }
-    // ---- values
+    for (int t = 0; t < QT; ++t)
+      pf[t] = soften<HT>(sc[t], acc[t], m_run[t], l_run[t], vs, a.scale, masked, [&](int e) { return k0 + e >= seen[t] || !c.there; });
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
       bf16x8 vf;
-      if constexpr (ES == 1) vf = h & 1 ? widen8(cur.v[h >> 1][2], cur.v[h >> 1][3], 1.f) : widen8(cur.v[h >> 1][0], cur.v[h >> 1][1], 1.f);
-      else vf = as_bf16x8(cur.v[h]);
+      if constexpr (ES == 1) vf = h & 1 ? widen8(c.v[h >> 1][2], c.v[h >> 1][3], 1.f) : widen8(c.v[h >> 1][0], c.v[h >> 1][1], 1.f);
+      else vf = as_bf16x8(c.v[h]);
 #pragma unroll
       for (int t = 0; t < QT; ++t) acc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[t][h], 0, 0, 0);
     }
-    cur = next;
-    page = page_next;
+  };
+  C one, two;
+  if (mine > 0) fetch(one, 0);
+  for (int i = 0; i < mine; i += 2) {
+    fetch(two, i + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    step(one, i);
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(one, i + 2);
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + 1 < mine) step(two, i + 1);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // ---- the waves' parts meet: (m, sum, O) of each, in their order
@@ -267,7 +330,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(Args a, int tiles) {
     for (int h = 0; h < HT; ++h) slot[(t * HT + h) * 64 + lane] = make_float4(acc[t][h][0], acc[t][h][1], acc[t][h][2], acc[t][h][3]);
   }
   __syncthreads();
-  const int total = a.prefix_slices + a.slices, at_slice = PREFIX ? slice : a.prefix_slices + slice;
+  const int at_slice = PREFIX ? part.slice : a.prefix_slices + part.slice;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float m_all = -FLT_MAX, l_all = 0.f, f[kWaves];
@@ -283,9 +346,10 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(Args a, int tiles) {
       f[w] = __builtin_amdgcn_exp2f(f[w] - m_all);
       l_all += ml.y * f[w];
     }
-    if (first + t * 16 + col >= queries) continue;
-    const size_t at = ((size_t)row[t] * a.heads + head[t]) * total + at_slice;
-    if (!DIRECT && wave == 0 && grp == 0) a.sums[at] = make_float2(m_all, l_all);
+    const int m = part.first + t * 16 + col;
+    if (m >= part.queries) continue;
+    int row, head, unused;
+    part.query(a, m, &row, &head, &unused);
     for (int p = wave; p < HT / 2; p += kWaves) {
       float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -294,67 +358,287 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(Args a, int tiles) {
         o[0] += x.x * f[w]; o[1] += x.y * f[w]; o[2] += x.z * f[w]; o[3] += x.w * f[w];
         o[4] += y.x * f[w]; o[5] += y.y * f[w]; o[6] += y.z * f[w]; o[7] += y.w * f[w];
       }
-      if constexpr (DIRECT) {
-        const float inv = l_all == 0.f ? 0.f : 1.0f / l_all;
-        *(uint4*)(a.out + (size_t)row[t] * a.out_ld + (size_t)head[t] * a.out_head + p * 32 + grp * 8) =
-            make_uint4(pack2_bf16(o[0] * inv, o[1] * inv), pack2_bf16(o[2] * inv, o[3] * inv), pack2_bf16(o[4] * inv, o[5] * inv),
-                       pack2_bf16(o[6] * inv, o[7] * inv));
-      } else {
-        float4* to = (float4*)(a.part + at * HD + p * 32 + grp * 8);
-        to[0] = make_float4(o[0], o[1], o[2], o[3]);
-        to[1] = make_float4(o[4], o[5], o[6], o[7]);
-      }
+      leave<HD, DIRECT>(a, row, head, at_slice, p * 32 + grp * 8, o, m_all, l_all);
     }
   }
 }
 
-// The slices of a row of queries meet: a wave each, a lane HD/64 components.
-template <int HD>
+// Many queries: a wave owns QT tiles of 16, a block 64 QT, and its waves go through the keys together.  Each chunk comes through registers, where codes
+// are widened once for all, into one of two stages of LDS; the next one's pieces are on their way meanwhile.
+template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_many_kernel(Args a, int tiles) {
+  constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
+  constexpr int KP = 2 * U * 64, ALL = KvChunk<ES, HD>::kBytes / 16, N = ALL / 256;   // pieces of 16 bytes: keys, all, a thread's
+  constexpr int KF = 2 * HB * 64, STAGE = KF + HT * 64 + 8;                              // of a stage: keys, all with the powers of two
+  static_assert(ALL % 256 == 0 && KP % 64 == 0, "a wave's pieces are keys or values");
+  __shared__ u32x4 lds[2 * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = lane >> 4, col = lane & 15;
+  Part part;
+  if (!part_of<64 * QT, PREFIX>(a, tiles, part)) return;
+  const int first = part.first + wave * 16 * QT;
+
+  bf16x8 qf[QT][HB];
+  int seen[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    int row, head;
+    part.query(a, first + t * 16 + col, &row, &head, &seen[t]);
+    const bf16_t* p = a.q + (size_t)row * a.q_ld + (size_t)head * a.q_head + grp * (HD / 4);
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) qf[t][hb] = as_bf16x8(*(const u32x4*)(p + hb * 8));
+  }
+  f32x4 acc[QT][HT];
+  float m_run[QT], l_run[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    m_run[t] = -FLT_MAX;
+    l_run[t] = 0.f;
+#pragma unroll
+    for (int h = 0; h < HT; ++h) acc[t][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int n = max(part.c_hi - part.c_lo, 0);
+  Pages pages = {part.table, part.c_lo, 1, part.c_hi - 1, a.place.shift, 0};
+  u32x4 piece[N];
+  uint32_t ks[N], vs1 = 0;
+  int there = 0;
+  auto load = [&](int i) {
+    const int page = pages.of(i, lane), no = part.c_lo + i;
+    there = page >= 0 && page < a.pages;
+    const size_t chunk = ((((size_t)(there ? page : 0) * a.place.kv_heads + part.kvh) << a.place.shift) + (no & ((1 << a.place.shift) - 1)));
+    const u32x4* p = (const u32x4*)(a.data + chunk * KvChunk<ES, HD>::kBytes);
+    const uint8_t* s = a.scales + chunk * 64;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int q = j * 256 + (int)threadIdx.x;
+      piece[j] = p[q];
+      if constexpr (ES == 1) {
+        if (j * 256 + wave * 64 < KP) ks[j] = s[(col >> 2) * 8 + (q / (U * 64)) * 4 + (col & 3)];
+      }
+    }
+    if (threadIdx.x < 32) vs1 = s[32 + threadIdx.x];
+  };
+  auto store = [&](u32x4* stage, int i) {
+    const int k0 = (part.c_lo + i) * 32 + grp * 8;
+    const bool tail = (part.c_lo + i) * 32 + 32 > part.s.keys || !there;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int q = j * 256 + wave * 64;      // (of the wave: keys or values)
+      if (q < KP) {
+        if constexpr (ES == 1) {
+          const int t2 = q / (U * 64), u = q / 64 % U;
+          const float f = power_of(ks[j]);
+          union { bf16x8 b; u32x4 v; } x, y;
+          x.b = widen8(piece[j][0], piece[j][1], f);
+          y.b = widen8(piece[j][2], piece[j][3], f);
+          stage[(t2 * HB + 2 * u) * 64 + lane] = x.v;
+          stage[(t2 * HB + 2 * u + 1) * 64 + lane] = y.v;
+        } else {
+          stage[q + lane] = piece[j];
+        }
+      } else {
+        if (tail) cut_values<ES>(piece[j], there ? part.s.keys - k0 : 0);
+        const int h = (q - KP) / 64;
+        if constexpr (ES == 1) {
+          union { bf16x8 b; u32x4 v; } x, y;
+          x.b = widen8(piece[j][0], piece[j][1], 1.f);
+          y.b = widen8(piece[j][2], piece[j][3], 1.f);
+          stage[KF + 2 * h * 64 + lane] = x.v;
+          stage[KF + (2 * h + 1) * 64 + lane] = y.v;
+        } else {
+          stage[KF + h * 64 + lane] = piece[j];
+        }
+      }
+    }
+    if (threadIdx.x < 32) ((float*)(stage + KF + HT * 64))[threadIdx.x] = power_of(vs1);
+  };
+  int there_now = 0;
+  if (n > 0) {
+    load(0);
+    store(lds, 0);
+    there_now = there;
+    if (n > 1) load(1);
+  }
+  block_barrier_nofence();
+  for (int i = 0; i < n; ++i) {
+    const u32x4* stage = lds + (i & 1) * STAGE;
+    const bool there_i = there_now;
+    if (i + 1 < n) {
+      store(lds + (~i & 1) * STAGE, i + 1);
+      there_now = there;
+      if (i + 2 < n) load(i + 2);
+    }
+    f32x4 sc[QT][2];
+#pragma unroll
+    for (int t2 = 0; t2 < 2; ++t2) {
+      bf16x8 kf[HB];
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb) kf[hb] = as_bf16x8(stage[(t2 * HB + hb) * 64 + lane]);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        sc[t][t2] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], qf[t][hb], sc[t][t2], 0, 0, 0);
+      }
+    }
+    float vs[8];
+    {
+      const float4 x = ((const float4*)(stage + KF + HT * 64))[grp * 2], y = ((const float4*)(stage + KF + HT * 64))[grp * 2 + 1];
+      vs[0] = x.x; vs[1] = x.y; vs[2] = x.z; vs[3] = x.w; vs[4] = y.x; vs[5] = y.y; vs[6] = y.z; vs[7] = y.w;
+    }
+    const int key0 = (part.c_lo + i) * 32, k0 = key0 + grp * 8;
+    const bool masked = key0 + 32 > part.seen_first || !there_i;
+    bf16x8 pf[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+      pf[t] = soften<HT>(sc[t], acc[t], m_run[t], l_run[t], vs, a.scale, masked, [&](int e) { return k0 + e >= seen[t] || !there_i; });
+#pragma unroll
+    for (int h = 0; h < HT; ++h) {
+      const bf16x8 vf = as_bf16x8(stage[KF + h * 64 + lane]);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) acc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[t][h], 0, 0, 0);
+    }
+    block_barrier_nofence();
+  }
+
+  const int at_slice = PREFIX ? part.slice : a.prefix_slices + part.slice;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float l = l_run[t];
+    l += other_row(l);
+    l += other_half(l);
+    const int m = first + t * 16 + col;
+    if (m >= part.queries) continue;
+    int row, head, unused;
+    part.query(a, m, &row, &head, &unused);
+#pragma unroll
+    for (int p = 0; p < HT / 2; ++p) {
+      const f32x4 x = acc[t][2 * p], y = acc[t][2 * p + 1];
+      const float o[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+      leave<HD, DIRECT>(a, row, head, at_slice, p * 32 + grp * 8, o, m_run[t], l);
+    }
+  }
+}
+
+// The slices of a row of queries meet in their order: W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
+// lane's each, two at most, so that all of them are on their way at once.
+constexpr int kSlicesMax = 64;    // of the prefix, and of a sequence's own keys
+
+template <int HD, int W>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(Args a) {
   constexpr int N = HD / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  typedef float fN __attribute__((ext_vector_type(N)));
+  __shared__ float meet[4][64][N];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave % W;
   const Seq s = seq_of(a, blockIdx.y);
-  const int i = blockIdx.x * 4 + wave, r = i / a.heads, head = i - r * a.heads;
-  if (r >= s.n) return;
+  const int i = blockIdx.x * (4 / W) + wave / W, r = i / a.heads, head = i - r * a.heads;
   const int total = a.prefix_slices + a.slices;
-  const int own = a.slices ? max(1, (((s.keys + 31) >> 5) + a.split - 1) / a.split) : 0;
-  const size_t at = ((size_t)(s.row0 + r) * a.heads + head) * total;
-  float m = -FLT_MAX, l = 0.f, o[N] = {};
-  for (int z = 0; z < a.prefix_slices + own; ++z) m = fmaxf(m, a.sums[at + z].x);
-  for (int z = 0; z < a.prefix_slices + own; ++z) {
-    const float2 ml = a.sums[at + z];
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    l += ml.y * f;
+  const int own = max(1, (((s.keys + 31) >> 5) + a.split - 1) / a.split), n = a.prefix_slices + own;
+  const bool live = r < s.n;
+  float o[N] = {}, inv = 0.f;
+  if (live) {
+    const size_t at = ((size_t)(s.row0 + r) * a.heads + head) * total;
+    float2 x = make_float2(-FLT_MAX, 0.f), y = x;
+    if (lane < n) x = a.sums[at + lane];
+    if (lane + 64 < n) y = a.sums[at + lane + 64];
+    const float m = wave_max_dpp(fmaxf(x.x, y.x));
+    const float fx = __builtin_amdgcn_exp2f(x.x - m), fy = __builtin_amdgcn_exp2f(y.x - m);
+    const float l = wave_sum_dpp(fmaf(x.y, fx, y.y * fy));
+    inv = l == 0.f ? 0.f : 1.0f / l;
+    const float* part = a.part + at * HD + lane * N;
+    auto weight = [&](int z) {
+      return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(z < 64 ? fx : fy), z & 63));
+    };
+    int z = sub;
+    for (; z + 3 * W < n; z += 4 * W) {
+      fN v[4];
 #pragma unroll
-    for (int e = 0; e < N; ++e) o[e] += a.part[(at + z) * HD + lane * N + e] * f;
+      for (int k = 0; k < 4; ++k) v[k] = *(const fN*)(part + (size_t)(z + k * W) * HD);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] += v[k][e] * weight(z + k * W);
+    }
+    for (; z < n; z += W) {
+      const fN v = *(const fN*)(part + (size_t)z * HD);
+#pragma unroll
+      for (int e = 0; e < N; ++e) o[e] += v[e] * weight(z);
+    }
   }
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  bf16_t* to = a.out + (size_t)(s.row0 + r) * a.out_ld + (size_t)head * a.out_head + lane * N;
+  if constexpr (W > 1) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) to[e] = f32_to_bf16(o[e] * inv);
+    for (int e = 0; e < N; ++e) meet[wave][lane][e] = o[e];
+    __syncthreads();
+    if (!live || sub != 0) return;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      o[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) o[e] += meet[wave + w][lane][e];
+    }
+  }
+  if (!live) return;
+  bf16_t* to = a.out + (size_t)(s.row0 + r) * a.out_ld + (size_t)head * a.out_head + lane * N;
+  if constexpr (N == 2) *(uint32_t*)to = pack2_bf16(o[0] * inv, o[1] * inv);
+  else *to = f32_to_bf16(o[0] * inv);
 }
 
 namespace {
 
-// how the keys are cut
-struct Plan { int split, slices, prefix_split, prefix_slices; };
-int cut(int chunks, long others, int* split) {
-  const long want = max(1L, 1024 / max(others, 1L));                       // blocks that fill the compute units
-  const int most = max(1, chunks / 8);                                     // two chunks to a wave at least
-  const int n = (int)min(want, (long)most);
-  *split = (chunks + n - 1) / n;
-  return (chunks + *split - 1) / *split;
+// How a call's queries of one sequence and kv head, or of the prefix, are cut into blocks, and the keys into slices.
+struct Cut {
+  bool many;
+  int qt, tiles, split, slices;
+};
+Cut cut(long queries, int chunks, long others) {
+  Cut c;
+  c.many = queries > 48;
+  if (c.many) {
+    c.qt = queries <= 64 ? 1 : queries <= 128 || (queries > 192 && queries <= 256) ? 2 : 3;
+    c.tiles = (int)((queries + 64 * c.qt - 1) / (64 * c.qt));
+  } else {
+    c.qt = (int)max(1L, (queries + 15) / 16);
+    c.tiles = 1;
+  }
+  const long want = (c.many ? 512 : 1024) / max(others * c.tiles, 1L);     // blocks that fill the compute units
+  const long most = max(1, chunks / 8);                                    // (8 chunks to a slice at least)
+  const int n = (int)max(1L, min(min(want, most), (long)kSlicesMax));
+  c.split = (chunks + n - 1) / n;
+  c.slices = (chunks + c.split - 1) / c.split;
+  return c;
 }
+struct Plan { Cut own, prefix; };
 Plan plan_of(const KvCache& c, const KvAttention& a) {
-  const int group = a.heads / c.kv_heads;
-  const long tiles = ((long)a.max_rows * group + 15) / 16, all = ((long)a.rows * group + 15) / 16;
+  const long group = a.heads / c.kv_heads;
   Plan p = {};
-  p.slices = cut(max(1, (a.max_keys + 31) / 32), (long)c.kv_heads * a.seqs * tiles, &p.split);
-  if (a.prefix_len > 0) p.prefix_slices = cut((a.prefix_len + 31) / 32, c.kv_heads * all, &p.prefix_split);
+  p.own = cut(a.max_rows * group, max(1, (a.max_keys + 31) / 32), (long)c.kv_heads * a.seqs);
+  if (a.prefix_len > 0) p.prefix = cut(a.rows * group, (a.prefix_len + 31) / 32, c.kv_heads);
   return p;
 }
 size_t part_bytes(const KvCache& c, const KvAttention& a, int slices) {
   return ((size_t)a.rows * a.heads * slices * c.head_dim * 4 + 255) / 256 * 256;
+}
+
+template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
+void launch_few(const Args& a, long blocks, hipStream_t s) {
+  constexpr int lds = kWaves * QT * (HD / 16 * 64 + 32) * 16;
+  static std::atomic<uint64_t> allowed{0};
+  if (lds > 65536) allow_lds((const void*)kv_attention_few_kernel<ES, HD, QT, PREFIX, DIRECT>, lds, allowed);
+  kv_attention_few_kernel<ES, HD, QT, PREFIX, DIRECT><<<(unsigned)blocks, 256, lds, s>>>(a, 1);
+}
+template <int ES, int HD, bool PREFIX, bool DIRECT>
+void launch_cut(const Args& a, const Cut& c, hipStream_t s) {
+  const long blocks = (long)a.place.kv_heads * (PREFIX ? 1 : a.seqs) * c.slices * c.tiles;
+  if (c.many) {
+    if (c.qt == 1) kv_attention_many_kernel<ES, HD, 1, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
+    else if (c.qt == 2) kv_attention_many_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
+    else kv_attention_many_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
+  } else {
+    if (c.qt == 1) launch_few<ES, HD, 1, PREFIX, DIRECT>(a, blocks, s);
+    else if (c.qt == 2) launch_few<ES, HD, 2, PREFIX, DIRECT>(a, blocks, s);
+    else launch_few<ES, HD, 3, PREFIX, DIRECT>(a, blocks, s);
+  }
 }
 
 template <int ES, int HD>
@@ -369,30 +653,23 @@ void launch(const KvCache& c, const KvAttention& k, const Plan& p, void* workspa
   a.data = c.data; a.scales = c.data + kv_code_bytes(c);
   a.place = {c.page == 32 ? 0 : c.page == 64 ? 1 : c.page == 128 ? 2 : 3, c.kv_heads};
   a.pages = c.pages;
-  a.split = p.split; a.slices = p.slices; a.prefix_split = p.prefix_split; a.prefix_slices = p.prefix_slices;
-  const int total = p.slices + p.prefix_slices;
+  a.split = p.own.split; a.slices = p.own.slices; a.prefix_split = p.prefix.split; a.prefix_slices = p.prefix.slices;
+  const int total = a.slices + a.prefix_slices;
   a.part = (float*)workspace;
   a.sums = (float2*)((char*)workspace + part_bytes(c, k, total));
-  constexpr int QT = 1;
-  constexpr size_t lds = (size_t)kWaves * QT * (HD / 16 * 64 + 32) * 16;
-  const long tiles = ((long)a.max_rows * a.group + 16 * QT - 1) / (16 * QT);
-  if (total == 1) {
-    kv_attention_kernel<ES, HD, QT, false, true><<<(unsigned)(c.kv_heads * a.slices * tiles * a.seqs), 256, lds, s>>>(a, (int)tiles);
-    return;
-  }
-  if (p.prefix_slices) {
-    const long all = ((long)a.rows * a.group + 16 * QT - 1) / (16 * QT);
-    kv_attention_kernel<ES, HD, QT, true, false><<<(unsigned)(c.kv_heads * a.prefix_slices * all), 256, lds, s>>>(a, (int)all);
-  }
-  kv_attention_kernel<ES, HD, QT, false, false><<<(unsigned)(c.kv_heads * a.slices * tiles * a.seqs), 256, lds, s>>>(a, (int)tiles);
-  kv_attention_join_kernel<HD><<<dim3((unsigned)(((long)a.max_rows * a.heads + 3) / 4), a.seqs), 256, 0, s>>>(a);
+  if (total == 1) return launch_cut<ES, HD, false, true>(a, p.own, s);
+  if (a.prefix_slices) launch_cut<ES, HD, true, false>(a, p.prefix, s);
+  launch_cut<ES, HD, false, false>(a, p.own, s);
+  const long queries = (long)a.max_rows * a.heads;
+  if (total > 8) kv_attention_join_kernel<HD, 4><<<dim3((unsigned)queries, a.seqs), 256, 0, s>>>(a);
+  else kv_attention_join_kernel<HD, 1><<<dim3((unsigned)((queries + 3) / 4), a.seqs), 256, 0, s>>>(a);
 }
 
 }  // namespace
 
 size_t kv_attention_workspace(const KvCache& c, const KvAttention& a) {
   const Plan p = plan_of(c, a);
-  const int total = p.slices + p.prefix_slices;
+  const int total = p.own.slices + p.prefix.slices;
   return total == 1 ? 0 : part_bytes(c, a, total) + (size_t)a.rows * a.heads * total * 8;
 }
 
