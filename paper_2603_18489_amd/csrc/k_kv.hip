@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows a) {
   const int first = has_run ? t.first[run] : 0, run_slot = has_run ? t.slot[Tile<ROWS>::SIDE + first] : 0;
   for (int h = blockIdx.y * 4 + (threadIdx.x >> 6); h < a.place.kv_heads; h += gridDim.y * 4) {
     // values of the runs: 8 tokens x 8 components
-    if (has_run) {
+    if (has_run && blockIdx.z == 0) {
       const T* p = (const T*)a.v + (size_t)(row0 + first) * a.v_ld + (size_t)h * a.v_head + cv;
       float v[8][8];
 #pragma unroll
@@ -270,29 +270,31 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows a) {
       if (cv == 0) *(uint2*)(a.scales + chunk * 64 + 32 + (run_slot & 31)) = make_uint2(s[0], s[1]);
     }
     // keys, and values of the rows in no run: 16 components of a token
-#pragma unroll 2
-    for (int i = 0; i < ROWS * LK / 64; ++i) {
+    for (int i = blockIdx.z; i < ROWS * LK / 64; i += gridDim.z) {
       const int j = i * (64 / LK) + lane / LK, c0 = lane % LK * 16, slot = t.slot[Tile<ROWS>::SIDE + j], w = slot & 31;
-      if (slot < 0) continue;
-      const size_t chunk = a.place.chunk(slot, h);
-      uint8_t* to = a.data + chunk * L::kBytes;
-      float v[16];
-      uint32_t words[4 * ES];
-      load_values((const T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide, v);
-      uint32_t s = stored<ES, 16, HD>(v, words, kNaN);
+      const bool single = (t.single >> j) & 1;
+      if (slot >= 0) {
+        const size_t chunk = a.place.chunk(slot, h);
+        uint8_t* to = a.data + chunk * L::kBytes;
+        float k[16], v[16];
+        uint32_t words[4 * ES];
+        load_values((const T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide, k);
+        if (single) load_values((const T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide, v);
+        uint32_t s = stored<ES, 16, HD>(k, words, kNaN);
 #pragma unroll
-      for (int n = 0; n < ES; ++n)
-        *(uint4*)(to + L::key_at(w, c0 + n * 8)) = make_uint4(words[4 * n], words[4 * n + 1], words[4 * n + 2], words[4 * n + 3]);
-      if (c0 == 0) a.scales[chunk * 64 + w] = (uint8_t)s;
-      if (!((t.single >> j) & 1)) continue;
-      load_values((const T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide, v);
-      s = stored<ES, 16, HD>(v, words, 0);
+        for (int n = 0; n < ES; ++n)
+          *(uint4*)(to + L::key_at(w, c0 + n * 8)) = make_uint4(words[4 * n], words[4 * n + 1], words[4 * n + 2], words[4 * n + 3]);
+        if (c0 == 0) a.scales[chunk * 64 + w] = (uint8_t)s;
+        if (single) {
+          s = stored<ES, 16, HD>(v, words, 0);
 #pragma unroll
-      for (int n = 0; n < 16; ++n) {
-        if constexpr (ES == 1) to[L::value_at(w, c0 + n)] = (uint8_t)(words[n >> 2] >> (8 * (n & 3)));
-        else *(uint16_t*)(to + L::value_at(w, c0 + n)) = (uint16_t)(words[n >> 1] >> (16 * (n & 1)));
+          for (int n = 0; n < 16; ++n) {
+            if constexpr (ES == 1) to[L::value_at(w, c0 + n)] = (uint8_t)(words[n >> 2] >> (8 * (n & 3)));
+            else *(uint16_t*)(to + L::value_at(w, c0 + n)) = (uint16_t)(words[n >> 1] >> (16 * (n & 1)));
+          }
+          if (c0 == 0) a.scales[chunk * 64 + 32 + w] = (uint8_t)s;
+        }
       }
-      if (c0 == 0) a.scales[chunk * 64 + 32 + w] = (uint8_t)s;
     }
   }
 }
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvRows a) {
   const bool has_run = run < t.runs;
   const int first = has_run ? t.first[run] : 0, run_slot = has_run ? t.slot[Tile<ROWS>::SIDE + first] : 0;
   for (int h = blockIdx.y * 4 + (threadIdx.x >> 6); h < a.place.kv_heads; h += gridDim.y * 4) {
-    if (has_run) {
+    if (has_run && blockIdx.z == 0) {
       const size_t chunk = a.place.chunk(run_slot, h);
       const uint8_t* from = a.data + chunk * L::kBytes;
       uint32_t w[8][2 * ES], o[8][2 * ES];
@@ -333,38 +335,36 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvRows a) {
         store_values(p + (size_t)r * a.v_ld, a.wide, v);
       }
     }
-#pragma unroll 2
-    for (int i = 0; i < ROWS * LK / 64; ++i) {
+    for (int i = blockIdx.z; i < ROWS * LK / 64; i += gridDim.z) {
       const int j = i * (64 / LK) + lane / LK, c0 = lane % LK * 16, slot = t.slot[Tile<ROWS>::SIDE + j], w = slot & 31;
-      if (row0 + j >= a.rows) continue;
-      T* k = (T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0;
-      T* v = (T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0;
-      float x[16] = {};
-      if (slot < 0) {
-        store_values(k, a.wide, x);
-        store_values(v, a.wide, x);
-        continue;
-      }
-      const size_t chunk = a.place.chunk(slot, h);
-      const uint8_t* from = a.data + chunk * L::kBytes;
-      uint32_t words[4 * ES];
+      if (row0 + j < a.rows) {
+        const bool there = slot >= 0, single = (t.single >> j) & 1;
+        float k[16] = {}, v[16] = {};
+        if (there) {
+          const size_t chunk = a.place.chunk(slot, h);
+          const uint8_t* from = a.data + chunk * L::kBytes;
+          uint32_t kw[4 * ES], vw[4 * ES];
 #pragma unroll
-      for (int n = 0; n < ES; ++n) {
-        const uint4 u = *(const uint4*)(from + L::key_at(w, c0 + n * 8));
-        words[4 * n] = u.x; words[4 * n + 1] = u.y; words[4 * n + 2] = u.z; words[4 * n + 3] = u.w;
-      }
-      values_of<ES>(words, a.scales[chunk * 64 + w], x);
-      store_values(k, a.wide, x);
-      if (!((t.single >> j) & 1)) continue;
+          for (int n = 0; n < ES; ++n) {
+            const uint4 u = *(const uint4*)(from + L::key_at(w, c0 + n * 8));
+            kw[4 * n] = u.x; kw[4 * n + 1] = u.y; kw[4 * n + 2] = u.z; kw[4 * n + 3] = u.w;
+          }
+          const uint32_t ks = a.scales[chunk * 64 + w], vs = a.scales[chunk * 64 + 32 + w];
 #pragma unroll
-      for (int n = 0; n < 4 * ES; ++n) words[n] = 0;
+          for (int n = 0; n < 4 * ES; ++n) vw[n] = 0;
+          if (single) {
 #pragma unroll
-      for (int n = 0; n < 16; ++n) {
-        if constexpr (ES == 1) words[n >> 2] |= (uint32_t)from[L::value_at(w, c0 + n)] << (8 * (n & 3));
-        else words[n >> 1] |= (uint32_t) * (const uint16_t*)(from + L::value_at(w, c0 + n)) << (16 * (n & 1));
+            for (int n = 0; n < 16; ++n) {
+              if constexpr (ES == 1) vw[n >> 2] |= (uint32_t)from[L::value_at(w, c0 + n)] << (8 * (n & 3));
+              else vw[n >> 1] |= (uint32_t) * (const uint16_t*)(from + L::value_at(w, c0 + n)) << (16 * (n & 1));
+            }
+          }
+          values_of<ES>(kw, ks, k);
+          values_of<ES>(vw, vs, v);
+        }
+        store_values((T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide, k);
+        if (single || !there) store_values((T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide, v);
       }
-      values_of<ES>(words, a.scales[chunk * 64 + 32 + w], x);
-      store_values(v, a.wide, x);
     }
   }
 }
@@ -381,15 +381,15 @@ static KvRows rows_of(const KvCache& c, const void* k, const void* v, bool bf16,
   return a;
 }
 
-// Blocks that share a tile of rows, four heads at a time: as many as there are heads for where tiles are few.  (Each of them looks for rows that
-// name the same slot.)
-static int blocks_of_a_tile(int tiles, int heads) { return min((heads + 3) / 4, max(1, 2048 / max(tiles, 1))); }
+// Blocks that share a tile of rows: as many as there are heads for, four to a block, and four beside each other that share the rows in no run, as far as that
+// makes no more than 2048 blocks.  (Each of them looks for rows that name the same slot.)
+static dim3 kv_grid(int tiles, int heads) {
+  const int y = min((heads + 3) / 4, max(1, 2048 / tiles));
+  return dim3(tiles, y, tiles * y <= 512 ? 4 : 1);
+}
 
-#define EC_KV_LAUNCH(KERNEL, T, ES, HD)                                                                  \
-  do {                                                                                                   \
-    const int tiles = (rows + kTileRows<HD> - 1) / kTileRows<HD>;                                        \
-    KERNEL<T, ES, HD><<<dim3(tiles, blocks_of_a_tile(tiles, c.kv_heads)), 256, 0, s>>>(a);               \
-  } while (0)
+#define EC_KV_LAUNCH(KERNEL, T, ES, HD) \
+  KERNEL<T, ES, HD><<<kv_grid((rows + kTileRows<HD> - 1) / kTileRows<HD>, c.kv_heads), 256, 0, s>>>(a)
 #define EC_KV_PICK(KERNEL)                                                                      \
   do {                                                                                          \
     if (bf16) {                                                                                 \

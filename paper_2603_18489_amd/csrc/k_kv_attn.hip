@@ -39,6 +39,7 @@ __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) {
   return c.b;
 }
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }   // (255: infinity, which makes NaN of 0)
+__device__ __forceinline__ uint32_t byte_of(uint32_t word, int n) { return (word >> (8 * (n & 3))) & 255u; }
 
 // what a kernel knows of the call
 struct Args {
@@ -128,36 +129,23 @@ struct Pages {
   }
 };
 
-// Scores of 16 queries and 32 keys (S^T: a lane has 8 neighbouring keys of query lane & 15) to the probabilities that multiply the values: the
-// running maximum m and sum l move on, acc with them.  hidden(e): whether the lane's key e is not to be seen; asked only where `masked`.
-template <int HT, typename Hidden>
-__device__ __forceinline__ bf16x8 soften(f32x4 (&sc)[2], f32x4 (&acc)[HT], float& m, float& l, const float (&vs)[8], float scale, bool masked,
-                                         Hidden hidden) {
-  if (masked) {
+// The exponentials' reference is a maximum that lags behind by up to 2^kLag: moving it multiplies a whole tile of results, and with a lag the
+// first chunks settle it for most queries.  (Probabilities of up to 2^kLag are as exact as those of up to 1: all of this is floating point.)
+constexpr float kLag = 8.f;
+
+// largest of the scores of 16 queries and 32 keys (S^T: a lane has 8 neighbouring keys of query lane & 15), in every lane of the query
+__device__ __forceinline__ float top_score(const f32x4 (&sc)[2], float scale) {
+  return max_of_swap32(max_of_swap16(max_of_8(sc[0], sc[1]))) * scale;
+}
+// the maximum m moves to mx, and what has been added up with it
+template <int HT, typename Sum> __device__ __forceinline__ void move_top(f32x4 (&acc)[HT], float& m, Sum& l, float mx) {
+  const float m_new = max_of(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
+  m = m_new;
+  l *= alpha;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (hidden(e)) sc[e >> 2][e & 3] = -INFINITY;
-  }
-  const float mx = max_of_swap32(max_of_swap16(max_of_8(sc[0], sc[1]))) * scale;
-  if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
-    const float m_new = max_of(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
-    m = m_new;
-    l *= alpha;
-#pragma unroll
-    for (int h = 0; h < HT; ++h) acc[h] *= alpha;
-  }
-  float p[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], scale, -m));
-    l += p[e];
-    p[e] *= vs[e];
-  }
-  if (masked) {   // (a hidden key's power of two may be none)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (hidden(e)) p[e] = 0.f;
-  }
+  for (int h = 0; h < HT; ++h) acc[h] *= alpha;
+}
+__device__ __forceinline__ bf16x8 pack8(const float (&p)[8]) {
   return u4_as_bf16x8(make_uint4(pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]), pack2_bf16(p[4], p[5]), pack2_bf16(p[6], p[7])));
 }
 
@@ -195,22 +183,27 @@ template <int ES, int HD> struct Chunk {
   u32x4 k[2 * U], v[V];
   uint32_t ks[2];
   u32x2 vs;
-  int there;
-  __device__ __forceinline__ void load(const Args& a, int page, int no, int kvh, int lane) {
+  const u32x4* data;
+  const uint8_t* scales;
+  bool there;
+  __device__ __forceinline__ void at(const Args& a, int page, int no, int kvh) {
     there = page >= 0 && page < a.pages;
     const size_t chunk = ((((size_t)(there ? page : 0) * a.place.kv_heads + kvh) << a.place.shift) + (no & ((1 << a.place.shift) - 1)));
-    const u32x4* p = (const u32x4*)(a.data + chunk * KvChunk<ES, HD>::kBytes) + lane;
+    data = (const u32x4*)(a.data + chunk * KvChunk<ES, HD>::kBytes);
+    scales = a.scales + chunk * 64;
+  }
+  __device__ __forceinline__ void keys(int lane) {
 #pragma unroll
-    for (int i = 0; i < 2 * U; ++i) k[i] = p[i * 64];
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = p[(2 * U + i) * 64];
-    const uint8_t* s = a.scales + chunk * 64;
-    const int w = ((lane & 15) >> 2) * 8 + (lane & 3);
+    for (int i = 0; i < 2 * U; ++i) k[i] = data[i * 64 + lane];
     if constexpr (ES == 1) {
-      ks[0] = s[w];
-      ks[1] = s[w + 4];
+      ks[0] = ((const uint32_t*)scales)[((lane & 15) >> 2) * 2];
+      ks[1] = ((const uint32_t*)scales)[((lane & 15) >> 2) * 2 + 1];
     }
-    vs = *(const u32x2*)(s + 32 + (lane >> 4) * 8);
+  }
+  __device__ __forceinline__ void values(int lane) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = data[(2 * U + i) * 64 + lane];
+    vs = *(const u32x2*)(scales + 32 + (lane >> 4) * 8);
   }
 };
 
@@ -219,19 +212,24 @@ template <int ES, int HD> struct Chunk {
 constexpr int kWaves = 4;
 
 // Few queries: up to 48 of a sequence and kv head.  A block's waves go through the chunks of its slice in turn, each with all QT tiles of 16
-// queries and a chunk's pieces in registers, the next chunk's on their way, and meet in LDS.
+// queries and a chunk's pieces in registers, and meet in LDS.  The next chunk's keys are on their way from when this one's are used, the values too; one tile of
+// queries leaves registers for a second chunk.  The power of two of a key's values multiplies its probability.
+// With one tile the matrix cores wait for memory, so that a probability can be two bfloat16 numbers, 2^-17 together, instead of one.
 // DIRECT: there is one slice, and the block writes the result.
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
-__global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a, int tiles) {
   constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
   typedef Chunk<ES, HD> C;
-  extern __shared__ float4 lds[];
+  constexpr int SLOT = HT * 64 + 32;   // float4 of a wave's part of a tile
+  constexpr bool PARKED = QT > 2;      // queries in LDS, as a third tile's registers would spill others
+  __shared__ float4 lds[kWaves * SLOT];
+  __shared__ u32x4 parked[PARKED ? QT * HB * 64 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane >> 4, col = lane & 15;
   Part part;
   if (!part_of<16 * QT, PREFIX>(a, tiles, part)) return;
 
-  bf16x8 qf[QT][HB];
+  bf16x8 qf[PARKED ? 1 : QT][HB];
   int seen[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -239,8 +237,12 @@ __global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles
     part.query(a, part.first + t * 16 + col, &row, &head, &seen[t]);
     const bf16_t* p = a.q + (size_t)row * a.q_ld + (size_t)head * a.q_head + grp * (HD / 4);
 #pragma unroll
-    for (int hb = 0; hb < HB; ++hb) qf[t][hb] = as_bf16x8(*(const u32x4*)(p + hb * 8));
+    for (int hb = 0; hb < HB; ++hb) {
+      if constexpr (!PARKED) qf[t][hb] = as_bf16x8(*(const u32x4*)(p + hb * 8));
+      else if (hb % kWaves == wave) parked[(t * HB + hb) * 64 + lane] = *(const u32x4*)(p + hb * 8);
+    }
   }
+  if constexpr (PARKED) __syncthreads();
   f32x4 acc[QT][HT];
   float m_run[QT], l_run[QT];
 #pragma unroll
@@ -254,13 +256,12 @@ __global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles
   const int from = part.c_lo + wave;                                                        // this wave's first chunk
   const int mine = from < part.c_hi ? (part.c_hi - from + kWaves - 1) / kWaves : 0;         // and how many it has
   Pages pages = {part.table, from, kWaves, from + kWaves * (mine - 1), a.place.shift, 0};
-  auto fetch = [&](C& c, int i) {
+  auto place = [&](C& c, int i) {
     const int n = min(i, mine - 1);     // (behind the last chunk it comes once more, from the cache)
-    c.load(a, pages.of(n, lane), from + kWaves * n, part.kvh, lane);
+    c.at(a, pages.of(n, lane), from + kWaves * n, part.kvh);
   };
-  auto step = [&](C& c, int i) {
-    const int key0 = (from + kWaves * i) * 32, k0 = key0 + grp * 8;
-    f32x4 sc[QT][2];
+  f32x4 sc[QT][2];
+  auto score = [&](const C& c) {
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
       bf16x8 kf[HB];
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles
       for (int u = 0; u < U; ++u) {
         const u32x4 k = c.k[t2 * U + u];
         if constexpr (ES == 1) {
-          const float f = power_of(c.ks[t2]);
+          const float f = power_of(byte_of(c.ks[t2], lane));
           kf[2 * u] = widen8(k[0], k[1], f);
           kf[2 * u + 1] = widen8(k[2], k[3], f);
         } else {
@@ -279,82 +280,144 @@ __global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles
       for (int t = 0; t < QT; ++t) {
         sc[t][t2] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], qf[t][hb], sc[t][t2], 0, 0, 0);
+        for (int hb = 0; hb < HB; ++hb) {
+          const bf16x8 q = PARKED ? as_bf16x8(parked[(t * HB + hb) * 64 + lane]) : qf[PARKED ? 0 : t][hb];
+          sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], q, sc[t][t2], 0, 0, 0);
+        }
       }
     }
-    const bool masked = key0 + 32 > part.seen_first || !c.there;
+  };
+  auto attend = [&](C& c, int i, bool there) {
+    const int key0 = (from + kWaves * i) * 32, k0 = key0 + grp * 8;
+    const bool masked = key0 + 32 > part.seen_first || !there;
     if (masked) {
-      const int live = c.there ? part.s.keys - k0 : 0;
+      const int live = there ? part.s.keys - k0 : 0;
 #pragma unroll
       for (int h = 0; h < C::V; ++h) cut_values<ES>(c.v[h], live);
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (k0 + e >= seen[t] || !there) sc[t][e >> 2][e & 3] = -INFINITY;
     }
     float vs[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) vs[e] = power_of((c.vs[e >> 2] >> (8 * (e & 3))) & 255u);
-    bf16x8 pf[QT];
+    bf16x8 pf[QT], pl[QT];
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
-      pf[t] = soften<HT>(sc[t], acc[t], m_run[t], l_run[t], vs, a.scale, masked, [&](int e) { return k0 + e >= seen[t] || !c.there; });
+    for (int t = 0; t < QT; ++t) {
+      const float mx = top_score(sc[t], a.scale);
+      if (__builtin_amdgcn_ballot_w64(mx > m_run[t] + kLag) != 0) move_top(acc[t], m_run[t], l_run[t], mx);
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e >> 2][e & 3], a.scale, -m_run[t]));
+        l_run[t] += p[e];
+        p[e] *= vs[e];
+      }
+      if (masked) {   // (a hidden key's power of two may be none)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (k0 + e >= seen[t] || !there) p[e] = 0.f;
+      }
+      pf[t] = pack8(p);
+      if constexpr (QT == 1) {
+        union { bf16x8 b; uint32_t u[4]; } c = {pf[t]};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] -= __uint_as_float(e & 1 ? c.u[e >> 1] & 0xffff0000u : c.u[e >> 1] << 16);
+        pl[t] = pack8(p);
+      }
+    }
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
       bf16x8 vf;
       if constexpr (ES == 1) vf = h & 1 ? widen8(c.v[h >> 1][2], c.v[h >> 1][3], 1.f) : widen8(c.v[h >> 1][0], c.v[h >> 1][1], 1.f);
       else vf = as_bf16x8(c.v[h]);
 #pragma unroll
-      for (int t = 0; t < QT; ++t) acc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[t][h], 0, 0, 0);
+      for (int t = 0; t < QT; ++t) {
+        acc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[t][h], 0, 0, 0);
+        if constexpr (QT == 1) acc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[t], acc[t][h], 0, 0, 0);
+      }
     }
   };
-  C one, two;
-  if (mine > 0) fetch(one, 0);
-  for (int i = 0; i < mine; i += 2) {
-    fetch(two, i + 1);
-    __builtin_amdgcn_sched_barrier(0);
-    step(one, i);
-    __builtin_amdgcn_sched_barrier(0);
-    fetch(one, i + 2);
-    __builtin_amdgcn_sched_barrier(0);
-    if (i + 1 < mine) step(two, i + 1);
-    __builtin_amdgcn_sched_barrier(0);
+  if constexpr (QT == 1) {
+    C one, two;
+    if (mine > 0) {
+      place(one, 0);
+      one.keys(lane);
+      one.values(lane);
+    }
+    for (int i = 0; i < mine; i += 2) {
+      place(two, i + 1);
+      two.keys(lane);
+      two.values(lane);
+      __builtin_amdgcn_sched_barrier(0);
+      score(one);
+      attend(one, i, one.there);
+      __builtin_amdgcn_sched_barrier(0);
+      place(one, i + 2);
+      one.keys(lane);
+      one.values(lane);
+      __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < mine) {
+        score(two);
+        attend(two, i + 1, two.there);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  } else {
+    C c;
+    if (mine > 0) {
+      place(c, 0);
+      c.keys(lane);
+      c.values(lane);
+    }
+    for (int i = 0; i < mine; ++i) {
+      score(c);
+      __builtin_amdgcn_sched_barrier(0);
+      const bool there = c.there;
+      place(c, i + 1);
+      c.keys(lane);
+      __builtin_amdgcn_sched_barrier(0);
+      attend(c, i, there);
+      __builtin_amdgcn_sched_barrier(0);
+      c.values(lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
-  // ---- the waves' parts meet: (m, sum, O) of each, in their order
-  constexpr int SLOT = QT * (HT * 64 + 32);   // float4
+  // ---- the waves' parts meet, tile by tile: (m, sum, O) of each, in their order
   float4* slot = lds + (size_t)wave * SLOT;
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    float l = l_run[t];
-    l += other_row(l);
-    l += other_half(l);
-    ((float2*)(slot + QT * HT * 64))[t * 64 + lane] = make_float2(m_run[t], l);
-#pragma unroll
-    for (int h = 0; h < HT; ++h) slot[(t * HT + h) * 64 + lane] = make_float4(acc[t][h][0], acc[t][h][1], acc[t][h][2], acc[t][h][3]);
-  }
-  __syncthreads();
   const int at_slice = PREFIX ? part.slice : a.prefix_slices + part.slice;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
+    if (t > 0) __syncthreads();
+    float l = l_run[t];
+    l += other_row(l);
+    l += other_half(l);
+    ((float2*)(slot + HT * 64))[lane] = make_float2(m_run[t], l);
+#pragma unroll
+    for (int h = 0; h < HT; ++h) slot[h * 64 + lane] = make_float4(acc[t][h][0], acc[t][h][1], acc[t][h][2], acc[t][h][3]);
+    __syncthreads();
     float m_all = -FLT_MAX, l_all = 0.f, f[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float2 ml = ((const float2*)(lds + (size_t)w * SLOT + QT * HT * 64))[t * 64 + lane];
-      f[w] = ml.x;
-      m_all = fmaxf(m_all, ml.x);
+      f[w] = ((const float2*)(lds + (size_t)w * SLOT + HT * 64))[lane].x;
+      m_all = fmaxf(m_all, f[w]);
     }
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float2 ml = ((const float2*)(lds + (size_t)w * SLOT + QT * HT * 64))[t * 64 + lane];
       f[w] = __builtin_amdgcn_exp2f(f[w] - m_all);
-      l_all += ml.y * f[w];
+      l_all += ((const float2*)(lds + (size_t)w * SLOT + HT * 64))[lane].y * f[w];
     }
     const int m = part.first + t * 16 + col;
-    if (m >= part.queries) continue;
     int row, head, unused;
     part.query(a, m, &row, &head, &unused);
-    for (int p = wave; p < HT / 2; p += kWaves) {
+    for (int p = wave; p < HT / 2 && m < part.queries; p += kWaves) {
       float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        const float4 x = lds[(size_t)w * SLOT + (t * HT + 2 * p) * 64 + lane], y = lds[(size_t)w * SLOT + (t * HT + 2 * p + 1) * 64 + lane];
+        const float4 x = lds[(size_t)w * SLOT + 2 * p * 64 + lane], y = lds[(size_t)w * SLOT + (2 * p + 1) * 64 + lane];
         o[0] += x.x * f[w]; o[1] += x.y * f[w]; o[2] += x.z * f[w]; o[3] += x.w * f[w];
         o[4] += y.x * f[w]; o[5] += y.y * f[w]; o[6] += y.z * f[w]; o[7] += y.w * f[w];
       }
@@ -363,13 +426,32 @@ __global__ __launch_bounds__(256) void kv_attention_few_kernel(Args a, int tiles
   }
 }
 
+// 16 codes of values, of 8 keys whose powers of two are the bytes of vs, as bfloat16
+__device__ __forceinline__ void widen_values(u32x4 v, u32x2 vs, u32x4& x, u32x4& y) {
+  union { bf16x2 h; uint32_t u; } a, b;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {   // keys 2 k and 2 k + 1
+    const uint32_t two = vs[k >> 1] >> (16 * (k & 1));
+    const float f = power_of(two & 255u), g = power_of((two >> 8) & 255u);
+    const uint32_t w = v[k >> 1], z = v[2 + (k >> 1)];
+    a.h = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false);
+    b.h = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, g, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, g, false);
+    x[k] = (a.u & 0xffffu) | (b.u & 0xffff0000u);
+    a.h = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(z, f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(z, f, false);
+    b.h = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(z, g, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(z, g, false);
+    y[k] = (a.u & 0xffffu) | (b.u & 0xffff0000u);
+  }
+}
+
 // Many queries: a wave owns QT tiles of 16, a block 64 QT, and its waves go through the keys together.  Each chunk comes through registers, where codes
-// are widened once for all, into one of two stages of LDS; the next one's pieces are on their way meanwhile.
+// are widened once for all, values with their powers of two, into one of two stages of LDS; the next one's pieces are on their way meanwhile.  The
+// probabilities' sums are a product of P^T with ones: what is rounded is what is added up.
+// Chunks that hold a key which some query does not see, or values that are NaN, go a slower way; the others' code has one rare branch.
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_many_kernel(Args a, int tiles) {
   constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
   constexpr int KP = 2 * U * 64, ALL = KvChunk<ES, HD>::kBytes / 16, N = ALL / 256;   // pieces of 16 bytes: keys, all, a thread's
-  constexpr int KF = 2 * HB * 64, STAGE = KF + HT * 64 + 8;                              // of a stage: keys, all with the powers of two
+  constexpr int KF = 2 * HB * 64, STAGE = KF + HT * 64;                                  // of a stage: keys, all
   static_assert(ALL % 256 == 0 && KP % 64 == 0, "a wave's pieces are keys or values");
   __shared__ u32x4 lds[2 * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -388,12 +470,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) qf[t][hb] = as_bf16x8(*(const u32x4*)(p + hb * 8));
   }
-  f32x4 acc[QT][HT];
-  float m_run[QT], l_run[QT];
+  f32x4 acc[QT][HT], l_run[QT];
+  float m_run[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     m_run[t] = -FLT_MAX;
-    l_run[t] = 0.f;
+    l_run[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int h = 0; h < HT; ++h) acc[t][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
@@ -401,9 +483,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int n = max(part.c_hi - part.c_lo, 0);
   Pages pages = {part.table, part.c_lo, 1, part.c_hi - 1, a.place.shift, 0};
   u32x4 piece[N];
-  uint32_t ks[N], vs1 = 0;
-  int there = 0;
+  uint32_t ks[N], four = 0;     // (words: a byte would be widened, and waited for, long before it is used)
+  u32x2 vs = {};
+  bool there = false;
+  // whether a wave's j-th pieces are keys: known when compiled, unless a chunk's keys are less than the block's threads
+  auto is_keys = [&](int j) { return KP % 256 == 0 ? j * 256 < KP : j * 256 + wave * 64 < KP; };
+  // (nothing here hangs on a condition: where loads and what was loaded before meet, the loads would be waited for.  Behind the last chunk it comes again.)
   auto load = [&](int i) {
+    i = min(i, n - 1);
     const int page = pages.of(i, lane), no = part.c_lo + i;
     there = page >= 0 && page < a.pages;
     const size_t chunk = ((((size_t)(there ? page : 0) * a.place.kv_heads + part.kvh) << a.place.shift) + (no & ((1 << a.place.shift) - 1)));
@@ -414,22 +501,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       const int q = j * 256 + (int)threadIdx.x;
       piece[j] = p[q];
       if constexpr (ES == 1) {
-        if (j * 256 + wave * 64 < KP) ks[j] = s[(col >> 2) * 8 + (q / (U * 64)) * 4 + (col & 3)];
+        if (is_keys(j)) ks[j] = ((const uint32_t*)s)[(col >> 2) * 2 + q / (U * 64)];
       }
     }
-    if (threadIdx.x < 32) vs1 = s[32 + threadIdx.x];
+    if constexpr (ES == 1) vs = *(const u32x2*)(s + 32 + grp * 8);
+    four = ((const uint32_t*)s)[8 + (lane & 31) / 4];
   };
+  // what a step has to know of the chunk that is in LDS: keys of no page, and a bit for each key whose values are NaN
+  struct Known { bool there; uint32_t bad; };
   auto store = [&](u32x4* stage, int i) {
-    const int k0 = (part.c_lo + i) * 32 + grp * 8;
-    const bool tail = (part.c_lo + i) * 32 + 32 > part.s.keys || !there;
+    const int k0 = (part.c_lo + i) * 32 + grp * 8, live = there ? part.s.keys - k0 : 0;
+    Known known = {there, (uint32_t)__builtin_amdgcn_ballot_w64(byte_of(four, lane) == 255u)};
+    if ((part.c_lo + i) * 32 + 32 > part.s.keys || !there || known.bad != 0) {
+      asm volatile("; the last chunk, or one with values that are NaN");    // (a branch and no selections)
+      if constexpr (ES == 1) {     // powers of two that are none, of keys that are not there or of zeros: any will do
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= live || ((vs[e >> 2] >> (8 * (e & 3))) & 255u) == 255u) vs[e >> 2] &= ~(255u << (8 * (e & 3)));
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (!is_keys(j)) cut_values<ES>(piece[j], live);
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int q = j * 256 + wave * 64;      // (of the wave: keys or values)
-      if (q < KP) {
+      union { bf16x8 b; u32x4 v; } x, y;
+      if (is_keys(j)) {
         if constexpr (ES == 1) {
           const int t2 = q / (U * 64), u = q / 64 % U;
-          const float f = power_of(ks[j]);
-          union { bf16x8 b; u32x4 v; } x, y;
+          const float f = power_of(byte_of(ks[j], lane));
           x.b = widen8(piece[j][0], piece[j][1], f);
           y.b = widen8(piece[j][2], piece[j][3], f);
           stage[(t2 * HB + 2 * u) * 64 + lane] = x.v;
@@ -438,12 +539,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
           stage[q + lane] = piece[j];
         }
       } else {
-        if (tail) cut_values<ES>(piece[j], there ? part.s.keys - k0 : 0);
         const int h = (q - KP) / 64;
         if constexpr (ES == 1) {
-          union { bf16x8 b; u32x4 v; } x, y;
-          x.b = widen8(piece[j][0], piece[j][1], 1.f);
-          y.b = widen8(piece[j][2], piece[j][3], 1.f);
+          widen_values(piece[j], vs, x.v, y.v);
           stage[KF + 2 * h * 64 + lane] = x.v;
           stage[KF + (2 * h + 1) * 64 + lane] = y.v;
         } else {
@@ -451,24 +549,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
       }
     }
-    if (threadIdx.x < 32) ((float*)(stage + KF + HT * 64))[threadIdx.x] = power_of(vs1);
+    return known;
   };
-  int there_now = 0;
-  if (n > 0) {
-    load(0);
-    store(lds, 0);
-    there_now = there;
-    if (n > 1) load(1);
-  }
-  block_barrier_nofence();
-  for (int i = 0; i < n; ++i) {
-    const u32x4* stage = lds + (i & 1) * STAGE;
-    const bool there_i = there_now;
-    if (i + 1 < n) {
-      store(lds + (~i & 1) * STAGE, i + 1);
-      there_now = there;
-      if (i + 2 < n) load(i + 2);
-    }
+  const bf16x8 ones = u4_as_bf16x8(make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+  auto step = [&](const u32x4* stage, int i, Known known) {
+    const bool slow = (part.c_lo + i) * 32 + 32 > part.seen_first || !known.there || known.bad;
     f32x4 sc[QT][2];
 #pragma unroll
     for (int t2 = 0; t2 < 2; ++t2) {
@@ -482,32 +567,65 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int hb = 0; hb < HB; ++hb) sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], qf[t][hb], sc[t][t2], 0, 0, 0);
       }
     }
-    float vs[8];
-    {
-      const float4 x = ((const float4*)(stage + KF + HT * 64))[grp * 2], y = ((const float4*)(stage + KF + HT * 64))[grp * 2 + 1];
-      vs[0] = x.x; vs[1] = x.y; vs[2] = x.z; vs[3] = x.w; vs[4] = y.x; vs[5] = y.y; vs[6] = y.z; vs[7] = y.w;
+    __builtin_amdgcn_sched_barrier(0);    // (reads of values that are brought forward to here would take the registers of two tiles)
+    const int k0 = (part.c_lo + i) * 32 + grp * 8;
+    if (slow) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if ((known.bad >> (grp * 8 + e)) & 1u) sc[t][e >> 2][e & 3] = __uint_as_float(0x7fc00000u);
+          if (k0 + e >= seen[t] || !known.there) sc[t][e >> 2][e & 3] = -INFINITY;
+        }
     }
-    const int key0 = (part.c_lo + i) * 32, k0 = key0 + grp * 8;
-    const bool masked = key0 + 32 > part.seen_first || !there_i;
+    float mx[QT];
+    bool up = false;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      mx[t] = top_score(sc[t], a.scale);
+      up = up || mx[t] > m_run[t] + kLag;
+    }
+    if (__builtin_amdgcn_ballot_w64(up) != 0) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) move_top(acc[t], m_run[t], l_run[t], mx[t]);
+    }
     bf16x8 pf[QT];
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
-      pf[t] = soften<HT>(sc[t], acc[t], m_run[t], l_run[t], vs, a.scale, masked, [&](int e) { return k0 + e >= seen[t] || !there_i; });
+    for (int t = 0; t < QT; ++t) {
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(sc[t][e >> 2][e & 3], a.scale, -m_run[t]));
+      pf[t] = pack8(p);
+      l_run[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], l_run[t], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
       const bf16x8 vf = as_bf16x8(stage[KF + h * 64 + lane]);
 #pragma unroll
       for (int t = 0; t < QT; ++t) acc[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[t], acc[t][h], 0, 0, 0);
     }
+  };
+  Known next = {false, 0};
+  if (n > 0) {
+    load(0);
+    next = store(lds, 0);
+    load(1);
+  }
+  block_barrier_nofence();
+  for (int i = 0; i < n; ++i) {
+    const u32x4* stage = lds + (i & 1) * STAGE;
+    const Known now = next;
+    next = store(lds + (~i & 1) * STAGE, i + 1);     // (behind the last chunk: what no one reads)
+    load(i + 2);
+    step(stage, i, now);
     block_barrier_nofence();
   }
 
   const int at_slice = PREFIX ? part.slice : a.prefix_slices + part.slice;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    float l = l_run[t];
-    l += other_row(l);
-    l += other_half(l);
+    const float l = l_run[t][0];
     const int m = first + t * 16 + col;
     if (m >= part.queries) continue;
     int row, head, unused;
@@ -620,13 +738,6 @@ size_t part_bytes(const KvCache& c, const KvAttention& a, int slices) {
   return ((size_t)a.rows * a.heads * slices * c.head_dim * 4 + 255) / 256 * 256;
 }
 
-template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
-void launch_few(const Args& a, long blocks, hipStream_t s) {
-  constexpr int lds = kWaves * QT * (HD / 16 * 64 + 32) * 16;
-  static std::atomic<uint64_t> allowed{0};
-  if (lds > 65536) allow_lds((const void*)kv_attention_few_kernel<ES, HD, QT, PREFIX, DIRECT>, lds, allowed);
-  kv_attention_few_kernel<ES, HD, QT, PREFIX, DIRECT><<<(unsigned)blocks, 256, lds, s>>>(a, 1);
-}
 template <int ES, int HD, bool PREFIX, bool DIRECT>
 void launch_cut(const Args& a, const Cut& c, hipStream_t s) {
   const long blocks = (long)a.place.kv_heads * (PREFIX ? 1 : a.seqs) * c.slices * c.tiles;
@@ -635,9 +746,9 @@ void launch_cut(const Args& a, const Cut& c, hipStream_t s) {
     else if (c.qt == 2) kv_attention_many_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
     else kv_attention_many_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
   } else {
-    if (c.qt == 1) launch_few<ES, HD, 1, PREFIX, DIRECT>(a, blocks, s);
-    else if (c.qt == 2) launch_few<ES, HD, 2, PREFIX, DIRECT>(a, blocks, s);
-    else launch_few<ES, HD, 3, PREFIX, DIRECT>(a, blocks, s);
+    if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
+    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
+    else kv_attention_few_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
   }
 }
 
