@@ -91,18 +91,17 @@ struct Part {
     *seen = causal ? s.keys - s.n + 1 + r : s.keys;
   }
 };
-// false: nothing to do.  EACH: queries of a block.  The heads' and sequences' blocks lie next to each other, so that blocks that read the same keys are
-// a multiple of kv_heads apart and mostly share an XCD's L2; late rows, which see most under `causal`, go first.
+// false: nothing to do.  EACH: queries of a block.  Blocks that read the same keys are kv_heads apart, next to each other otherwise: mostly on one
+// XCD, whose L2 they share.  Late rows, which see most under `causal`, go first.
 template <int EACH, bool PREFIX>
 __device__ __forceinline__ bool part_of(const Args& a, int tiles, Part& p) {
   unsigned id = blockIdx.x;
   p.kvh = id % a.place.kv_heads;
   id /= a.place.kv_heads;
-  const int seqs = PREFIX ? 1 : a.seqs, b = id % seqs;
-  id /= seqs;
-  const int slices = PREFIX ? a.prefix_slices : a.slices;
+  const int tile = tiles - 1 - (int)(id % tiles);
+  id /= tiles;
+  const int slices = PREFIX ? a.prefix_slices : a.slices, b = id / slices;
   p.slice = id % slices;
-  const int tile = tiles - 1 - (int)(id / slices);
   p.s = PREFIX ? Seq{0, a.rows, a.prefix_len} : seq_of(a, b);
   p.first = tile * EACH;
   p.queries = p.s.n * a.group;
@@ -124,7 +123,10 @@ struct Pages {
   const int* table;
   int first, step, last, shift, ids;
   __device__ __forceinline__ int of(int i, int lane) {
-    if ((i & 63) == 0) ids = table[min(first + step * (i + lane), last) >> shift];
+    if ((i & 63) == 0) {
+      ids = table[min(first + step * (i + lane), last) >> shift];
+      asm volatile("" : "+v"(ids));   // (waited for here: where this path meets the other, every load on its way would be)
+    }
     return __builtin_amdgcn_readlane(ids, i & 63);
   }
 };
@@ -277,10 +279,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
       }
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        sc[t][t2] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < QT; ++t) sc[t][t2] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) {
+      for (int hb = 0; hb < HB; ++hb) {      // (the tiles in turn: a product waits for the one before it on the same sums)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
           const bf16x8 q = PARKED ? as_bf16x8(parked[(t * HB + hb) * 64 + lane]) : qf[PARKED ? 0 : t][hb];
           sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], q, sc[t][t2], 0, 0, 0);
         }
@@ -561,13 +564,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb) kf[hb] = as_bf16x8(stage[(t2 * HB + hb) * 64 + lane]);
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        sc[t][t2] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < QT; ++t) sc[t][t2] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], qf[t][hb], sc[t][t2], 0, 0, 0);
-      }
+      for (int hb = 0; hb < HB; ++hb)      // (the tiles in turn: a product waits for the one before it on the same sums)
+#pragma unroll
+        for (int t = 0; t < QT; ++t) sc[t][t2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[hb], qf[t][hb], sc[t][t2], 0, 0, 0);
     }
-    __builtin_amdgcn_sched_barrier(0);    // (reads of values that are brought forward to here would take the registers of two tiles)
+    __builtin_amdgcn_sched_barrier(0x8);    // (products may pass; reads of values that are brought forward to here would take the registers of two tiles)
     const int k0 = (part.c_lo + i) * 32 + grp * 8;
     if (slow) {
 #pragma unroll
@@ -719,7 +722,7 @@ Cut cut(long queries, int chunks, long others) {
     c.qt = (int)max(1L, (queries + 15) / 16);
     c.tiles = 1;
   }
-  const long want = (c.many ? 512 : 1024) / max(others * c.tiles, 1L);     // blocks that fill the compute units
+  const long want = (c.many || c.qt > 1 ? 512 : 1024) / max(others * c.tiles, 1L);     // blocks that fill the compute units
   const long most = max(1, chunks / 8);                                    // (8 chunks to a slice at least)
   const int n = (int)max(1L, min(min(want, most), (long)kSlicesMax));
   c.split = (chunks + n - 1) / n;
