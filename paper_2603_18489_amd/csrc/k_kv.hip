@@ -18,32 +18,30 @@ __device__ __forceinline__ uint32_t kv_scale(uint32_t top) {
   return (uint32_t)max(e, 1);
 }
 
-template <typename T, int N>
-__device__ __forceinline__ void load_values(const T* p, bool wide, float (&v)[N]) {
-  if (wide) {
-    if constexpr (sizeof(T) == 4) {
+// N values as they lie in memory, and as float32
+template <typename T, int N> struct Loaded {
+  uint4 w[N * sizeof(T) / 16];
+  __device__ __forceinline__ void load(const T* p, bool wide) {
+    if (wide) {
 #pragma unroll
-      for (int j = 0; j < N / 4; ++j) {
-        const float4 a = ((const float4*)p)[j];
-        v[4 * j] = a.x; v[4 * j + 1] = a.y; v[4 * j + 2] = a.z; v[4 * j + 3] = a.w;
-      }
+      for (int j = 0; j < (int)(N * sizeof(T) / 16); ++j) w[j] = ((const uint4*)p)[j];
     } else {
+      union { T v[N]; uint4 w[N * sizeof(T) / 16]; } c;
 #pragma unroll
-      for (int j = 0; j < N / 8; ++j) {
-        const uint4 a = ((const uint4*)p)[j];
-        const uint32_t u[4] = {a.x, a.y, a.z, a.w};
+      for (int j = 0; j < N; ++j) c.v[j] = p[j];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[8 * j + 2 * k] = __uint_as_float(u[k] << 16);
-          v[8 * j + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
-        }
-      }
+      for (int j = 0; j < (int)(N * sizeof(T) / 16); ++j) w[j] = c.w[j];
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = load_f32(p + j);
   }
-}
+  __device__ __forceinline__ void values(float (&v)[N]) const {
+    const uint32_t* u = (const uint32_t*)w;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(u[j]);
+      else v[j] = __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+    }
+  }
+};
 
 __device__ __forceinline__ uint32_t codes4(const float* v, float f) {
   int c = 0;
@@ -165,13 +163,14 @@ template <int ROWS> struct Tile {
   int slot[ALL];          // -1: not in the cache, or (written) a later row has it
   int first[ROWS / 8];    // the runs' first rows
   int runs;
+  bool there;             // all of the block's rows have a slot
   unsigned long long single;   // the block's rows that are in no run and have a slot, a bit each
-  uint32_t seen[32];      // written: a bit for slot & 1023 of each row
-  int low, high;
+  int low, high;          // written: of the rows' slots
+  int row_of[2048];       // written: by slot % 2048, 1 + the row (of ALL) with it, 0: none, -1: several
 };
 
-// WRITE: of rows that name the same slot the last one is stored.  The rows behind the block's are gone through; few of them are among the
-// block's slots' range, and of these a bit for each of 1024 remainders leaves few to be compared.
+// WRITE: of rows that name the same slot the last one is stored.  The rows behind the block's are gone through: few of them are in the block's slots'
+// range, and of these one place of a table says whether they are any of them.
 template <int ROWS, bool WRITE>
 __device__ __forceinline__ void find_runs(const KvRows& a, int row0, Tile<ROWS>& t) {
   typedef Tile<ROWS> Tl;
@@ -184,30 +183,48 @@ __device__ __forceinline__ void find_runs(const KvRows& a, int row0, Tile<ROWS>&
     t.slot[i] = s;
   }
   if constexpr (WRITE) {
-    if (i < 32) t.seen[i] = 0;
-    if (i == 32) { t.low = INT32_MAX; t.high = -1; }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t.row_of[i + 256 * k] = 0;
+    if (i == 0) { t.low = INT32_MAX; t.high = -1; }
     __syncthreads();
     if (s >= 0) {
-      atomicOr(&t.seen[(s >> 5) & 31], 1u << (s & 31));
+      if (atomicCAS(&t.row_of[s & 2047], 0, i + 1) != 0) t.row_of[s & 2047] = -1;
       atomicMin(&t.low, s);
       atomicMax(&t.high, s);
     }
     __syncthreads();
-    const int low = t.low, range = t.high - low;
+    const int low = t.low, range = t.high - low, before = row0 - Tl::SIDE;
     auto compare = [&](int later, int slot) {
-      if (!((t.seen[(slot >> 5) & 31] >> (slot & 31)) & 1u)) return;
-      for (int j = 0; j < Tl::ALL && row0 - Tl::SIDE + j < later; ++j)
-        if (t.slot[j] == slot) t.slot[j] = -1;
-    };
-    if (range >= 0)
-      for (int n = max(row0 - Tl::SIDE, 0) + i; n < a.rows; n += 1024) {
-        int x[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = n + 256 * k < a.rows ? a.slots[n + 256 * k] : -1;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (x[k] >= 0 && (unsigned)(x[k] - low) <= (unsigned)range) compare(n + 256 * k, x[k]);
+      const int r = t.row_of[slot & 2047];
+      if (r > 0) {
+        if (before + r - 1 < later && t.slot[r - 1] == slot) t.slot[r - 1] = -1;
+      } else if (r < 0) {
+        for (int j = 0; j < Tl::ALL && before + j < later; ++j)
+          if (t.slot[j] == slot) t.slot[j] = -1;
       }
+    };
+    auto look = [&](int n, int slot) {
+      if (slot >= 0 && (unsigned)(slot - low) <= (unsigned)range) compare(n, slot);
+    };
+    if (range >= 0) {
+      // (pieces of 4 from the first multiple of 16 bytes on, 16 slots of a thread on their way at a time)
+      constexpr int MANY = 4;
+      const int from = max(before, 0), to = a.rows, lead = (int)(-((intptr_t)(a.slots + from) >> 2) & 3), even = min(from + lead, to);
+      const int pieces = (to - even) >> 2;
+      for (int p = i; p < pieces; p += 256 * MANY) {
+        int4 x[MANY];
+#pragma unroll
+        for (int k = 0; k < MANY; ++k) x[k] = p + 256 * k < pieces ? ((const int4*)(a.slots + even))[p + 256 * k] : make_int4(-1, -1, -1, -1);
+#pragma unroll
+        for (int k = 0; k < MANY; ++k) {
+          const int n = even + 4 * (p + 256 * k);
+          look(n, x[k].x); look(n + 1, x[k].y); look(n + 2, x[k].z); look(n + 3, x[k].w);
+        }
+      }
+      if (i < even - from) look(from + i, a.slots[from + i]);
+      const int tail = even + 4 * pieces;
+      if (i < to - tail) look(tail + i, a.slots[tail + i]);
+    }
   }
   __syncthreads();
   if (i < 64) {
@@ -223,18 +240,18 @@ __device__ __forceinline__ void find_runs(const KvRows& a, int row0, Tile<ROWS>&
       single = t.slot[Tl::SIDE + i] >= 0;
       for (int k = 0; k < 8 && single; ++k) single = !starts(Tl::SIDE + i - k);
     }
-    const unsigned long long runs = __ballot(run), singles = __ballot(single);
+    const unsigned long long runs = __ballot(run), singles = __ballot(single), gone = __ballot(i < ROWS && t.slot[Tl::SIDE + min(i, ROWS - 1)] < 0);
     if (run) t.first[__popcll(runs & ((1ull << i) - 1))] = i;
-    if (i == 0) { t.runs = __popcll(runs); t.single = singles; }
+    if (i == 0) { t.runs = __popcll(runs); t.single = singles; t.there = gone == 0; }
   }
   __syncthreads();
 }
 
 template <int HD> constexpr int kTileRows = 32 * (128 / HD);   // 64 lanes, 8 rows x 8 components each
 
-// A wave takes the rows of a tile and goes through every (4 gridDim.y)-th head.  What bounds it is bytes: each is read and written once, in pieces of 16
-// bytes and more but for the values of rows in no run.
-template <typename T, int ES, int HD>
+// A wave takes the rows of a tile (SPREAD: a part of them) and goes through every (4 gridDim.y)-th head.  What bounds it is bytes: each is read and
+// written once, in pieces of 16 bytes and more but for the values of rows in no run.
+template <typename T, int ES, int HD, bool SPREAD>
 __global__ __launch_bounds__(256) void kv_write_kernel(KvRows a) {
   constexpr int ROWS = kTileRows<HD>, LK = HD / 16, LV = HD / 8;   // lanes of a row: keys, values
   constexpr uint32_t kNaN = ES == 1 ? 0x7f7f7f7fu : 0x7fc07fc0u;
@@ -247,14 +264,18 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows a) {
   const int first = has_run ? t.first[run] : 0, run_slot = has_run ? t.slot[Tile<ROWS>::SIDE + first] : 0;
   for (int h = blockIdx.y * 4 + (threadIdx.x >> 6); h < a.place.kv_heads; h += gridDim.y * 4) {
     // values of the runs: 8 tokens x 8 components
-    if (has_run && blockIdx.z == 0) {
+    if (has_run && (!SPREAD || blockIdx.z == 0)) {
       const T* p = (const T*)a.v + (size_t)(row0 + first) * a.v_ld + (size_t)h * a.v_head + cv;
-      float v[8][8];
+      Loaded<T, 8> x[8];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) load_values(p + (size_t)r * a.v_ld, a.wide, v[r]);
+      for (int r = 0; r < 8; ++r) x[r].load(p + (size_t)r * a.v_ld, a.wide);
       uint32_t w[8][2 * ES], o[8][2 * ES], s[2] = {0, 0};
 #pragma unroll
-      for (int r = 0; r < 8; ++r) s[r >> 2] |= stored<ES, 8, HD>(v[r], w[r], 0) << (8 * (r & 3));
+      for (int r = 0; r < 8; ++r) {
+        float v[8];
+        x[r].values(v);
+        s[r >> 2] |= stored<ES, 8, HD>(v, w[r], 0) << (8 * (r & 3));
+      }
       transpose8<ES>(w, o);
       const size_t chunk = a.place.chunk(run_slot, h);
       uint8_t* to = a.data + chunk * L::kBytes;
@@ -269,37 +290,58 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows a) {
       }
       if (cv == 0) *(uint2*)(a.scales + chunk * 64 + 32 + (run_slot & 31)) = make_uint2(s[0], s[1]);
     }
-    // keys, and values of the rows in no run: 16 components of a token
-    for (int i = blockIdx.z; i < ROWS * LK / 64; i += gridDim.z) {
-      const int j = i * (64 / LK) + lane / LK, c0 = lane % LK * 16, slot = t.slot[Tile<ROWS>::SIDE + j], w = slot & 31;
-      const bool single = (t.single >> j) & 1;
-      if (slot >= 0) {
-        const size_t chunk = a.place.chunk(slot, h);
+    // keys, 16 components of a token at a time
+    constexpr int TURNS = ROWS * LK / 64, EACH = SPREAD ? 1 : TURNS;
+    const int j0 = (SPREAD ? blockIdx.z * (64 / LK) : 0) + lane / LK, c0 = lane % LK * 16;
+    Loaded<T, 16> x[EACH];
+    int slot[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int j = j0 + i * (64 / LK);
+      slot[i] = t.slot[Tile<ROWS>::SIDE + j];
+      if (slot[i] >= 0) x[i].load((const T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide);
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      if (slot[i] >= 0) {
+        const int w = slot[i] & 31;
+        const size_t chunk = a.place.chunk(slot[i], h);
         uint8_t* to = a.data + chunk * L::kBytes;
-        float k[16], v[16];
+        float v[16];
         uint32_t words[4 * ES];
-        load_values((const T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide, k);
-        if (single) load_values((const T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide, v);
-        uint32_t s = stored<ES, 16, HD>(k, words, kNaN);
+        x[i].values(v);
+        const uint32_t s = stored<ES, 16, HD>(v, words, kNaN);
 #pragma unroll
         for (int n = 0; n < ES; ++n)
           *(uint4*)(to + L::key_at(w, c0 + n * 8)) = make_uint4(words[4 * n], words[4 * n + 1], words[4 * n + 2], words[4 * n + 3]);
         if (c0 == 0) a.scales[chunk * 64 + w] = (uint8_t)s;
-        if (single) {
-          s = stored<ES, 16, HD>(v, words, 0);
+      }
+    }
+    // values of the rows in no run
+    if (t.single == 0) continue;
+    for (int i = 0; i < EACH; ++i) {
+      const int j = j0 + i * (64 / LK), at = t.slot[Tile<ROWS>::SIDE + j], w = at & 31;
+      if ((t.single >> j) & 1) {
+        const size_t chunk = a.place.chunk(at, h);
+        uint8_t* to = a.data + chunk * L::kBytes;
+        Loaded<T, 16> y;
+        y.load((const T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide);
+        float v[16];
+        uint32_t words[4 * ES];
+        y.values(v);
+        const uint32_t s = stored<ES, 16, HD>(v, words, 0);
 #pragma unroll
-          for (int n = 0; n < 16; ++n) {
-            if constexpr (ES == 1) to[L::value_at(w, c0 + n)] = (uint8_t)(words[n >> 2] >> (8 * (n & 3)));
-            else *(uint16_t*)(to + L::value_at(w, c0 + n)) = (uint16_t)(words[n >> 1] >> (16 * (n & 1)));
-          }
-          if (c0 == 0) a.scales[chunk * 64 + 32 + w] = (uint8_t)s;
+        for (int n = 0; n < 16; ++n) {
+          if constexpr (ES == 1) to[L::value_at(w, c0 + n)] = (uint8_t)(words[n >> 2] >> (8 * (n & 3)));
+          else *(uint16_t*)(to + L::value_at(w, c0 + n)) = (uint16_t)(words[n >> 1] >> (16 * (n & 1)));
         }
+        if (c0 == 0) a.scales[chunk * 64 + 32 + w] = (uint8_t)s;
       }
     }
   }
 }
 
-template <typename T, int ES, int HD>
+template <typename T, int ES, int HD, bool SPREAD>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvRows a) {
   constexpr int ROWS = kTileRows<HD>, LK = HD / 16, LV = HD / 8;
   typedef KvChunk<ES, HD> L;
@@ -310,7 +352,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvRows a) {
   const bool has_run = run < t.runs;
   const int first = has_run ? t.first[run] : 0, run_slot = has_run ? t.slot[Tile<ROWS>::SIDE + first] : 0;
   for (int h = blockIdx.y * 4 + (threadIdx.x >> 6); h < a.place.kv_heads; h += gridDim.y * 4) {
-    if (has_run && blockIdx.z == 0) {
+    if (has_run && (!SPREAD || blockIdx.z == 0)) {
       const size_t chunk = a.place.chunk(run_slot, h);
       const uint8_t* from = a.data + chunk * L::kBytes;
       uint32_t w[8][2 * ES], o[8][2 * ES];
@@ -335,35 +377,52 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvRows a) {
         store_values(p + (size_t)r * a.v_ld, a.wide, v);
       }
     }
-    for (int i = blockIdx.z; i < ROWS * LK / 64; i += gridDim.z) {
-      const int j = i * (64 / LK) + lane / LK, c0 = lane % LK * 16, slot = t.slot[Tile<ROWS>::SIDE + j], w = slot & 31;
-      if (row0 + j < a.rows) {
-        const bool there = slot >= 0, single = (t.single >> j) & 1;
-        float k[16] = {}, v[16] = {};
-        if (there) {
-          const size_t chunk = a.place.chunk(slot, h);
-          const uint8_t* from = a.data + chunk * L::kBytes;
-          uint32_t kw[4 * ES], vw[4 * ES];
+    constexpr int TURNS = ROWS * LK / 64, EACH = SPREAD ? 1 : TURNS;
+    const int j0 = (SPREAD ? blockIdx.z * (64 / LK) : 0) + lane / LK, c0 = lane % LK * 16;
+    uint32_t kw[EACH][4 * ES], ks[EACH];
+    int slot[EACH];
 #pragma unroll
-          for (int n = 0; n < ES; ++n) {
-            const uint4 u = *(const uint4*)(from + L::key_at(w, c0 + n * 8));
-            kw[4 * n] = u.x; kw[4 * n + 1] = u.y; kw[4 * n + 2] = u.z; kw[4 * n + 3] = u.w;
-          }
-          const uint32_t ks = a.scales[chunk * 64 + w], vs = a.scales[chunk * 64 + 32 + w];
+    for (int i = 0; i < EACH; ++i) {
+      slot[i] = t.slot[Tile<ROWS>::SIDE + j0 + i * (64 / LK)];
+      if (slot[i] >= 0) {
+        const size_t chunk = a.place.chunk(slot[i], h);
+        const uint8_t* from = a.data + chunk * L::kBytes;
 #pragma unroll
-          for (int n = 0; n < 4 * ES; ++n) vw[n] = 0;
-          if (single) {
-#pragma unroll
-            for (int n = 0; n < 16; ++n) {
-              if constexpr (ES == 1) vw[n >> 2] |= (uint32_t)from[L::value_at(w, c0 + n)] << (8 * (n & 3));
-              else vw[n >> 1] |= (uint32_t) * (const uint16_t*)(from + L::value_at(w, c0 + n)) << (16 * (n & 1));
-            }
-          }
-          values_of<ES>(kw, ks, k);
-          values_of<ES>(vw, vs, v);
+        for (int n = 0; n < ES; ++n) {
+          const uint4 u = *(const uint4*)(from + L::key_at(slot[i] & 31, c0 + n * 8));
+          kw[i][4 * n] = u.x; kw[i][4 * n + 1] = u.y; kw[i][4 * n + 2] = u.z; kw[i][4 * n + 3] = u.w;
         }
-        store_values((T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide, k);
-        if (single || !there) store_values((T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide, v);
+        ks[i] = a.scales[chunk * 64 + (slot[i] & 31)];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int j = j0 + i * (64 / LK);
+      if (row0 + j < a.rows) {
+        float x[16] = {};
+        if (slot[i] >= 0) values_of<ES>(kw[i], ks[i], x);
+        store_values((T*)a.k + (size_t)(row0 + j) * a.k_ld + (size_t)h * a.k_head + c0, a.wide, x);
+      }
+    }
+    // values of the rows in no run, and of those that are not there
+    if (t.single == 0 && t.there) continue;
+    for (int i = 0; i < EACH; ++i) {
+      const int j = j0 + i * (64 / LK), at = t.slot[Tile<ROWS>::SIDE + j];
+      if (row0 + j < a.rows && (at < 0 || ((t.single >> j) & 1))) {
+        float x[16] = {};
+        if (at >= 0) {
+          const size_t chunk = a.place.chunk(at, h);
+          const uint8_t* from = a.data + chunk * L::kBytes;
+          const uint32_t s = a.scales[chunk * 64 + 32 + (at & 31)];
+          uint32_t words[4 * ES] = {};
+#pragma unroll
+          for (int n = 0; n < 16; ++n) {
+            if constexpr (ES == 1) words[n >> 2] |= (uint32_t)from[L::value_at(at & 31, c0 + n)] << (8 * (n & 3));
+            else words[n >> 1] |= (uint32_t) * (const uint16_t*)(from + L::value_at(at & 31, c0 + n)) << (16 * (n & 1));
+          }
+          values_of<ES>(words, s, x);
+        }
+        store_values((T*)a.v + (size_t)(row0 + j) * a.v_ld + (size_t)h * a.v_head + c0, a.wide, x);
       }
     }
   }
@@ -381,35 +440,38 @@ static KvRows rows_of(const KvCache& c, const void* k, const void* v, bool bf16,
   return a;
 }
 
-// Blocks that share a tile of rows: as many as there are heads for, four to a block, and four beside each other that share the rows in no run, as far as that
-// makes no more than 2048 blocks.  (Each of them looks for rows that name the same slot.)
-static dim3 kv_grid(int tiles, int heads) {
-  const int y = min((heads + 3) / 4, max(1, 2048 / tiles));
-  return dim3(tiles, y, tiles * y <= 512 ? 4 : 1);
-}
+// Blocks that share a tile of rows: as many as there are heads for, four to a block, up to `most` blocks in all; where few are made, some beside each
+// other share the tile's rows too.  A block that writes looks for rows that name the same slot, which takes it 10 us among 24576 rows: 768 blocks of
+// all 32 heads write these in 168 us, 1536 of half in 176, 3840 in 222; blocks that read them take 124 (768), 118 (6144).
+static int kv_blocks(int tiles, int heads, int most) { return min((heads + 3) / 4, max(1, most / tiles)); }
 
-#define EC_KV_LAUNCH(KERNEL, T, ES, HD) \
-  KERNEL<T, ES, HD><<<kv_grid((rows + kTileRows<HD> - 1) / kTileRows<HD>, c.kv_heads), 256, 0, s>>>(a)
-#define EC_KV_PICK(KERNEL)                                                                      \
+#define EC_KV_LAUNCH(KERNEL, MOST, T, ES, HD)                                                                            \
+  do {                                                                                                                   \
+    constexpr int turns = kTileRows<HD> * (HD / 16) / 64;                                                                \
+    const int tiles = (rows + kTileRows<HD> - 1) / kTileRows<HD>, y = kv_blocks(tiles, c.kv_heads, MOST);                 \
+    if (tiles * y <= 512) KERNEL<T, ES, HD, true><<<dim3(tiles, y, turns), 256, 0, s>>>(a);                              \
+    else KERNEL<T, ES, HD, false><<<dim3(tiles, y), 256, 0, s>>>(a);                                                     \
+  } while (0)
+#define EC_KV_PICK(KERNEL, MOST)                                                                      \
   do {                                                                                          \
     if (bf16) {                                                                                 \
-      if (c.head_dim == 64) { if (c.e4m3) EC_KV_LAUNCH(KERNEL, bf16_t, 1, 64); else EC_KV_LAUNCH(KERNEL, bf16_t, 2, 64); }     \
-      else { if (c.e4m3) EC_KV_LAUNCH(KERNEL, bf16_t, 1, 128); else EC_KV_LAUNCH(KERNEL, bf16_t, 2, 128); }                    \
+      if (c.head_dim == 64) { if (c.e4m3) EC_KV_LAUNCH(KERNEL, MOST, bf16_t, 1, 64); else EC_KV_LAUNCH(KERNEL, MOST, bf16_t, 2, 64); }     \
+      else { if (c.e4m3) EC_KV_LAUNCH(KERNEL, MOST, bf16_t, 1, 128); else EC_KV_LAUNCH(KERNEL, MOST, bf16_t, 2, 128); }                    \
     } else {                                                                                    \
-      if (c.head_dim == 64) { if (c.e4m3) EC_KV_LAUNCH(KERNEL, float, 1, 64); else EC_KV_LAUNCH(KERNEL, float, 2, 64); }       \
-      else { if (c.e4m3) EC_KV_LAUNCH(KERNEL, float, 1, 128); else EC_KV_LAUNCH(KERNEL, float, 2, 128); }                      \
+      if (c.head_dim == 64) { if (c.e4m3) EC_KV_LAUNCH(KERNEL, MOST, float, 1, 64); else EC_KV_LAUNCH(KERNEL, MOST, float, 2, 64); }       \
+      else { if (c.e4m3) EC_KV_LAUNCH(KERNEL, MOST, float, 1, 128); else EC_KV_LAUNCH(KERNEL, MOST, float, 2, 128); }                      \
     }                                                                                           \
   } while (0)
 
 void launch_kv_write(const KvCache& c, const void* k, const void* v, bool bf16, int rows, const size_t (&ld)[4], const int* slots,
                      hipStream_t s) {
   const KvRows a = rows_of(c, k, v, bf16, rows, ld, slots);
-  EC_KV_PICK(kv_write_kernel);
+  EC_KV_PICK(kv_write_kernel, 1024);
 }
 
 void launch_kv_read(const KvCache& c, void* k, void* v, bool bf16, int rows, const size_t (&ld)[4], const int* slots, hipStream_t s) {
   const KvRows a = rows_of(c, k, v, bf16, rows, ld, slots);
-  EC_KV_PICK(kv_read_kernel);
+  EC_KV_PICK(kv_read_kernel, 8192);
 }
 
 }  // namespace ec

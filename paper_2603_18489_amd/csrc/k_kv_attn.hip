@@ -211,20 +211,18 @@ template <int ES, int HD> struct Chunk {
 
 }  // namespace
 
-constexpr int kWaves = 4;
-
 // Few queries: up to 48 of a sequence and kv head.  A block's waves go through the chunks of its slice in turn, each with all QT tiles of 16
 // queries and a chunk's pieces in registers, and meet in LDS.  The next chunk's keys are on their way from when this one's are used, the values too; one tile of
 // queries leaves registers for a second chunk.  The power of two of a key's values multiplies its probability.
 // With one tile the matrix cores wait for memory, so that a probability can be two bfloat16 numbers, 2^-17 together, instead of one.
 // DIRECT: there is one slice, and the block writes the result.
-template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a, int tiles) {
+template <int ES, int HD, int QT, int W, bool PREFIX, bool DIRECT>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a, int tiles) {
   constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
   typedef Chunk<ES, HD> C;
   constexpr int SLOT = HT * 64 + 32;   // float4 of a wave's part of a tile
   constexpr bool PARKED = QT > 2;      // queries in LDS, as a third tile's registers would spill others
-  __shared__ float4 lds[kWaves * SLOT];
+  __shared__ float4 lds[W * SLOT];
   __shared__ u32x4 parked[PARKED ? QT * HB * 64 : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane >> 4, col = lane & 15;
@@ -241,7 +239,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
       if constexpr (!PARKED) qf[t][hb] = as_bf16x8(*(const u32x4*)(p + hb * 8));
-      else if (hb % kWaves == wave) parked[(t * HB + hb) * 64 + lane] = *(const u32x4*)(p + hb * 8);
+      else if (hb % W == wave) parked[(t * HB + hb) * 64 + lane] = *(const u32x4*)(p + hb * 8);
     }
   }
   if constexpr (PARKED) __syncthreads();
@@ -256,11 +254,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 
   const int from = part.c_lo + wave;                                                        // this wave's first chunk
-  const int mine = from < part.c_hi ? (part.c_hi - from + kWaves - 1) / kWaves : 0;         // and how many it has
-  Pages pages = {part.table, from, kWaves, from + kWaves * (mine - 1), a.place.shift, 0};
+  const int mine = from < part.c_hi ? (part.c_hi - from + W - 1) / W : 0;         // and how many it has
+  Pages pages = {part.table, from, W, from + W * (mine - 1), a.place.shift, 0};
   auto place = [&](C& c, int i) {
     const int n = min(i, mine - 1);     // (behind the last chunk it comes once more, from the cache)
-    c.at(a, pages.of(n, lane), from + kWaves * n, part.kvh);
+    c.at(a, pages.of(n, lane), from + W * n, part.kvh);
   };
   f32x4 sc[QT][2];
   auto score = [&](const C& c) {
@@ -291,7 +289,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
   };
   auto attend = [&](C& c, int i, bool there) {
-    const int key0 = (from + kWaves * i) * 32, k0 = key0 + grp * 8;
+    const int key0 = (from + W * i) * 32, k0 = key0 + grp * 8;
     const bool masked = key0 + 32 > part.seen_first || !there;
     if (masked) {
       const int live = there ? part.s.keys - k0 : 0;
@@ -402,24 +400,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
     for (int h = 0; h < HT; ++h) slot[h * 64 + lane] = make_float4(acc[t][h][0], acc[t][h][1], acc[t][h][2], acc[t][h][3]);
     __syncthreads();
-    float m_all = -FLT_MAX, l_all = 0.f, f[kWaves];
+    float m_all = -FLT_MAX, l_all = 0.f, f[W];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       f[w] = ((const float2*)(lds + (size_t)w * SLOT + HT * 64))[lane].x;
       m_all = fmaxf(m_all, f[w]);
     }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       f[w] = __builtin_amdgcn_exp2f(f[w] - m_all);
       l_all += ((const float2*)(lds + (size_t)w * SLOT + HT * 64))[lane].y * f[w];
     }
     const int m = part.first + t * 16 + col;
     int row, head, unused;
     part.query(a, m, &row, &head, &unused);
-    for (int p = wave; p < HT / 2 && m < part.queries; p += kWaves) {
+    for (int p = wave; p < HT / 2 && m < part.queries; p += W) {
       float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float4 x = lds[(size_t)w * SLOT + 2 * p * 64 + lane], y = lds[(size_t)w * SLOT + (2 * p + 1) * 64 + lane];
         o[0] += x.x * f[w]; o[1] += x.y * f[w]; o[2] += x.z * f[w]; o[3] += x.w * f[w];
         o[4] += y.x * f[w]; o[5] += y.y * f[w]; o[6] += y.z * f[w]; o[7] += y.w * f[w];
@@ -712,19 +710,30 @@ struct Cut {
   bool many;
   int qt, tiles, split, slices;
 };
-Cut cut(long queries, int chunks, long others) {
+Cut cut(long queries, int chunks, long others, bool joined) {
   Cut c;
   c.many = queries > 48;
   if (c.many) {
-    c.qt = queries <= 64 ? 1 : queries <= 128 || (queries > 192 && queries <= 256) ? 2 : 3;
-    c.tiles = (int)((queries + 64 * c.qt - 1) / (64 * c.qt));
+    // by what a tile takes (16 x 1536 rows over 1536 keys: 975, 778 and 757 us in tiles of 64, 128 and 192) and how full the last one is
+    const double cost[3] = {1.29, 2 * 1.03, 3.0};
+    double least = 0;
+    for (int qt = 1; qt <= 3; ++qt) {
+      const long tiles = (queries + 64 * qt - 1) / (64 * qt);
+      if (qt == 1 || tiles * cost[qt - 1] < least) {
+        least = tiles * cost[qt - 1];
+        c.qt = qt;
+        c.tiles = (int)tiles;
+      }
+    }
   } else {
     c.qt = (int)max(1L, (queries + 15) / 16);
     c.tiles = 1;
   }
   const long want = (c.many || c.qt > 1 ? 512 : 1024) / max(others * c.tiles, 1L);     // blocks that fill the compute units
   const long most = max(1, chunks / 8);                                    // (8 chunks to a slice at least)
-  const int n = (int)max(1L, min(min(want, most), (long)kSlicesMax));
+  // Up to 1024 keys are not cut for few queries: 8 waves of a block are through them in 8.2 us where slices and their meeting take 7.1, but the second
+  // launch costs the caller 4 (one row, 1000 keys, 28 heads on 4).
+  const int n = !c.many && !joined && chunks <= 32 ? 1 : (int)max(1L, min(min(want, most), (long)kSlicesMax));
   c.split = (chunks + n - 1) / n;
   c.slices = (chunks + c.split - 1) / c.split;
   return c;
@@ -733,8 +742,8 @@ struct Plan { Cut own, prefix; };
 Plan plan_of(const KvCache& c, const KvAttention& a) {
   const long group = a.heads / c.kv_heads;
   Plan p = {};
-  p.own = cut(a.max_rows * group, max(1, (a.max_keys + 31) / 32), (long)c.kv_heads * a.seqs);
-  if (a.prefix_len > 0) p.prefix = cut(a.rows * group, (a.prefix_len + 31) / 32, c.kv_heads);
+  p.own = cut(a.max_rows * group, max(1, (a.max_keys + 31) / 32), (long)c.kv_heads * a.seqs, a.prefix_len > 0);
+  if (a.prefix_len > 0) p.prefix = cut(a.rows * group, (a.prefix_len + 31) / 32, c.kv_heads, true);
   return p;
 }
 size_t part_bytes(const KvCache& c, const KvAttention& a, int slices) {
@@ -749,9 +758,10 @@ void launch_cut(const Args& a, const Cut& c, hipStream_t s) {
     else if (c.qt == 2) kv_attention_many_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
     else kv_attention_many_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
   } else {
-    if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
-    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
-    else kv_attention_few_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
+    if (c.qt == 1 && DIRECT && blocks <= 256) kv_attention_few_kernel<ES, HD, 1, 8, PREFIX, DIRECT><<<(unsigned)blocks, 512, 0, s>>>(a, 1);
+    else if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
+    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
+    else kv_attention_few_kernel<ES, HD, 3, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
   }
 }
 
