@@ -628,17 +628,18 @@ def kv_cache(pages: int, kv_heads: int, head_dim: int, page: int = 64, dtype=Non
     return KvCache(torch.zeros((size,), dtype=torch.uint8, device=device), kind, pages, page, kv_heads, head_dim)
 
 
-def _cache_struct(lib, cache: KvCache):
-    import torch
-    c = ec_kv_cache(cache.data.data_ptr() or None, cache.kind, cache.pages, cache.page, cache.kv_heads, cache.head_dim)
-    _need(cache.data.dtype == torch.uint8 and cache.data.is_contiguous() and cache.data.numel() >= max(lib.ec_kv_bytes(C.byref(c)), 1),
-          "data is not a cache of kv_cache")
-    return c
+def _cache_struct(torch, cache: KvCache):
+    data, kind, pages, page, heads, dim = cache
+    # (bytes as ec_kv_bytes counts them, without another call, which the library refuses limits for)
+    _need(data.dtype == torch.uint8 and data.is_contiguous() and
+          0 < 2 * pages * page * heads * (dim * (2 if kind == EC_T_BF16 else 1) + 1) <= data.numel(), "data is not a cache of kv_cache")
+    return ec_kv_cache(data.data_ptr(), kind, pages, page, heads, dim)
 
 
 def kv_write(cache: KvCache, k, v, slots, stream=None) -> None:
     """ec_kv_write: float32 or bfloat16 CUDA tensors [rows, kv_heads, head_dim] into the slots (int32 [rows]) of a cache.  A row whose slot is
     not in the cache (-1) is left out; of rows that name the same slot the last one is stored."""
+    import torch
     kind = _plain_type(k.dtype)
     rows, heads, dim, k_ld, k_head = _heads_of(k, "k")
     _need(v.dtype == k.dtype and v.shape == k.shape, "v must have k's shape and type")
@@ -648,7 +649,7 @@ def kv_write(cache: KvCache, k, v, slots, stream=None) -> None:
     lib = _lib or load_library()
 
     def call(raw):
-        c = _cache_struct(lib, cache)
+        c = _cache_struct(torch, cache)
         _done(lib, lib.ec_kv_write(C.byref(c), k.data_ptr(), v.data_ptr(), kind, rows, k_ld, k_head, v_ld, v_head, slots.data_ptr(), raw))
     return _place(stream, call, cache.data, k, v, slots)
 
@@ -666,7 +667,7 @@ def kv_read(cache: KvCache, slots, dtype=None, stream=None):
     lib = _lib or load_library()
 
     def call(raw):
-        c = _cache_struct(lib, cache)
+        c = _cache_struct(torch, cache)
         k, v = (torch.empty((rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.data.device) for _ in range(2))
         head, ld = cache.head_dim, cache.kv_heads * cache.head_dim
         _done(lib, lib.ec_kv_read(C.byref(c), slots.data_ptr(), rows, k.data_ptr(), v.data_ptr(), kind, ld, head, ld, head, raw))
@@ -714,7 +715,7 @@ def kv_attention(q, cache: KvCache, table, lengths, starts=None, max_rows: Optio
                               dim ** -0.5 if scale is None else scale, table.stride(0) if seqs > 1 else width)
 
     def call(raw):
-        c = _cache_struct(lib, cache)
+        c = _cache_struct(torch, cache)
         y = out
         if y is None:
             y = (torch.empty if starts is None else torch.zeros)((rows, heads, dim), dtype=q.dtype, device=q.device)

@@ -44,6 +44,20 @@ def data(rows, heads, head_dim, dtype, pad=0, last=4096, seed=0):
 
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,heads,head_dim,dim", [(100, 64, 128, 38), (41, 1, 512, 510), (9, 33, 64, 22), (3, 5, 16, 2)])
+def test_pairs_off_every_alignment(rows, heads, head_dim, dim, dtype, interleaved):
+    x, at = data(rows, heads, head_dim, dtype)
+    plan = ec.rotary_plan(dim, 10000.0, interleaved, amplitude=0.5)
+    y = ec.rotary(x, at, plan)
+    check(y, x, at, theta_of(dim, 10000.0), dtype, interleaved, 0.5)
+    off = torch.empty(rows * heads * head_dim + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)     # no piece of which lies on 16 bytes
+    assert torch.equal(ec.rotary(x, at, plan, out=off), y)
+    ec.rotary(x, at, plan, out=x)
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,heads,head_dim,dim,pad", [(1, 1, 2, 2, 0), (1, 64, 128, 128, 0), (3, 5, 64, 64, 8), (5, 3, 128, 64, 4), (7, 2, 96, 38, 0),
                                                          (2, 7, 80, 22, 3), (33, 9, 512, 512, 0), (17, 4, 6, 4, 1), (1000, 36, 128, 128, 0),
                                                          (65, 1, 3, 2, 0), (257, 1024, 2, 2, 2)])

@@ -192,10 +192,10 @@ def test_the_binding_refuses():
             call()
     with pytest.raises(ec.EcError):
         ec.rotary_plan(7, device="cpu")
-    assert binding._cache_struct(ec.load_library(), c).pages == 3
+    assert binding._cache_struct(torch, c).pages == 3
     for data in (c.data[:-1], c.data.float(), c.data[::2]):
         with pytest.raises(ValueError, match="kv_cache"):
-            binding._cache_struct(ec.load_library(), c._replace(data=data))
+            binding._cache_struct(torch, c._replace(data=data))
 
 
 def test_the_plain_quantiser_of_the_tests():
