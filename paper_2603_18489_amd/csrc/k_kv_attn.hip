@@ -135,10 +135,10 @@ struct Pages {
 // first chunks settle it for most queries.  (Probabilities of up to 2^kLag are as exact as those of up to 1: all of this is floating point.)
 constexpr float kLag = 8.f;
 
-// largest of the scores of 16 queries and 32 keys (S^T: a lane has 8 neighbouring keys of query lane & 15), in every lane of the query
-__device__ __forceinline__ float top_score(const f32x4 (&sc)[2], float scale) {
-  return max_of_swap32(max_of_swap16(max_of_8(sc[0], sc[1]))) * scale;
-}
+// The scores of 16 queries and 32 keys (S^T: a lane has 8 neighbouring keys of query lane & 15): a lane's largest, which alone says whether the
+// maximum has to move, and the query's, in each of its lanes
+__device__ __forceinline__ float top_of_lane(const f32x4 (&sc)[2], float scale) { return max_of_8(sc[0], sc[1]) * scale; }
+__device__ __forceinline__ float top_of_query(float lane_top) { return max_of_swap32(max_of_swap16(lane_top)); }
 // the maximum m moves to mx, and what has been added up with it
 template <int HT, typename Sum> __device__ __forceinline__ void move_top(f32x4 (&acc)[HT], float& m, Sum& l, float mx) {
   const float m_new = max_of(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
@@ -307,8 +307,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     bf16x8 pf[QT], pl[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const float mx = top_score(sc[t], a.scale);
-      if (__builtin_amdgcn_ballot_w64(mx > m_run[t] + kLag) != 0) move_top(acc[t], m_run[t], l_run[t], mx);
+      const float mx = top_of_lane(sc[t], a.scale);
+      if (__builtin_amdgcn_ballot_w64(mx > m_run[t] + kLag) != 0) move_top(acc[t], m_run[t], l_run[t], top_of_query(mx));
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -427,14 +427,13 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   }
 }
 
-// 16 codes of values, of 8 keys whose powers of two are the bytes of vs, as bfloat16
+// 16 codes of values, of 8 keys whose powers of two are the bytes of vs, as bfloat16.  (The conversion takes a factor's exponent bits alone.)
 __device__ __forceinline__ void widen_values(u32x4 v, u32x2 vs, u32x4& x, u32x4& y) {
   union { bf16x2 h; uint32_t u; } a, b;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {   // keys 2 k and 2 k + 1
-    const uint32_t two = vs[k >> 1] >> (16 * (k & 1));
-    const float f = power_of(two & 255u), g = power_of((two >> 8) & 255u);
-    const uint32_t w = v[k >> 1], z = v[2 + (k >> 1)];
+    const uint32_t s = vs[k >> 1], w = v[k >> 1], z = v[2 + (k >> 1)];
+    const float f = __uint_as_float(k & 1 ? s << 7 : s << 23), g = __uint_as_float(k & 1 ? s >> 1 : s << 15);
     a.h = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, false);
     b.h = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, g, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, g, false);
     x[k] = (a.u & 0xffffu) | (b.u & 0xffff0000u);
@@ -583,12 +582,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     bool up = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      mx[t] = top_score(sc[t], a.scale);
+      mx[t] = top_of_lane(sc[t], a.scale);
       up = up || mx[t] > m_run[t] + kLag;
     }
     if (__builtin_amdgcn_ballot_w64(up) != 0) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t) move_top(acc[t], m_run[t], l_run[t], mx[t]);
+      for (int t = 0; t < QT; ++t) move_top(acc[t], m_run[t], l_run[t], top_of_query(mx[t]));
     }
     bf16x8 pf[QT];
 #pragma unroll
