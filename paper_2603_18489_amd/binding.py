@@ -548,17 +548,20 @@ def mxfp4_linear(x, w: Mxfp4Matrix, dtype=None, stream=None):
 
 def _heads_of(x, what: str):
     """rows, heads, components and the two strides of a tensor [rows, heads, head_dim] whose components are next to each other"""
-    _need(x.dim() == 3, f"{what} must be [rows, heads, head_dim]")
+    if x.dim() != 3:
+        raise ValueError(f"{what} must be [rows, heads, head_dim]")
     rows, heads, dim = x.shape
-    _need(max(rows, heads, dim) <= _INT_MAX, "at most 2^31 - 1 rows, heads and components")
     ld, ld_head, one = x.stride()
-    _need(one == 1 or dim <= 1, "the components of a head must be next to each other")
+    if rows > _INT_MAX or heads > _INT_MAX or dim > _INT_MAX:
+        raise ValueError("at most 2^31 - 1 rows, heads and components")
+    if one != 1 and dim > 1:
+        raise ValueError("the components of a head must be next to each other")
     return rows, heads, dim, ld if rows > 1 else 0, ld_head if heads > 1 else 0
 
 
-def _ints(t, size, what: str):
-    import torch
-    _need(t.dtype == torch.int32 and tuple(t.shape) == size and t.is_contiguous(), f"{what} must be contiguous int32 {list(size)}")
+def _ints(torch, t, size, what: str):
+    if t.dtype != torch.int32 or t.shape != size or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 {list(size)}")
 
 
 class RotaryPlan(NamedTuple):
@@ -588,20 +591,26 @@ def rotary(x, positions, plan: RotaryPlan, inverse: bool = False, out=None, stre
     import torch
     kind = _plain_type(x.dtype)
     rows, heads, dim, ld, ld_head = _heads_of(x, "x")
-    _ints(positions, (rows,), "positions")
-    _need(plan.turns.dtype == torch.float64 and plan.turns.is_contiguous() and tuple(plan.turns.shape) == (plan.dim // 2,),
-          "turns must be contiguous float64 [dim/2], as rotary_plan makes them")
+    _ints(torch, positions, (rows,), "positions")
+    turns, turning, interleaved, amplitude = plan
+    if turns.dtype != torch.float64 or turns.shape != (turning // 2,) or not turns.is_contiguous():
+        raise ValueError("turns must be contiguous float64 [dim/2], as rotary_plan makes them")
     if out is not None:
         _need(out.dtype == x.dtype and out.shape == x.shape, "out must have x's shape and type")
     lib = _lib or load_library()
 
     def call(raw):
-        y = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device) if out is None else out
-        _, _, _, to, to_head = _heads_of(y, "out")
-        _done(lib, lib.ec_rotary(x.data_ptr(), kind, rows, heads, dim, ld, ld_head, positions.data_ptr(), plan.turns.data_ptr(), plan.dim,
-                                 plan.interleaved, plan.amplitude, inverse, y.data_ptr(), to, to_head, raw))
+        if out is None:
+            y, to, to_head = torch.empty((rows, heads, dim), dtype=x.dtype, device=x.device), heads * dim, dim
+        else:
+            y = out
+            _, _, _, to, to_head = _heads_of(y, "out")
+        _done(lib, lib.ec_rotary(x.data_ptr(), kind, rows, heads, dim, ld, ld_head, positions.data_ptr(), turns.data_ptr(), turning,
+                                 interleaved, amplitude, inverse, y.data_ptr(), to, to_head, raw))
         return y
-    return _place(stream, call, x, positions, plan.turns, *(() if out is None else (out,)))
+    if out is None:
+        return _place(stream, call, x, positions, turns)
+    return _place(stream, call, x, positions, turns, out)
 
 
 class KvCache(NamedTuple):
@@ -645,7 +654,7 @@ def kv_write(cache: KvCache, k, v, slots, stream=None) -> None:
     _need(v.dtype == k.dtype and v.shape == k.shape, "v must have k's shape and type")
     _, _, _, v_ld, v_head = _heads_of(v, "v")
     _need((heads, dim) == (cache.kv_heads, cache.head_dim), "k and v have other heads than the cache")
-    _ints(slots, (rows,), "slots")
+    _ints(torch, slots, (rows,), "slots")
     lib = _lib or load_library()
 
     def call(raw):
@@ -660,16 +669,17 @@ def kv_read(cache: KvCache, slots, dtype=None, stream=None):
     import torch
     dtype = torch.bfloat16 if dtype is None else dtype
     kind = _plain_type(dtype)
-    _need(slots.dim() == 1, "slots must be contiguous int32 [rows]")
+    if slots.dim() != 1 or slots.shape[0] > _INT_MAX:
+        raise ValueError("slots must be contiguous int32 [rows], at most 2^31 - 1")
     rows = slots.shape[0]
-    _ints(slots, (rows,), "slots")
-    _need(rows <= _INT_MAX, "at most 2^31 - 1 rows")
+    _ints(torch, slots, (rows,), "slots")
     lib = _lib or load_library()
 
     def call(raw):
         c = _cache_struct(torch, cache)
-        k, v = (torch.empty((rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.data.device) for _ in range(2))
         head, ld = cache.head_dim, cache.kv_heads * cache.head_dim
+        k = torch.empty((rows, cache.kv_heads, head), dtype=dtype, device=cache.data.device)
+        v = torch.empty_like(k)
         _done(lib, lib.ec_kv_read(C.byref(c), slots.data_ptr(), rows, k.data_ptr(), v.data_ptr(), kind, ld, head, ld, head, raw))
         return k, v
     return _place(stream, call, cache.data, slots)
@@ -684,42 +694,49 @@ def kv_attention(q, cache: KvCache, table, lengths, starts=None, max_rows: Optio
     the host to be less than all rows and the whole table; what is beyond is not computed.  scale: 1 / sqrt(head_dim) by default.  Without `out`
     the rows of no sequence are zeros; with it they are left as they were.  No gradients."""
     import torch
-    _need(q.dtype == torch.bfloat16, "q must be bfloat16")
+    if q.dtype != torch.bfloat16:
+        raise ValueError("q must be bfloat16")
     rows, heads, dim, ld, ld_head = _heads_of(q, "q")
-    _need(dim == cache.head_dim, "q has another head_dim than the cache")
-    _need(table.dim() == 2 and table.dtype == torch.int32 and (table.shape[1] <= 1 or table.stride(1) == 1), "table must be int32 [seqs, pages]")
+    if dim != cache.head_dim:
+        raise ValueError("q has another head_dim than the cache")
+    if table.dim() != 2 or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be int32 [seqs, pages]")
     seqs, width = table.shape
-    _need(max(seqs, width) <= _INT_MAX, "at most 2^31 - 1 sequences and pages")
-    _ints(lengths, (seqs,), "lengths")
+    _ints(torch, lengths, (seqs,), "lengths")
     tensors = [cache.data, q, table, lengths]
     if starts is not None:
-        _ints(starts, (seqs + 1,), "starts")
+        _ints(torch, starts, (seqs + 1,), "starts")
         tensors.append(starts)
+        max_rows = rows if max_rows is None else min(max_rows, rows)
     else:
-        _need(seqs > 0 and rows % seqs == 0 and max_rows in (None, rows // seqs), "without starts every sequence has rows / seqs rows")
+        if seqs < 1 or rows % seqs or max_rows not in (None, rows // seqs):
+            raise ValueError("without starts every sequence has rows / seqs rows")
         max_rows = rows // seqs
     prefix_pages = 0
     if prefix is not None:
         _need(prefix.dim() == 1, "prefix must be contiguous int32 [pages]")
         prefix_pages = prefix.shape[0]
-        _ints(prefix, (prefix_pages,), "prefix")
+        _ints(torch, prefix, (prefix_pages,), "prefix")
         tensors.append(prefix)
     if out is not None:
         _need(out.dtype == q.dtype and out.shape == q.shape, "out must have q's shape and type")
         tensors.append(out)
-    max_rows = rows if max_rows is None else min(max_rows, rows)
-    max_keys = min(width * cache.page, _INT_MAX) if max_keys is None else max_keys
-    _need(max(prefix_len, prefix_pages, max_keys) <= _INT_MAX and min(prefix_len, max_rows, max_keys) >= 0, "lengths must be in [0, 2^31)")
+    if max_keys is None:
+        max_keys = min(width * cache.page, _INT_MAX)
+    if not (0 <= max_rows and 0 <= max_keys <= _INT_MAX and 0 <= prefix_len <= _INT_MAX and prefix_pages <= _INT_MAX and seqs <= _INT_MAX and width <= _INT_MAX):
+        raise ValueError("sizes and lengths must be in [0, 2^31)")
     lib = _lib or load_library()
     cfg = ec_kv_attention_cfg(rows, heads, seqs, max_rows, max_keys, width, prefix_pages, prefix_len, causal,
                               dim ** -0.5 if scale is None else scale, table.stride(0) if seqs > 1 else width)
 
     def call(raw):
         c = _cache_struct(torch, cache)
-        y = out
-        if y is None:
+        if out is None:
             y = (torch.empty if starts is None else torch.zeros)((rows, heads, dim), dtype=q.dtype, device=q.device)
-        _, _, _, to, to_head = _heads_of(y, "out")
+            to, to_head = heads * dim, dim
+        else:
+            y = out
+            _, _, _, to, to_head = _heads_of(y, "out")
         size = lib.ec_kv_attention_workspace_bytes(C.byref(c), C.byref(cfg))
         ws, at = _workspace(torch, size, q.device)
         _done(lib, lib.ec_kv_attention(C.byref(c), C.byref(cfg), q.data_ptr(), ld, ld_head, table.data_ptr(), lengths.data_ptr(),
