@@ -143,18 +143,14 @@ static void launch_rotary_v(const RotaryArgs& a, bool interleaved, hipStream_t s
   else rotary_kernel<T, V, false><<<(unsigned)blocks, 256, lds, s>>>(a, RB);
 }
 
-void launch_rotary(const void* x, bool bf16, long rows, int heads, int head_dim, size_t ld, size_t ld_head, const int* positions,
-                   const double* turns, int dim, bool interleaved, float amplitude, bool inverse, void* out, size_t out_ld,
-                   size_t out_ld_head, hipStream_t s) {
-  const RotaryArgs a = {x, out, ld, ld_head, out_ld, out_ld_head, rows, heads, head_dim, dim, positions, turns, amplitude,
-                        inverse ? -1.f : 1.f};
+static void launch_rotary_rows(const RotaryArgs& a, bool bf16, bool interleaved, hipStream_t s) {
   // the largest power of two that everything is a multiple of
-  const size_t es = bf16 ? 2 : 4;
-  const size_t all = ld | ld_head | out_ld | out_ld_head | (size_t)(dim / 2) | (size_t)(head_dim - dim) | (size_t)x / es | (size_t)out / es;
+  const size_t es = bf16 ? 2 : 4, strides = a.ld | a.ld_head | a.out_ld | a.out_ld_head;
+  const size_t all = strides | (size_t)(a.dim / 2) | (size_t)(a.head_dim - a.dim) | (size_t)a.x / es | (size_t)a.out / es;
   const int v = all % 8 == 0 && bf16 ? 8 : all % 4 == 0 ? 4 : all % 2 == 0 ? 2 : 1;
   // (22273 x 64 heads of 128 in bfloat16, of which 38 components turn: 325 us pair by pair; 24576 rows of them through LDS: 230)
-  const size_t whole = (ld | ld_head | out_ld | out_ld_head | (size_t)head_dim) * es | (size_t)x | (size_t)out;
-  if (v < (bf16 ? 4 : 2) && whole % 16 == 0 && (rows > 1 || heads > 1)) {
+  const size_t whole = (strides | (size_t)a.head_dim) * es | (size_t)a.x | (size_t)a.out;
+  if (v < (bf16 ? 4 : 2) && whole % 16 == 0 && (a.rows > 1 || a.heads > 1)) {
     if (bf16) launch_rotary_any<bf16_t, 8>(a, interleaved, s);
     else launch_rotary_any<float, 4>(a, interleaved, s);
     return;
@@ -169,6 +165,17 @@ void launch_rotary(const void* x, bool bf16, long rows, int heads, int head_dim,
     else if (v == 2) launch_rotary_v<float, 2>(a, interleaved, s);
     else launch_rotary_v<float, 1>(a, interleaved, s);
   }
+}
+
+void launch_rotary(const void* x, bool bf16, long rows, int heads, int head_dim, size_t ld, size_t ld_head, const int* positions,
+                   const double* turns, int dim, bool interleaved, float amplitude, bool inverse, void* out, size_t out_ld,
+                   size_t out_ld_head, hipStream_t s) {
+  // A launch has less than 2^32 threads: of 2^23 heads, or of one row, both kernels take fewer than 2^23 blocks of 256
+  const long most = max(1L, (1L << 23) / heads);
+  const size_t es = bf16 ? 2 : 4;
+  for (long r = 0; r < rows; r += most)
+    launch_rotary_rows({(const char*)x + r * ld * es, (char*)out + r * out_ld * es, ld, ld_head, out_ld, out_ld_head, min(most, rows - r), heads,
+                        head_dim, dim, positions + r, turns, amplitude, inverse ? -1.f : 1.f}, bf16, interleaved, s);
 }
 
 }  // namespace ec

@@ -145,3 +145,19 @@ def test_no_rows_infinities_and_a_graph():
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     assert torch.equal(ec.rotary(x, at, plan, stream=s), out)
+
+
+@pytest.mark.parametrize("dtype,heads,head_dim,dim", [("bf16", 40, 8, 6), ("bf16", 9, 126, 126), ("f32", 35, 4, 2)])
+def test_rows_of_more_than_one_launch(dtype, heads, head_dim, dim):
+    """up to 2^24 rows, more threads than one launch may have; in place, and every stretch as a call of its own gives it"""
+    rows = 2 ** 24
+    plan, at = ec.rotary_plan(dim), torch.arange(rows, dtype=torch.int32, device="cuda").neg_()
+    x = torch.empty((rows, heads, head_dim), dtype=DTYPES[dtype], device="cuda")
+    x[:] = torch.randn((rows, 1, 1), device="cuda").to(x.dtype)
+    x[:, :, ::2] *= 0.5
+    each = 2 ** 23 // heads
+    spots = [slice(max(0, r - 3), min(rows, r + 5)) for r in (0, each, 2 * each, rows - each, rows // 2, rows)]
+    want = [ec.rotary(x[s].clone(), at[s], plan) for s in spots]
+    assert ec.rotary(x, at, plan, out=x) is x
+    for s, w in zip(spots, want):
+        assert torch.equal(x[s], w)
