@@ -482,18 +482,19 @@ int ec_kv_read(const ec_kv_cache *cache, const int32_t *slots, int32_t rows, voi
  * All sequences see the first prefix_len tokens of the pages prefix[] before their own, which are read once for all of them.
  *   out[r, h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q[r, h] . k_j),  over the prefix and the sequence's keys; of these, under causal
  * != 0, row i of n sees the keys before lengths[b] - n + i + 1.  Heads h of a group of heads / kv_heads share kv head h / group.  A row that
- * sees no key gets zeros, and keys that it does not see are without effect, NaN among them.  Probabilities are rounded to bfloat16 once,
- * everything else is held in float32 and the result rounded to bfloat16.
- * Kept inside the buffers whatever the tables hold: starts are clamped to [0, rows], a sequence's rows beyond max_rows and rows of no sequence are
- * left as they were, lengths are clamped to [0, max_keys], and the tokens of a page outside [0, pages) are not seen. */
+ * sees no key, or scores of -infinity alone, gets zeros, and keys that it does not see are without effect, NaN among them.  Probabilities are
+ * rounded to bfloat16 (in two parts, 2^-17 together, for up to 16 rows of a group's heads: max_rows group <= 16), everything else is held in float32 and
+ * the result rounded to bfloat16.  The sums are of p_j v_j with p_j up to 256 and have to fit float32: magnitudes of v from 2^100 on may overflow.
+ * Kept inside the buffers whatever the tables hold: starts are clamped to [0, rows] (and must ascend: no row is of two sequences), a sequence's rows beyond
+ * max_rows (which n does not count) and rows of no sequence are left as they were, lengths are clamped to [0, max_keys], and the tokens of a page outside [0, pages) are not seen. */
 typedef struct {
   int32_t rows, heads;           /* 0 .. 2^20; a multiple of kv_heads, at most 1024 */
   int32_t seqs;                  /* 1 .. 65535 */
-  int32_t max_rows, max_keys;    /* most of a sequence; what the launches are sized by: the closer, the cheaper */
+  int32_t max_rows, max_keys;    /* most of a sequence; what the launches are sized by: the closer, the cheaper.  max_keys at most 2^30 */
   int32_t table_pages;           /* pages of a sequence in the table: max_keys <= table_pages * page */
-  int32_t prefix_pages, prefix_len;
+  int32_t prefix_pages, prefix_len;   /* prefix_len <= prefix_pages * page, at most 2^30 */
   int32_t causal;
-  float scale;                   /* positive */
+  float scale;                   /* positive, at most 1e38 */
   size_t table_ld;               /* row stride of the table */
 } ec_kv_attention_cfg;
 /*  cfg        HOST, read before the call returns

@@ -12,6 +12,7 @@ constexpr int kHeadsMax = 1024;           // heads of a row, in and out of the c
 constexpr int kRotaryHeadDimMax = 512;
 constexpr int kKvRowsMax = 1 << 20;
 constexpr int kSeqsMax = 65535;
+constexpr int kKeysMax = 1 << 30;         // (the last chunk's end is an int)
 
 // The strides of [rows, heads, head_dim] let no two elements of a tensor that is written meet.
 bool apart(int64_t rows, int heads, int head_dim, size_t ld, size_t ld_head) {
@@ -50,10 +51,11 @@ const char* attention_error(const ec_kv_cache* c, const ec_kv_attention_cfg* a) 
   if (a->seqs < 1 || a->seqs > kSeqsMax) return "seqs must be in [1, 65535]";
   if (a->max_rows < 0 || a->max_rows > a->rows) return "max_rows must be in [0, rows]";
   if (a->table_pages < 0 || (a->seqs > 1 && a->table_ld < (size_t)a->table_pages)) return "table_pages must not be negative, nor table_ld smaller";
-  if (a->max_keys < 0 || a->max_keys > (int64_t)a->table_pages * c->page) return "max_keys must be in [0, table_pages * page]";
-  if (a->prefix_pages < 0 || a->prefix_len < 0 || a->prefix_len > (int64_t)a->prefix_pages * c->page)
-    return "prefix_len must be in [0, prefix_pages * page]";
-  if (!(a->scale > 0.f) || !std::isfinite(a->scale)) return "scale must be finite and positive";
+  if (a->max_keys < 0 || a->max_keys > kKeysMax || a->max_keys > (int64_t)a->table_pages * c->page)
+    return "max_keys must be in [0, table_pages * page], at most 2^30";
+  if (a->prefix_pages < 0 || a->prefix_len < 0 || a->prefix_len > kKeysMax || a->prefix_len > (int64_t)a->prefix_pages * c->page)
+    return "prefix_len must be in [0, prefix_pages * page], at most 2^30";
+  if (!(a->scale > 0.f) || !(a->scale <= 1e38f)) return "scale must be positive, at most 1e38";
   const int64_t queries = (int64_t)a->max_rows * (a->heads / c->kv_heads);
   if ((queries + 15) / 16 * a->seqs * c->kv_heads > INT32_MAX / 1024) return "too many rows of too many sequences: give a smaller max_rows";
   return nullptr;

@@ -223,6 +223,50 @@ def test_no_rows_no_keys_a_graph_and_another_stream():
     assert torch.equal(b.call(stream=s), want)
 
 
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("counts", [[1, 2], [20, 3], [150, 90]], ids=str)
+def test_powers_of_two_go_through(counts, cache):
+    """values of 2^80 and 2^-80, keys and queries that make up for each other: every step is exact in a power of two, so that the bits stay"""
+    b = Batch(counts, [100, 333], 4, 2, 128, 64, cache)
+    rng = np.random.default_rng(5)
+    k, v = (torch.from_numpy(rng.standard_normal((433, 2, 128)).astype(np.float32)).cuda() for _ in range(2))
+    ec.kv_write(b.cache, k, v, b.every)
+    want = b.call(causal=True)
+    for keys, values in ((40, 80), (-40, -80), (0, 90)):
+        ec.kv_write(b.cache, k * 2.0 ** keys, v * 2.0 ** values, b.every)
+        assert torch.equal(b.call(causal=True, q=b.q * 2.0 ** -keys), want * 2.0 ** values)
+
+
+def test_padding_two_calls_at_once_and_one_page_for_all():
+    """a batch padded with sequences of no keys, sequences that share a page, and two calls on two streams at the same time"""
+    b = Batch([2, 2, 2, 2], [64, 0, 500, 0], 28, 4, 128, 64, "e4m3", 700)
+    b.check(b.call(ragged=False))
+    b.check(b.call(ragged=False, causal=True), True)
+    table = np.tile(b.table[2], (4, 1))
+    same = ec.kv_attention(b.q, b.cache, ints(table), ints([500] * 4))
+    for s in range(4):
+        assert torch.equal(same[2 * s:2 * s + 2], ec.kv_attention(b.q[2 * s:2 * s + 2], b.cache, ints(table[:1]), ints([500])))
+    alone = b.call()
+    torch.cuda.synchronize()
+    outs, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        with torch.cuda.stream(s):
+            outs.append([b.call() for _ in range(10)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, alone) for some in outs for o in some)
+
+
+@pytest.mark.parametrize("n", [3, 40, 200])
+def test_rows_beyond_the_most_under_causal(n):
+    """a sequence of more rows than max_rows is one of max_rows rows: its first row sees lengths - max_rows + 1 keys"""
+    b = Batch([n + 5, n], [300, 250], 4, 2, 64, 32, "e4m3")
+    out = torch.full_like(b.q, 7.0)
+    b.call(causal=True, max_rows=n, out=out)
+    assert (out[n:n + 5] == 7).all()
+    less = torch.cat((b.q[:n], b.q[n + 5:]))
+    assert torch.equal(torch.cat((out[:n], out[n + 5:])), ec.kv_attention(less, b.cache, ints(b.table), ints(b.lengths), ints([0, n, 2 * n]), n, causal=True))
+
+
 def test_the_same_bits_every_time():
     b = Batch([34, 20, 1], [900, 1100, 40], 8, 4, 128, 64, "e4m3", 2000)
     first = b.call()

@@ -152,6 +152,12 @@ def test_attention_refuses(lib, bad):
     assert lib.ec_last_error(None)
 
 
+@pytest.mark.parametrize("bad", [dict(max_keys=2 ** 30 + 1), dict(prefix_len=2 ** 30 + 1), dict(scale=2e38)], ids=str)
+def test_attention_refuses_what_does_not_fit(lib, bad):
+    assert attention(lib, **dict(page=256, pages=1000, table_pages=2 ** 23, table_ld=2 ** 23, prefix_pages=2 ** 23) | bad) == ec.EC_ERR_ARG
+    assert lib.ec_last_error(None)
+
+
 def test_attention_workspace(lib):
     c = cache()
     for rows, seqs, keys, prefix in ((1, 1, 5000, 0), (3, 3, 100, 5000), (4, 4, 40, 1)):
