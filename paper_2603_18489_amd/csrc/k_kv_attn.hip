@@ -94,8 +94,7 @@ struct Part {
 // false: nothing to do.  EACH: queries of a block.  Blocks that read the same keys are kv_heads apart, next to each other otherwise: mostly on one
 // XCD, whose L2 they share.  Late rows, which see most under `causal`, go first.
 template <int EACH, bool PREFIX>
-__device__ __forceinline__ bool part_of(const Args& a, int tiles, Part& p) {
-  unsigned id = blockIdx.x;
+__device__ __forceinline__ bool part_of(const Args& a, unsigned id, int tiles, Part& p) {
   p.kvh = id % a.place.kv_heads;
   id /= a.place.kv_heads;
   const int tile = tiles - 1 - (int)(id % tiles);
@@ -216,18 +215,24 @@ template <int ES, int HD> struct Chunk {
 // queries leaves registers for a second chunk.  The power of two of a key's values multiplies its probability.
 // With one tile the matrix cores wait for memory, so that a probability can be two bfloat16 numbers, 2^-17 together, instead of one.
 // DIRECT: there is one slice, and the block writes the result.
+template <int HD, int QT, int W> struct Few {
+  static constexpr int HB = HD / 32, HT = HD / 16;
+  static constexpr int SLOT = HT * 64 + 32;     // float4 of a wave's part of a tile
+  static constexpr bool PARKED = QT > 2;        // queries in LDS, as a third tile's registers would spill others
+  static constexpr int LDS = W * SLOT + (PARKED ? QT * HB * 64 : 0);
+};
 template <int ES, int HD, int QT, int W, bool PREFIX, bool DIRECT>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a, int tiles) {
-  constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
+__device__ __forceinline__ void attend_few(const Args& a, unsigned id, int tiles, u32x4* mem) {
+  typedef Few<HD, QT, W> F;
+  constexpr int HB = F::HB, HT = F::HT, U = KvChunk<ES, HD>::kUnits, SLOT = F::SLOT;
+  constexpr bool PARKED = F::PARKED;
   typedef Chunk<ES, HD> C;
-  constexpr int SLOT = HT * 64 + 32;   // float4 of a wave's part of a tile
-  constexpr bool PARKED = QT > 2;      // queries in LDS, as a third tile's registers would spill others
-  __shared__ float4 lds[W * SLOT];
-  __shared__ u32x4 parked[PARKED ? QT * HB * 64 : 1];
+  float4* lds = (float4*)mem;
+  u32x4* parked = mem + W * SLOT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane >> 4, col = lane & 15;
   Part part;
-  if (!part_of<16 * QT, PREFIX>(a, tiles, part)) return;
+  if (!part_of<16 * QT, PREFIX>(a, id, tiles, part)) return;
 
   bf16x8 qf[PARKED ? 1 : QT][HB];
   int seen[QT];
@@ -447,17 +452,17 @@ __device__ __forceinline__ void widen_values(u32x4 v, u32x2 vs, u32x4& x, u32x4&
 // are widened once for all, values with their powers of two, into one of two stages of LDS; the next one's pieces are on their way meanwhile.  The
 // probabilities' sums are a product of P^T with ones: what is rounded is what is added up.
 // Chunks that hold a key which some query does not see, or values that are NaN, go a slower way; the others' code has one rare branch.
+template <int HD> constexpr int kManyLds = 2 * (2 * HD / 32 + HD / 16) * 64;
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_many_kernel(Args a, int tiles) {
+__device__ __forceinline__ void attend_many(const Args& a, unsigned id, int tiles, u32x4* lds) {
   constexpr int HB = HD / 32, HT = HD / 16, U = KvChunk<ES, HD>::kUnits;
   constexpr int KP = 2 * U * 64, ALL = KvChunk<ES, HD>::kBytes / 16, N = ALL / 256;   // pieces of 16 bytes: keys, all, a thread's
   constexpr int KF = 2 * HB * 64, STAGE = KF + HT * 64;                                  // of a stage: keys, all
-  static_assert(ALL % 256 == 0 && KP % 64 == 0, "a wave's pieces are keys or values");
-  __shared__ u32x4 lds[2 * STAGE];
+  static_assert(ALL % 256 == 0 && KP % 64 == 0 && 2 * STAGE == kManyLds<HD>, "a wave's pieces are keys or values");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = lane >> 4, col = lane & 15;
   Part part;
-  if (!part_of<64 * QT, PREFIX>(a, tiles, part)) return;
+  if (!part_of<64 * QT, PREFIX>(a, id, tiles, part)) return;
   const int first = part.first + wave * 16 * QT;
 
   bf16x8 qf[QT][HB];
@@ -639,6 +644,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 }
 
+template <int ES, int HD, int QT, int W, bool PREFIX, bool DIRECT>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a) {
+  __shared__ u32x4 lds[Few<HD, QT, W>::LDS];
+  attend_few<ES, HD, QT, W, PREFIX, DIRECT>(a, blockIdx.x, 1, lds);
+}
+template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_many_kernel(Args a, int tiles) {
+  __shared__ u32x4 lds[kManyLds<HD>];
+  attend_many<ES, HD, QT, PREFIX, DIRECT>(a, blockIdx.x, tiles, lds);
+}
+// The prefix, and sequences of up to 16 queries: one launch.  The sequences' blocks wait for memory and leave the matrix cores to the prefix', whose
+// blocks go first, as they take longer (64 rows of 28 heads on 4, 16384 keys before 511 each: 54 us in two launches, 46 in one, 55 the other way round).
+template <int ES, int HD, bool MANY, int QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_both_kernel(Args a, int tiles, unsigned prefix) {
+  constexpr int PRE = MANY ? kManyLds<HD> : Few<HD, QT, 4>::LDS, OWN = Few<HD, 1, 4>::LDS;
+  __shared__ u32x4 lds[PRE > OWN ? PRE : OWN];
+  if (blockIdx.x >= prefix) attend_few<ES, HD, 1, 4, false, false>(a, blockIdx.x - prefix, 1, lds);
+  else if constexpr (MANY) attend_many<ES, HD, QT, true, false>(a, blockIdx.x, tiles, lds);
+  else attend_few<ES, HD, QT, 4, true, false>(a, blockIdx.x, tiles, lds);
+}
+
 // The slices of a row of queries meet in their order: W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
 // lane's each, two at most, so that all of them are on their way at once.
 constexpr int kSlicesMax = 64;    // of the prefix, and of a sequence's own keys
@@ -757,11 +783,19 @@ void launch_cut(const Args& a, const Cut& c, hipStream_t s) {
     else if (c.qt == 2) kv_attention_many_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
     else kv_attention_many_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
   } else {
-    if (c.qt == 1 && DIRECT && blocks <= 256) kv_attention_few_kernel<ES, HD, 1, 8, PREFIX, DIRECT><<<(unsigned)blocks, 512, 0, s>>>(a, 1);
-    else if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
-    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
-    else kv_attention_few_kernel<ES, HD, 3, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, 1);
+    if (c.qt == 1 && DIRECT && blocks <= 256) kv_attention_few_kernel<ES, HD, 1, 8, PREFIX, DIRECT><<<(unsigned)blocks, 512, 0, s>>>(a);
+    else if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else kv_attention_few_kernel<ES, HD, 3, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
   }
+}
+
+template <int ES, int HD, bool MANY>
+void launch_both(const Args& a, const Plan& p, hipStream_t s) {
+  const unsigned prefix = (unsigned)(a.place.kv_heads * p.prefix.slices * p.prefix.tiles), blocks = prefix + (unsigned)(a.place.kv_heads * a.seqs * p.own.slices);
+  if (p.prefix.qt == 1) kv_attention_both_kernel<ES, HD, MANY, 1><<<blocks, 256, 0, s>>>(a, p.prefix.tiles, prefix);
+  else if (p.prefix.qt == 2) kv_attention_both_kernel<ES, HD, MANY, 2><<<blocks, 256, 0, s>>>(a, p.prefix.tiles, prefix);
+  else kv_attention_both_kernel<ES, HD, MANY, 3><<<blocks, 256, 0, s>>>(a, p.prefix.tiles, prefix);
 }
 
 template <int ES, int HD>
@@ -781,8 +815,13 @@ void launch(const KvCache& c, const KvAttention& k, const Plan& p, void* workspa
   a.part = (float*)workspace;
   a.sums = (float2*)((char*)workspace + part_bytes(c, k, total));
   if (total == 1) return launch_cut<ES, HD, false, true>(a, p.own, s);
-  if (a.prefix_slices) launch_cut<ES, HD, true, false>(a, p.prefix, s);
-  launch_cut<ES, HD, false, false>(a, p.own, s);
+  if (a.prefix_slices && !p.own.many && p.own.qt == 1) {
+    if (p.prefix.many) launch_both<ES, HD, true>(a, p, s);
+    else launch_both<ES, HD, false>(a, p, s);
+  } else {
+    if (a.prefix_slices) launch_cut<ES, HD, true, false>(a, p.prefix, s);
+    launch_cut<ES, HD, false, false>(a, p.own, s);
+  }
   const long queries = (long)a.max_rows * a.heads;
   if (total > 8) kv_attention_join_kernel<HD, 4><<<dim3((unsigned)queries, a.seqs), 256, 0, s>>>(a);
   else kv_attention_join_kernel<HD, 1><<<dim3((unsigned)((queries + 3) / 4), a.seqs), 256, 0, s>>>(a);
