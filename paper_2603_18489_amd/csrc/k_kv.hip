@@ -165,6 +165,7 @@ template <int ROWS> struct Tile {
   int runs;
   bool there;             // all of the block's rows have a slot
   unsigned long long single;   // the block's rows that are in no run and have a slot, a bit each
+  unsigned long long have[2], eight[2], linked[2];
   int low, high;          // written: of the rows' slots
   int row_of[2048];       // written: by slot % 2048, 1 + the row (of ALL) with it, 0: none, -1: several
 };
@@ -174,7 +175,7 @@ template <int ROWS> struct Tile {
 template <int ROWS, bool WRITE>
 __device__ __forceinline__ void find_runs(const KvRows& a, int row0, Tile<ROWS>& t) {
   typedef Tile<ROWS> Tl;
-  static_assert(ROWS <= 64 && Tl::ALL <= 256, "a bit for each row, a thread for each");
+  static_assert(ROWS <= 64 && Tl::ALL <= 128, "a bit for each row, a thread for each");
   const int i = threadIdx.x, r = row0 - Tl::SIDE + i;
   int s = -1;
   if (i < Tl::ALL) {
@@ -226,23 +227,30 @@ __device__ __forceinline__ void find_runs(const KvRows& a, int row0, Tile<ROWS>&
       if (i < to - tail) look(tail + i, a.slots[tail + i]);
     }
   }
+  // a bit for each row: has a slot; has a multiple of 8; the row behind it has the slot behind it
+  __syncthreads();
+  if (i < 128) {
+    const int at = i < Tl::ALL ? t.slot[i] : -1, next = i + 1 < Tl::ALL ? t.slot[i + 1] : -1;
+    const unsigned long long have = __ballot(at >= 0), eight = __ballot(at >= 0 && (at & 7) == 0), linked = __ballot(at >= 0 && next == at + 1);
+    if ((i & 63) == 0) { t.have[i >> 6] = have; t.eight[i >> 6] = eight; t.linked[i >> 6] = linked; }
+  }
   __syncthreads();
   if (i < 64) {
-    bool run = false, single = false;
-    if (i < ROWS) {
-      auto starts = [&](int at) {   // whether a run begins at row `at` of the tile
-        const int s0 = t.slot[at];
-        bool ok = s0 >= 0 && (s0 & 7) == 0;
-        for (int k = 1; k < 8; ++k) ok = ok && t.slot[at + k] == s0 + k;
-        return ok;
-      };
-      run = starts(Tl::SIDE + i);
-      single = t.slot[Tl::SIDE + i] >= 0;
-      for (int k = 0; k < 8 && single; ++k) single = !starts(Tl::SIDE + i - k);
+    typedef unsigned __int128 Bits;
+    auto bits = [](const unsigned long long (&w)[2]) { return (Bits)w[1] << 64 | w[0]; };
+    const Bits have = bits(t.have), one = bits(t.linked), two = one & one >> 1, four = two & two >> 2;
+    const Bits run = bits(t.eight) & four & two >> 4 & one >> 6;
+    Bits in_run = run | run << 1;
+    in_run |= in_run << 2;
+    in_run |= in_run << 4;
+    constexpr unsigned long long BLOCK = ~0ull >> (64 - ROWS);
+    const unsigned long long runs = (unsigned long long)(run >> Tl::SIDE) & BLOCK;
+    if (i < ROWS && ((runs >> i) & 1)) t.first[__popcll(runs & ((1ull << i) - 1))] = i;
+    if (i == 0) {
+      t.runs = __popcll(runs);
+      t.single = (unsigned long long)((have & ~in_run) >> Tl::SIDE) & BLOCK;
+      t.there = ((unsigned long long)(have >> Tl::SIDE) & BLOCK) == BLOCK;
     }
-    const unsigned long long runs = __ballot(run), singles = __ballot(single), gone = __ballot(i < ROWS && t.slot[Tl::SIDE + min(i, ROWS - 1)] < 0);
-    if (run) t.first[__popcll(runs & ((1ull << i) - 1))] = i;
-    if (i == 0) { t.runs = __popcll(runs); t.single = singles; t.there = gone == 0; }
   }
   __syncthreads();
 }
