@@ -4,9 +4,9 @@
 // what was added up so far multiplied by exp(m_old - m_new) whenever m grows.  Per 32 keys (a chunk) and 16 rows of queries (a row of
 // queries: one head of one row, the heads of a kv head's group next to each other):
 //   S^T[keys x queries] = K . Q^T, softmax down the keys, O^T[components x queries] += V^T . P^T
-// with the operands as they lie in the cache.  e4m3 keys are widened to bfloat16 with their power of two, exactly; values are widened
-// without it, exactly, and the probability takes it, an exact product again, before its one rounding to bfloat16 (2^-9 of it at most).
-// Scores, maxima, sums and outputs are float32.
+// with the operands as they lie in the cache.  e4m3 keys are widened to bfloat16 with their power of two, exactly.  Values are widened
+// so too where many queries share them; few queries' probabilities take it instead, an exact product again, before they are rounded to bfloat16 (2^-8 of them
+// at most, 2^-16 with up to 16 queries).  Scores, maxima and sums are float32.
 //
 // Keys are cut into slices of chunks, a block each; the slices' (m, sum, O) meet in a second launch, in their order.  The prefix' slices take
 // the rows of all sequences at once, so that its keys are read once for all.  A query that sees no key gets zeros: m begins at the lowest
@@ -213,8 +213,10 @@ template <int ES, int HD> struct Chunk {
 // Few queries: up to 48 of a sequence and kv head.  A block's waves go through the chunks of its slice in turn, each with all QT tiles of 16
 // queries and a chunk's pieces in registers, and meet in LDS.  The next chunk's keys are on their way from when this one's are used, the values too; one tile of
 // queries leaves registers for a second chunk.  The power of two of a key's values multiplies its probability.
-// With one tile the matrix cores wait for memory, so that a probability can be two bfloat16 numbers, 2^-17 together, instead of one.
+// With one tile the matrix cores wait for memory, so that a probability can be two bfloat16 numbers, 2^-16 together, instead of one.
 // DIRECT: there is one slice, and the block writes the result.
+// 1 row over 131071 bfloat16 keys (28 heads on 4): 48 us, 5.7 TB/s.  16 sequences of up to 34 rows over up to 1536 e4m3 keys (32 heads): 32 us, 3 tiles,
+// as long as their bytes and products take one after the other.  1 row over 1000 keys: 8.2, a chain of loads.
 template <int HD, int QT, int W> struct Few {
   static constexpr int HB = HD / 32, HT = HD / 16;
   static constexpr int SLOT = HT * 64 + 32;     // float4 of a wave's part of a tile
@@ -451,6 +453,8 @@ __device__ __forceinline__ void widen_values(u32x4 v, u32x2 vs, u32x4& x, u32x4&
 // Many queries: a wave owns QT tiles of 16, a block 64 QT, and its waves go through the keys together.  Each chunk comes through registers, where codes
 // are widened once for all, values with their powers of two, into one of two stages of LDS; the next one's pieces are on their way meanwhile.  The
 // probabilities' sums are a product of P^T with ones: what is rounded is what is added up.
+// 16 x 1536 rows over 1536 e4m3 keys, 32 heads of 128: 645 to 720 us, 0.86 to 0.96 PFLOP/s.  What bounds it is the issue of instructions: a 16 x 16 x 32 product
+// takes a SIMD 17 cycles, beside which one more instruction is free, and softmax and widening add theirs.
 // Chunks that hold a key which some query does not see, or values that are NaN, go a slower way; the others' code has one rare branch.
 template <int HD> constexpr int kManyLds = 2 * (2 * HD / 32 + HD / 16) * 64;
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
@@ -665,7 +669,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   else attend_few<ES, HD, QT, 4, true, false>(a, blockIdx.x, tiles, lds);
 }
 
-// The slices of a row of queries meet in their order: W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
+// The slices of a row of queries meet in their order (28 heads, 64 rows, 33 slices: 30 MB in 7.5 us): W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
 // lane's each, two at most, so that all of them are on their way at once.
 constexpr int kSlicesMax = 64;    // of the prefix, and of a sequence's own keys
 
@@ -739,7 +743,7 @@ Cut cut(long queries, int chunks, long others, bool joined) {
   Cut c;
   c.many = queries > 48;
   if (c.many) {
-    // by what a tile takes (16 x 1536 rows over 1536 keys: 975, 778 and 757 us in tiles of 64, 128 and 192) and how full the last one is
+    // by what a tile takes (16 x 1536 rows over 1536 keys: 911, 737 and 718 us in tiles of 64, 128 and 192) and how full the last one is
     const double cost[3] = {1.29, 2 * 1.03, 3.0};
     double least = 0;
     for (int qt = 1; qt <= 3; ++qt) {
