@@ -483,8 +483,9 @@ int ec_kv_read(const ec_kv_cache *cache, const int32_t *slots, int32_t rows, voi
  *   out[r, h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q[r, h] . k_j),  over the prefix and the sequence's keys; of these, under causal
  * != 0, row i of n sees the keys before lengths[b] - n + i + 1.  Heads h of a group of heads / kv_heads share kv head h / group.  A row that
  * sees no key, or scores of -infinity alone, gets zeros, and keys that it does not see are without effect, NaN among them.  Probabilities are
- * rounded to bfloat16 (in two parts, 2^-16 together, for up to 16 rows of a group's heads: max_rows group <= 16), everything else is held in float32 and
- * the result rounded to bfloat16.  The sums are of p_j v_j with p_j up to 256 and have to fit float32: magnitudes of v from 2^100 on may overflow.
+ * rounded to bfloat16, as operands of matrix products: of a sequence's own keys in two parts, 2^-16 together, where max_rows group <= 16; of the prefix'
+ * keys, whose queries are the rows of the whole call, where rows group <= 16; in one part, 2^-8, elsewhere.  Everything else is held in float32 and
+ * the result rounded to bfloat16. The sums are of p_j v_j with p_j up to 256 and have to fit float32: magnitudes of v from 2^100 on may overflow.
  * Kept inside the buffers whatever the tables hold: starts are clamped to [0, rows] (and must ascend: no row is of two sequences), a sequence's rows beyond
  * max_rows (which n does not count) and rows of no sequence are left as they were, lengths are clamped to [0, max_keys], and the tokens of a page outside [0, pages) are not seen. */
 typedef struct {
