@@ -502,9 +502,11 @@ typedef struct {
  *  q, out     DEVICE bfloat16 [rows, heads, head_dim], 16-byte aligned, strides (as ec_rotary's) multiples of 8 elements; out must not overlap q
  *  table      DEVICE int32 [seqs, table_pages]; lengths DEVICE int32 [seqs]; starts DEVICE int32 [seqs + 1] or NULL; prefix DEVICE int32
  *             [prefix_pages] (may be NULL for prefix_len 0)
- *  workspace  DEVICE, 256-byte aligned, >= ec_kv_attention_workspace_bytes(cache, cfg) (0 for many sizes, and for arguments outside the limits;
- *             cache->data is not looked at); BORROWED for the call: calls that overlap in time, and captured graphs that may run side by
- *             side, need one each
+ *  workspace  DEVICE, 256-byte aligned, >= ec_kv_attention_workspace_bytes(cache, cfg) (0 for short sequences without a prefix, and for arguments outside the
+ *             limits; cache->data is not looked at); BORROWED for the call: calls that overlap in time, and captured graphs that may run side
+ *             by side, need one each.  One for so many rows, max_rows, seqs, max_keys and prefix_len serves less of each too, where all rows are of sequences
+ *             (rows <= seqs * max_rows).  It is at most about 51 MB (26 for head_dim 64) for own keys and as much for a prefix', or, with a prefix, 520 bytes
+ *             (264) to a head of a row for each of the two where that is more
  * Enqueues on hip_stream and returns without synchronising; may be captured.  Errors: EC_ERR_ARG, EC_ERR_WORKSPACE, EC_ERR_HIP. */
 size_t ec_kv_attention_workspace_bytes(const ec_kv_cache *cache, const ec_kv_attention_cfg *cfg);
 int ec_kv_attention(const ec_kv_cache *cache, const ec_kv_attention_cfg *cfg, const void *q, size_t q_ld, size_t q_ld_head,

@@ -767,6 +767,8 @@ struct Cut {
   bool many;
   int qt, tiles, split, slices;
 };
+constexpr int kBlocks = 512, kBlocksFew = 1024;   // blocks that fill the compute units: of many queries or several tiles, of one tile
+constexpr int kSliceChunks = 8, kUncut = 32;       // chunks of a slice at least; chunks that few queries' blocks take as one
 Cut cut(long queries, int chunks, long others, bool joined) {
   Cut c;
   c.many = queries > 48;
@@ -786,11 +788,11 @@ Cut cut(long queries, int chunks, long others, bool joined) {
     c.qt = (int)max(1L, (queries + 15) / 16);
     c.tiles = 1;
   }
-  const long want = (c.many || c.qt > 1 ? 512 : 1024) / max(others * c.tiles, 1L);     // blocks that fill the compute units
-  const long most = max(1, chunks / 8);                                    // (8 chunks to a slice at least)
+  const long want = (c.many || c.qt > 1 ? kBlocks : kBlocksFew) / max(others * c.tiles, 1L);
+  const long most = max(1, chunks / kSliceChunks);
   // Up to 1024 keys are not cut for few queries: 8 waves of a block are through them in 8.2 us where slices and their meeting take 7.1, but the second
   // launch costs the caller 4 (one row, 1000 keys, 28 heads on 4).
-  const int n = !c.many && !joined && chunks <= 32 ? 1 : (int)max(1L, min(min(want, most), (long)kSlicesMax));
+  const int n = !c.many && !joined && chunks <= kUncut ? 1 : (int)max(1L, min(min(want, most), (long)kSlicesMax));
   c.split = (chunks + n - 1) / n;
   c.slices = (chunks + c.split - 1) / c.split;
   return c;
@@ -803,8 +805,17 @@ Plan plan_of(const KvCache& c, const KvAttention& a) {
   if (a.prefix_len > 0) p.prefix = cut(a.rows * group, (a.prefix_len + 31) / 32, c.kv_heads, true);
   return p;
 }
-size_t part_bytes(const KvCache& c, const KvAttention& a, int slices) {
-  return ((size_t)a.rows * a.heads * slices * c.head_dim * 4 + 255) / 256 * 256;
+// `parts`: heads of rows times slices
+size_t part_bytes(const KvCache& c, size_t parts) { return (parts * c.head_dim * 4 + 255) / 256 * 256; }
+size_t parts_bytes(const KvCache& c, size_t parts) { return part_bytes(c, parts) + parts * sizeof(float2); }
+
+// Most parts that cut() can make of up to `heads` heads of rows, `queries` queries and `chunks` chunks, 0: they are never cut.  Of b blocks of
+// keys that are made at most, `others` x tiles x slices <= b where there are slices at all, so that there are b parts to a query of a tile: as many as 16 queries
+// of 1024 blocks, 48 or 192 of 512.
+size_t most_parts(size_t heads, long queries, int chunks, bool joined) {
+  const size_t slices = queries <= 48 && !joined && chunks <= kUncut ? 1 : max(1, min(chunks / kSliceChunks, kSlicesMax));
+  const long few = min(queries, 16L) * kBlocksFew, more = queries > 16 ? min(queries, 192L) * kBlocks : 0;
+  return slices == 1 ? 0 : min(heads * slices, (size_t)max(few, more));
 }
 
 template <int ES, int HD, bool PREFIX, bool DIRECT>
@@ -847,7 +858,7 @@ void launch(const KvCache& c, const KvAttention& k, const Plan& p, void* workspa
   a.split = p.own.split; a.slices = p.own.slices; a.prefix_split = p.prefix.split; a.prefix_slices = p.prefix.slices;
   const int total = a.slices + a.prefix_slices;
   a.part = (float*)workspace;
-  a.sums = (float2*)((char*)workspace + part_bytes(c, k, total));
+  a.sums = (float2*)((char*)workspace + part_bytes(c, (size_t)k.rows * k.heads * total));
   if (total == 1) return launch_cut<ES, HD, false, true>(a, p.own, s);
   if (a.prefix_slices && !p.own.many && p.own.qt == 1) {
     if (p.prefix.many) launch_both<ES, HD, true>(a, p, s);
@@ -863,10 +874,16 @@ void launch(const KvCache& c, const KvAttention& k, const Plan& p, void* workspa
 
 }  // namespace
 
+// Fewer rows have fewer tiles and more slices of keys: there is room for whatever calls of as many rows, sequences and keys or fewer need.  (Rows that are of no
+// sequence have parts too; with them it is what the call itself needs.)
 size_t kv_attention_workspace(const KvCache& c, const KvAttention& a) {
   const Plan p = plan_of(c, a);
   const int total = p.own.slices + p.prefix.slices;
-  return total == 1 ? 0 : part_bytes(c, a, total) + (size_t)a.rows * a.heads * total * 8;
+  const long group = a.heads / c.kv_heads;
+  const size_t heads = (size_t)a.rows * a.heads, here = total == 1 ? 0 : heads * total;
+  size_t parts = most_parts(heads, a.max_rows * group, max(1, (a.max_keys + 31) / 32), a.prefix_len > 0);
+  if (a.prefix_len > 0) parts = max(parts, heads) + max(most_parts(heads, a.rows * group, (a.prefix_len + 31) / 32, true), heads);
+  return parts_bytes(c, max(parts, here));
 }
 
 void launch_kv_attention(const KvCache& c, const KvAttention& a, void* workspace, hipStream_t s) {
