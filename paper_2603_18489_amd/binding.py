@@ -709,9 +709,10 @@ def kv_attention(q, cache: KvCache, table, lengths, starts=None, max_rows: Optio
         tensors.append(starts)
         max_rows = rows if max_rows is None else min(max_rows, rows)
     else:
-        if seqs < 1 or rows % seqs or max_rows not in (None, rows // seqs):
+        each = rows // max(seqs, 1)
+        if rows != each * seqs or max_rows not in (None, each):
             raise ValueError("without starts every sequence has rows / seqs rows")
-        max_rows = rows // seqs
+        max_rows = each
     prefix_pages = 0
     if prefix is not None:
         _need(prefix.dim() == 1, "prefix must be contiguous int32 [pages]")
@@ -737,6 +738,8 @@ def kv_attention(q, cache: KvCache, table, lengths, starts=None, max_rows: Optio
         else:
             y = out
             _, _, _, to, to_head = _heads_of(y, "out")
+        if seqs == 0:
+            return y         # (no row is of a sequence)
         size = lib.ec_kv_attention_workspace_bytes(C.byref(c), C.byref(cfg))
         ws, at = _workspace(torch, size, q.device)
         _done(lib, lib.ec_kv_attention(C.byref(c), C.byref(cfg), q.data_ptr(), ld, ld_head, table.data_ptr(), lengths.data_ptr(),
