@@ -335,7 +335,7 @@ struct KvAttention {
   bf16_t* out; size_t out_ld, out_head;
   int rows, heads, seqs, max_rows, max_keys;
   const int *table, *lengths, *starts;
-  int width; size_t table_ld;
+  size_t table_ld;
   const int* prefix; int prefix_len;
   bool causal;
   float scale;

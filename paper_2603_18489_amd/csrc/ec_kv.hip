@@ -41,7 +41,7 @@ int check_data(const ec_kv_cache* c) {
 KvAttention attention_of(const ec_kv_attention_cfg* a) {
   KvAttention k = {};
   k.rows = a->rows; k.heads = a->heads; k.seqs = a->seqs; k.max_rows = a->max_rows; k.max_keys = a->max_keys;
-  k.width = a->table_pages; k.table_ld = a->table_ld; k.prefix_len = a->prefix_len; k.causal = a->causal != 0; k.scale = a->scale;
+  k.table_ld = a->table_ld; k.prefix_len = a->prefix_len; k.causal = a->causal != 0; k.scale = a->scale;
   return k;
 }
 const char* attention_error(const ec_kv_cache* c, const ec_kv_attention_cfg* a) {

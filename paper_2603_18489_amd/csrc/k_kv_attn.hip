@@ -49,7 +49,7 @@ struct Args {
   bf16_t* out; size_t out_ld, out_head;
   int rows, heads, group, seqs, max_rows, max_keys, each;
   const int *table, *lengths, *starts;
-  int width; size_t table_ld;
+  size_t table_ld;
   const int* prefix; int prefix_len;
   bool causal;
   float scale;                       // with log2(e)
@@ -697,7 +697,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   else attend_few<ES, HD, QT, 4, true, false>(a, blockIdx.x, tiles, lds);
 }
 
-// The slices of a row of queries meet in their order (28 heads, 64 rows, 33 slices: 30 MB in 7.5 us): W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
+// The slices of a row of queries meet in their order (28 heads, 64 rows, 34 slices: 31 MB in 7.5 us): W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
 // lane's each, two at most, so that all of them are on their way at once.
 constexpr int kSlicesMax = 64;    // of the prefix, and of a sequence's own keys
 
@@ -848,7 +848,7 @@ void launch(const KvCache& c, const KvAttention& k, const Plan& p, void* workspa
   a.out = k.out; a.out_ld = k.out_ld; a.out_head = k.out_head;
   a.rows = k.rows; a.heads = k.heads; a.group = k.heads / c.kv_heads;
   a.seqs = k.seqs; a.max_rows = k.max_rows; a.max_keys = k.max_keys; a.each = k.max_rows;
-  a.table = k.table; a.lengths = k.lengths; a.starts = k.starts; a.width = k.width; a.table_ld = k.table_ld;
+  a.table = k.table; a.lengths = k.lengths; a.starts = k.starts; a.table_ld = k.table_ld;
   a.prefix = k.prefix; a.prefix_len = k.prefix_len; a.causal = k.causal; a.scale = k.scale * 1.4426950408889634f;
   a.lag = kLag / a.scale;
   a.low = a.scale > 1.f ? -std::nextafter(FLT_MAX / a.scale, 0.f) : -FLT_MAX;
