@@ -145,7 +145,7 @@ __device__ __forceinline__ float top_of_query(float lane_top) { return max_of_sw
 // The maximum m is a score, not yet scaled, and a probability 2^(s scale - m scale) takes one multiplication and addition with the rounded m scale.  That
 // is off from the exact one by up to 2^-24 of itself, for all keys alike, and cancels - but from a scaled maximum of 2^31 on by a factor of 2^128, which
 // is no number, or zero.  From 2^24 on (`far`) exponents are (s - m) scale instead, where a score near m leaves no rounding.  (16 x 1536 rows over 1536 keys:
-// 629 us without, 632 with; 16 x 34 rows: 34.6 and 35.4, in bfloat16 63.8 and 65.6.)
+// 629 us without, 632 with; 16 x 34 rows: 34.9 and 35.3, in bfloat16 63.9 and 65.9.)
 constexpr float kFar = 16777216.f;
 __device__ __forceinline__ bool far(float m, float scale) { return !(fabsf(m * scale) < kFar); }
 // the exponent by which what was added up with maximum m goes over to maximum m_new
@@ -361,7 +361,7 @@ __device__ __forceinline__ void attend_few(const Args& a, unsigned id, int tiles
         pl[t] = pack8(p);
       }
     }
-    if constexpr (QT == 3) __builtin_amdgcn_sched_barrier(0);   // (values that are widened ahead of this would be spilled)
+    if constexpr (QT == 3 && ES == 2) __builtin_amdgcn_sched_barrier(0);   // (values that are read ahead of this would be spilled)
 #pragma unroll
     for (int h = 0; h < HT; ++h) {
       bf16x8 vf;
