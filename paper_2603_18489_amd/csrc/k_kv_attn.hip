@@ -239,16 +239,17 @@ template <int ES, int HD> struct Chunk {
 // DIRECT: there is one slice, and the block writes the result.
 // 1 row over 131071 bfloat16 keys (28 heads on 4): 48 us, 5.7 TB/s.  16 sequences of up to 34 rows over up to 1536 e4m3 keys (32 heads): 32 us, 3 tiles,
 // as long as their bytes and products take one after the other.  1 row over 1000 keys: 8.2, a chain of loads.
-template <int HD, int QT, int W> struct Few {
+template <int HD, int QT> struct Few {
+  static constexpr int W = 4;                   // waves
   static constexpr int HB = HD / 32, HT = HD / 16;
   static constexpr int SLOT = HT * 64 + 32;     // float4 of a wave's part of a tile
   static constexpr bool PARKED = QT > 2;        // queries in LDS, as a third tile's registers would spill others
   static constexpr int LDS = W * SLOT + (PARKED ? QT * HB * 64 : 0);
 };
-template <int ES, int HD, int QT, int W, bool PREFIX, bool DIRECT>
+template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
 __device__ __forceinline__ void attend_few(const Args& a, unsigned id, int tiles, u32x4* mem) {
-  typedef Few<HD, QT, W> F;
-  constexpr int HB = F::HB, HT = F::HT, U = KvChunk<ES, HD>::kUnits, SLOT = F::SLOT;
+  typedef Few<HD, QT> F;
+  constexpr int W = F::W, HB = F::HB, HT = F::HT, U = KvChunk<ES, HD>::kUnits, SLOT = F::SLOT;
   constexpr bool PARKED = F::PARKED;
   typedef Chunk<ES, HD> C;
   float4* lds = (float4*)mem;
@@ -676,10 +677,10 @@ __device__ __forceinline__ void attend_many(const Args& a, unsigned id, int tile
   }
 }
 
-template <int ES, int HD, int QT, int W, bool PREFIX, bool DIRECT>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a) {
-  __shared__ u32x4 lds[Few<HD, QT, W>::LDS];
-  attend_few<ES, HD, QT, W, PREFIX, DIRECT>(a, blockIdx.x, 1, lds);
+template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_few_kernel(Args a) {
+  __shared__ u32x4 lds[Few<HD, QT>::LDS];
+  attend_few<ES, HD, QT, PREFIX, DIRECT>(a, blockIdx.x, 1, lds);
 }
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_many_kernel(Args a, int tiles) {
@@ -690,11 +691,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // blocks go first, as they take longer (64 rows of 28 heads on 4, 16384 keys before 511 each: 54 us in two launches, 46 in one, 55 the other way round).
 template <int ES, int HD, bool MANY, int QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv_attention_both_kernel(Args a, int tiles, unsigned prefix) {
-  constexpr int PRE = MANY ? kManyLds<HD> : Few<HD, QT, 4>::LDS, OWN = Few<HD, 1, 4>::LDS;
+  constexpr int PRE = MANY ? kManyLds<HD> : Few<HD, QT>::LDS, OWN = Few<HD, 1>::LDS;
   __shared__ u32x4 lds[PRE > OWN ? PRE : OWN];
-  if (blockIdx.x >= prefix) attend_few<ES, HD, 1, 4, false, false>(a, blockIdx.x - prefix, 1, lds);
+  if (blockIdx.x >= prefix) attend_few<ES, HD, 1, false, false>(a, blockIdx.x - prefix, 1, lds);
   else if constexpr (MANY) attend_many<ES, HD, QT, true, false>(a, blockIdx.x, tiles, lds);
-  else attend_few<ES, HD, QT, 4, true, false>(a, blockIdx.x, tiles, lds);
+  else attend_few<ES, HD, QT, true, false>(a, blockIdx.x, tiles, lds);
 }
 
 // The slices of a row of queries meet in their order (28 heads, 64 rows, 34 slices: 31 MB in 7.5 us): W waves take every W-th slice, a lane HD/64 components.  The slices' (m, sum) are a
@@ -790,8 +791,8 @@ Cut cut(long queries, int chunks, long others, bool joined) {
   }
   const long want = (c.many || c.qt > 1 ? kBlocks : kBlocksFew) / max(others * c.tiles, 1L);
   const long most = max(1, chunks / kSliceChunks);
-  // Up to 1024 keys are not cut for few queries: 8 waves of a block are through them in 8.2 us where slices and their meeting take 7.1, but the second
-  // launch costs the caller 4 (one row, 1000 keys, 28 heads on 4).
+  // Up to 1024 keys are not cut for few queries: a block is through them in 8.5 us where slices and their meeting take 7.1, but the second launch costs the
+  // caller 4 (one row, 1000 keys, 28 heads on 4).
   const int n = !c.many && !joined && chunks <= kUncut ? 1 : (int)max(1L, min(min(want, most), (long)kSlicesMax));
   c.split = (chunks + n - 1) / n;
   c.slices = (chunks + c.split - 1) / c.split;
@@ -826,10 +827,9 @@ void launch_cut(const Args& a, const Cut& c, hipStream_t s) {
     else if (c.qt == 2) kv_attention_many_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
     else kv_attention_many_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a, c.tiles);
   } else {
-    if (c.qt == 1 && DIRECT && blocks <= 256) kv_attention_few_kernel<ES, HD, 1, 8, PREFIX, DIRECT><<<(unsigned)blocks, 512, 0, s>>>(a);
-    else if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
-    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
-    else kv_attention_few_kernel<ES, HD, 3, 4, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
+    if (c.qt == 1) kv_attention_few_kernel<ES, HD, 1, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else if (c.qt == 2) kv_attention_few_kernel<ES, HD, 2, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
+    else kv_attention_few_kernel<ES, HD, 3, PREFIX, DIRECT><<<(unsigned)blocks, 256, 0, s>>>(a);
   }
 }
 
