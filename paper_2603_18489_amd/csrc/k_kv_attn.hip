@@ -768,13 +768,16 @@ struct Cut {
   bool many;
   int qt, tiles, split, slices;
 };
-constexpr int kBlocks = 512, kBlocksFew = 1024;   // blocks that fill the compute units: of many queries or several tiles, of one tile
-constexpr int kSliceChunks = 8, kUncut = 32;       // chunks of a slice at least; chunks that few queries' blocks take as one
+// Blocks that fill the compute units, and chunks of a slice at least.  (1 row over 20000 keys of 32 heads: 32.7 us, of 1024 blocks 34.5, of 256 33.2; 600 rows of 28 heads
+// on 4 over 9000: 113, 127 and 167; 64 over 16384 shared ones: 42, 51 and 46.  1 row of 28 heads on 4 over 4096 keys: 7.6 us, slices of 4 chunks 8.1, of 16 8.8.)
+constexpr int kBlocks = 512, kSliceChunks = 8;
+constexpr int kUncut = 32;     // chunks that few queries' blocks take as one
 Cut cut(long queries, int chunks, long others, bool joined) {
   Cut c;
   c.many = queries > 48;
   if (c.many) {
-    // by what a tile takes (16 x 1536 rows over 1536 keys: 911, 737 and 718 us in tiles of 64, 128 and 192) and how full the last one is
+    // by what a tile takes (16 x 1536 rows over 1536 keys: 820, 646 and 630 us in tiles of 64, 128 and 192, 492, 403 and 380 with 64 components; 64 x 128 rows 323,
+    // 264 and 353) and how full the last one is
     const double cost[3] = {1.29, 2 * 1.03, 3.0};
     double least = 0;
     for (int qt = 1; qt <= 3; ++qt) {
@@ -789,7 +792,7 @@ Cut cut(long queries, int chunks, long others, bool joined) {
     c.qt = (int)max(1L, (queries + 15) / 16);
     c.tiles = 1;
   }
-  const long want = (c.many || c.qt > 1 ? kBlocks : kBlocksFew) / max(others * c.tiles, 1L);
+  const long want = kBlocks / max(others * c.tiles, 1L);
   const long most = max(1, chunks / kSliceChunks);
   // Up to 1024 keys are not cut for few queries: a block is through them in 8.5 us where slices and their meeting take 7.1, but the second launch costs the
   // caller 4 (one row, 1000 keys, 28 heads on 4).
@@ -810,13 +813,11 @@ Plan plan_of(const KvCache& c, const KvAttention& a) {
 size_t part_bytes(const KvCache& c, size_t parts) { return (parts * c.head_dim * 4 + 255) / 256 * 256; }
 size_t parts_bytes(const KvCache& c, size_t parts) { return part_bytes(c, parts) + parts * sizeof(float2); }
 
-// Most parts that cut() can make of up to `heads` heads of rows, `queries` queries and `chunks` chunks, 0: they are never cut.  Of b blocks of
-// keys that are made at most, `others` x tiles x slices <= b where there are slices at all, so that there are b parts to a query of a tile: as many as 16 queries
-// of 1024 blocks, 48 or 192 of 512.
+// Most parts that cut() can make of up to `heads` heads of rows, `queries` queries and `chunks` chunks, 0: they are never cut.  Where there are slices at
+// all, `others` x tiles x slices are at most kBlocks, so that there are that many parts to a query of a tile, of which a tile has 192 at most.
 size_t most_parts(size_t heads, long queries, int chunks, bool joined) {
   const size_t slices = queries <= 48 && !joined && chunks <= kUncut ? 1 : max(1, min(chunks / kSliceChunks, kSlicesMax));
-  const long few = min(queries, 16L) * kBlocksFew, more = queries > 16 ? min(queries, 192L) * kBlocks : 0;
-  return slices == 1 ? 0 : min(heads * slices, (size_t)max(few, more));
+  return slices == 1 ? 0 : min(heads * slices, (size_t)min(queries, 192L) * kBlocks);
 }
 
 template <int ES, int HD, bool PREFIX, bool DIRECT>
