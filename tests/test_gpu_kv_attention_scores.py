@@ -1,5 +1,5 @@
 """Scores that are far from zero, where one rounding of the scaled maximum is many units of the exponent: every product and sum of the scores here is
-exact in float32, so that the definition in 64 bits holds however large they are."""
+exact in float32, so that the definition in 64 bits holds however large they are.  Scores that are infinite."""
 import numpy as np
 import pytest
 import torch
@@ -17,7 +17,7 @@ SHAPES = [  # rows and keys of the sequences, heads, kv heads, head dim, page, p
 
 
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
-@pytest.mark.parametrize("scale", [2.0 ** -30, 2.0 ** -10, 2.0 ** -7, 1.0, 2.0 ** 20, 1e30])
+@pytest.mark.parametrize("scale", [1e-40, 2.0 ** -30, 2.0 ** -10, 2.0 ** -7, 1.0, 2.0 ** 20, 1e30])
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
 def test_scores_far_from_zero(shape, scale, cache):
     counts, lengths, heads, kv_heads, hd, page, prefix = shape
@@ -57,3 +57,38 @@ def test_scores_far_from_zero(shape, scale, cache):
                 bound = e * spread + HALF["bf16"] * (np.abs(want) + e * spread) + 1e-38
                 far = np.abs(out[r, h] - want)
                 assert (far <= bound).all(), (i, r, h, m[r, h], (far / bound).max(), out[r, h][:4], want[:4])
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_infinite_scores(shape, cache):
+    """a query with scores of +infinity is NaN, one with -infinity alone zeros, and the others of its tile stay right"""
+    counts, lengths, heads, kv_heads, hd, page, prefix = shape
+    b = Batch(counts, lengths, heads, kv_heads, hd, page, cache, prefix, seed=5)
+    keys = [np.concatenate((b.k[-1], x)) for x in b.k[:-1]]
+    clean = b.call()
+    b.check(clean)
+    for value in (float("inf"), float("-inf")):
+        q = b.q.clone()
+        of = [(int(b.starts[i]), i) for i in range(len(counts))]       # the first row's last head of each sequence
+        for r, _ in of:
+            q[r, heads - 1, 3] = value
+        out = b.call(q=q)
+        for r, i in of:
+            s = (value * np.sign(keys[i][:, kv_heads - 1, 3]))
+            got = out[r, heads - 1]
+            if len(s) and (np.isnan(s).any() or s.max() == np.inf):
+                assert torch.isnan(got).all()
+            else:
+                assert (got == 0).all()
+            out[r, heads - 1] = clean[r, heads - 1]
+        b.check(out)
+    # all keys on one side
+    k, v = (t.clone() for t in ec.kv_read(b.cache, b.every, torch.float32))
+    k[..., 3] = -k[..., 3].abs() - 0.25
+    ec.kv_write(b.cache, k, v, b.every)
+    q = torch.zeros_like(b.q)
+    q[..., 3] = float("inf")
+    assert (b.call(q=q) == 0).all()
+    q[..., 3] = float("-inf")
+    assert torch.isnan(b.call(q=q)[[int(b.starts[i]) for i in range(len(counts)) if prefix + lengths[i]]]).all()
