@@ -451,14 +451,18 @@ static KvRows rows_of(const KvCache& c, const void* k, const void* v, bool bf16,
 
 // Blocks that share a tile of rows: as many as there are heads for, four to a block, up to `most` blocks in all; where few are made, some beside each
 // other share the tile's rows too.  A block that writes goes through the rows behind its own for such that name the same slot: 24576 rows of 32 heads are
-// written by 768 blocks of all heads in 152 us, by 1536 of half in 155, by 3840 in 189; read by 768 in 130, by 6144 in 122.
+// written by 768 blocks of all heads in 152 us, by 1536 of half in 155, by 3840 in 189; read by 768 in 130, by 6144 in 122.  (That is rows times rows, which many rows
+// feel: 131071 of 4 heads are written in 274 us, in four calls of a quarter in 187; 2^20 of one head in 11.0 ms, in 32 calls in 1.1.)
+// Up to kSpread blocks have `turns` times as many, of a part of the rows each: 34 rows here and there of 32 heads are written in 8.3 us instead of 13.9 and read in 4.7
+// instead of 9.5; of 376 blocks (1500 rows) writing takes 18.2 instead of 17.2 and reading 9.0 instead of 9.8, of 752 (3000 rows) 31.8 instead of 21.3 and 13.0 instead of 13.8.
+constexpr int kSpread = 512;
 static int kv_blocks(int tiles, int heads, int most) { return min((heads + 3) / 4, max(1, most / tiles)); }
 
 #define EC_KV_LAUNCH(KERNEL, MOST, T, ES, HD)                                                                            \
   do {                                                                                                                   \
     constexpr int turns = kTileRows<HD> * (HD / 16) / 64;                                                                \
     const int tiles = (rows + kTileRows<HD> - 1) / kTileRows<HD>, y = kv_blocks(tiles, c.kv_heads, MOST);                 \
-    if (tiles * y <= 512) KERNEL<T, ES, HD, true><<<dim3(tiles, y, turns), 256, 0, s>>>(a);                              \
+    if (tiles * y <= kSpread) KERNEL<T, ES, HD, true><<<dim3(tiles, y, turns), 256, 0, s>>>(a);                              \
     else KERNEL<T, ES, HD, false><<<dim3(tiles, y), 256, 0, s>>>(a);                                                     \
   } while (0)
 #define EC_KV_PICK(KERNEL, MOST)                                                                      \

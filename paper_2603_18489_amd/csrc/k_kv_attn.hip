@@ -6,7 +6,8 @@
 //   S^T[keys x queries] = K . Q^T, softmax down the keys, O^T[components x queries] += V^T . P^T
 // with the operands as they lie in the cache.  e4m3 keys are widened to bfloat16 with their power of two, exactly.  Values are widened
 // so too where many queries share them; few queries' probabilities take it instead, an exact product again, before they are rounded to bfloat16 (2^-8 of them
-// at most, 2^-16 with up to 16 queries).  Scores, maxima and sums are float32.
+// at most, 2^-16 with up to 16 queries).  Scores, maxima and sums are float32.  One part of a probability is off by less than the result's own rounding: together 0.0019 to
+// 0.0022 of the result, where the result's rounding alone is 0.0017.  A second part for more than 16 queries too would take 16 x 34 rows from 36.8 to 40.0 us, 16 x 1536 from 624 to 826.
 //
 // Keys are cut into slices of chunks, a block each; the slices' (m, sum, O) meet in a second launch, in their order.  The prefix' slices take
 // the rows of all sequences at once, so that its keys are read once for all.  A query that sees no key gets zeros: m begins so low
@@ -237,8 +238,8 @@ template <int ES, int HD> struct Chunk {
 // queries leaves registers for a second chunk.  The power of two of a key's values multiplies its probability.
 // With one tile the matrix cores wait for memory, so that a probability can be two bfloat16 numbers, 2^-16 together, instead of one.
 // DIRECT: there is one slice, and the block writes the result.
-// 1 row over 131071 bfloat16 keys (28 heads on 4): 48 us, 5.7 TB/s.  16 sequences of up to 34 rows over up to 1536 e4m3 keys (32 heads): 32 us, 3 tiles,
-// as long as their bytes and products take one after the other.  1 row over 1000 keys: 8.2, a chain of loads.
+// 1 row over 131071 bfloat16 keys (28 heads on 4): 48 us, 5.7 TB/s.  16 sequences of up to 34 rows over up to 1536 e4m3 keys (32 heads): 33 us, 3 tiles,
+// as long as their bytes and products take one after the other.  1 row over 1000 keys: 8.5, a chain of loads.
 template <int HD, int QT> struct Few {
   static constexpr int W = 4;                   // waves
   static constexpr int HB = HD / 32, HT = HD / 16;
@@ -480,8 +481,8 @@ __device__ __forceinline__ void widen_values(u32x4 v, u32x2 vs, u32x4& x, u32x4&
 // Many queries: a wave owns QT tiles of 16, a block 64 QT, and its waves go through the keys together.  Each chunk comes through registers, where codes
 // are widened once for all, values with their powers of two, into one of two stages of LDS; the next one's pieces are on their way meanwhile.  The
 // probabilities' sums are a product of P^T with ones: what is rounded is what is added up.
-// 16 x 1536 rows over 1536 e4m3 keys, 32 heads of 128: 645 to 720 us, 0.86 to 0.96 PFLOP/s.  What bounds it is the issue of instructions: a 16 x 16 x 32 product
-// takes a SIMD 17 cycles, beside which one more instruction is free, and softmax and widening add theirs.
+// 16 x 1536 rows over 1536 e4m3 keys, 32 heads of 128: 620 to 640 us, 0.97 to 1.0 PFLOP/s.  What bounds it is the issue of instructions: the matrix cores are at work in 43 % of
+// the cycles, and the other vector instructions, of softmax and widening, 3.6 to a product, issue in 43 % too, of which two waves a SIMD hide little behind products.
 // Chunks that hold a key which some query does not see, or values that are NaN, go a slower way; the others' code has one rare branch.
 template <int HD> constexpr int kManyLds = 2 * (2 * HD / 32 + HD / 16) * 64;
 template <int ES, int HD, int QT, bool PREFIX, bool DIRECT>
