@@ -487,7 +487,8 @@ int ec_kv_read(const ec_kv_cache *cache, const int32_t *slots, int32_t rows, voi
  * sees no key, or scores of -infinity alone, gets zeros, and keys that it does not see are without effect, NaN among them.  Probabilities are
  * rounded to bfloat16, as operands of matrix products: of a sequence's own keys in two parts, 2^-16 together, where max_rows group <= 16; of the prefix'
  * keys, whose queries are the rows of the whole call, where rows group <= 16; in one part, 2^-8, elsewhere.  Everything else is held in float32 and
- * the result rounded to bfloat16. The sums are of p_j v_j with p_j up to 256 and have to fit float32: magnitudes of v from 2^100 on may overflow.
+ * the result rounded to bfloat16.  The sums are of p_j v_j with p_j up to 256 and have to fit float32: magnitudes of v from 2^100 on may overflow, and
+ * as operands of bfloat16 products, magnitudes of v below 2^-100 and of k below 2^-126 count with fewer bits or as 0.
  * Kept inside the buffers whatever the tables hold: starts are clamped to [0, rows] (and must ascend: no row is of two sequences), a sequence's rows beyond
  * max_rows (which n does not count) and rows of no sequence are left as they were, lengths are clamped to [0, max_keys], and the tokens of a page outside [0, pages) are not seen.
  * A prefix is for sequences of few rows each: with one, every head of a row goes through the workspace in float32, twice or more.  Sequences of many rows are
