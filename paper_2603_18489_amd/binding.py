@@ -554,7 +554,7 @@ def _heads_of(x, what: str):
     ld, ld_head, one = x.stride()
     if rows > _INT_MAX or heads > _INT_MAX or dim > _INT_MAX:
         raise ValueError("at most 2^31 - 1 rows, heads and components")
-    if one != 1 and dim > 1:
+    if one != 1 and dim > 1 and rows > 0:
         raise ValueError("the components of a head must be next to each other")
     return rows, heads, dim, ld if rows > 1 else 0, ld_head if heads > 1 else 0
 

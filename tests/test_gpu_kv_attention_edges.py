@@ -47,3 +47,12 @@ def test_starts_and_lengths_that_are_none(counts, most, prefix, cache):
             got[32:32 + rows, 1:5, 16:144] = 7
             assert (got == 7).all(), (starts, lengths)
             assert (inside[~named] == 7).all() and (inside[named] != 7).any(axis=(1, 2)).all(), (starts, lengths)
+
+
+def test_no_rows_of_any_strides():
+    none = torch.from_numpy(np.ones((0, 2, 64), dtype=np.float32)).cuda()
+    cache, plan = ec.kv_cache(3, 2, 64, 32), ec.rotary_plan(64)
+    ec.kv_write(cache, none, none, ints([]))
+    assert (cache.data == 0).all()
+    assert ec.rotary(none, ints([]), plan).shape == (0, 2, 64)
+    assert ec.kv_attention(none.bfloat16(), cache, ints([[0]]), ints([5])).shape == (0, 2, 64)
